@@ -439,6 +439,62 @@ accerl_status accerl_tc_probe_i8(int32_t device, int32_t n, int32_t issuing_warp
                                  int32_t a_shift_rows, int32_t commit_every, float *ms_out,
                                  float *cycles_per_mma_out);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators of the Learner's side for policies over tokens (and over anything else whose rows are
+ * states).  They take no handle: every array is the caller's, device memory of the current device,
+ * and lives until the stream has passed the call.  Calls on different streams, or captured into
+ * different graphs, share nothing but what their arguments share.  `ld_...` is the distance of two
+ * rows in elements, at least the row's length.
+ * ------------------------------------------------------------------------------------------ */
+
+typedef enum { ACCERL_F32 = 0, ACCERL_BF16 = 1, ACCERL_F16 = 2 } accerl_dtype;
+
+/*
+ * Clipped policy loss with a KL and an entropy term over rows of logits, and its gradient: the
+ * Learner's step on what the Actors sampled (Section 2.3, Eq. IS: the ratio of the current to the
+ * behaviour policy, clipped; Section 2.2, Eq. KD: KL to another policy and an entropy bonus).
+ * Per row t with z its logits, a its action, logp = z_a - logsumexp(z), p = softmax(z):
+ *   r    = exp(logp - logp_old)
+ *   pg   = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)
+ *   kl   = sum_v p_v (log p_v - log q_v), q the softmax of logits_ref; or, with logp_ref,
+ *          exp(logp_ref - logp) - (logp_ref - logp) - 1 of the action taken; or 0 with neither
+ *   H    = -sum_v p_v log p_v
+ *   loss = sum_t w_t (pg + kl_coef kl - entropy_coef H)
+ * and grad[t][v] = d loss / d z[t][v].  At r A = clamp(r) A the gradient is the unclipped branch's.
+ * A row of weight 0 is not read: its grad, logp, kl and entropy are 0, whatever its arrays hold.  A logit of
+ * -inf has probability 0, takes no part in the sums and gets gradient 0; a row that has no other logits counts
+ * as loss 0 and gets gradient 0 and logp -inf.  Where p_v > 0 = q_v the KL is infinite and the gradient is not
+ * finite.  An action outside 0..n_actions-1 makes its row NaN.
+ */
+typedef struct {
+    const void *logits;      /* [rows][n_actions] of `dtype` */
+    const void *logits_ref;  /* the same of the reference policy, or NULL */
+    const void *actions;     /* [rows] int32_t, or int64_t where actions64 */
+    const float *logp_old;   /* [rows] */
+    const float *advantages; /* [rows] */
+    const float *logp_ref;   /* [rows] or NULL; not together with logits_ref */
+    const float *weights;    /* [rows], or NULL: 1 / rows for every row */
+    int64_t ld_logits, ld_logits_ref, ld_grad;
+    int32_t rows, n_actions; /* n_actions in 1 .. 262128 */
+    int32_t dtype;           /* accerl_dtype of logits, logits_ref and grad */
+    int32_t actions64;
+    float clip_low, clip_high, kl_coef, entropy_coef; /* clips in [0, inf], coefficients finite */
+    void *grad;     /* [rows][n_actions] of `dtype`, may be `logits` itself (with the same ld); NULL: no gradient */
+    float *logp;    /* [rows] */
+    float *kl;      /* [rows] */
+    float *entropy; /* [rows] */
+    float *stats;   /* [8]: loss, then the sums over t of w_t times pg, kl, H, (1 where the clamp decided); then
+                       sum w, the largest kl of a row of non-zero weight, sum w r */
+    float *terms;   /* [rows][2]: pg and r of the row (workspace of the sums; 8-byte aligned) */
+} accerl_policy_loss_args;
+
+/*
+ * Asynchronous on `cuda_stream`; one or two launches, no host synchronisation.  Sums over rows are taken in a
+ * fixed order: the same call gives the same bits.
+ * Errors: INVALID_ARG (null or misaligned pointer, sizes, coefficients), CUDA.
+ */
+accerl_status accerl_policy_loss(const accerl_policy_loss_args *args, void *cuda_stream);
+
 /*
  * Free the handle and its device memory.  Synchronises the device.  NULL is allowed.  Up to 512 MB of such
  * memory per process, and 64 MB of pinned host memory, stay with the library for the next policy (building one

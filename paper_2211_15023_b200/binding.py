@@ -85,6 +85,7 @@ def library() -> C.CDLL:
         lib.accerl_policy_selftest_wait.restype = C.c_int
         lib.accerl_tc_probe_i8.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32, C.POINTER(f32), C.POINTER(f32)]
         lib.accerl_tc_probe_i8.restype = C.c_int
+        lib.accerl_policy_loss.argtypes, lib.accerl_policy_loss.restype = [C.POINTER(PolicyLossArgs), vp], C.c_int
         lib.accerl_policy_destroy.argtypes = [vp]
         lib.accerl_policy_destroy.restype = None
         lib.accerl_trim.argtypes, lib.accerl_trim.restype = [], None
@@ -221,6 +222,108 @@ def act_mixed(smaller, original, obs, uniforms, select_uniforms, alpha, stream=N
         float(alpha), b, out["logits"].data_ptr(), out["actions"].data_ptr(), out["logp"].data_ptr(),
         out["value"].data_ptr() if "value" in out else None, out["entropy"].data_ptr(),
         out["use_smaller"].data_ptr(), _stream_of(obs, stream)))
+    return out
+
+
+# -- operators of the Learner's side ---------------------------------------------------------------
+_DTYPES = ("float32", "bfloat16", "float16")  # in the order of accerl_dtype
+
+
+class PolicyLossArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("logits", "logits_ref", "actions", "logp_old", "advantages", "logp_ref",
+                                          "weights")] + \
+        [(n, C.c_int64) for n in ("ld_logits", "ld_logits_ref", "ld_grad")] + \
+        [(n, C.c_int32) for n in ("rows", "n_actions", "dtype", "actions64")] + \
+        [(n, C.c_float) for n in ("clip_low", "clip_high", "kl_coef", "entropy_coef")] + \
+        [(n, C.c_void_p) for n in ("grad", "logp", "kl", "entropy", "stats", "terms")]
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _dtype_code(dtype):
+    import torch
+    for i, n in enumerate(_DTYPES):
+        if dtype is getattr(torch, n):
+            return i
+    raise AssertionError("dtype %s is none of %s" % (dtype, ", ".join(_DTYPES)))
+
+
+def _check_rows(t, like=None, dtype=None):
+    """A CUDA matrix whose rows lie one after another (any distance between them); on the device of `like`."""
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and \
+        (t.stride(0) >= t.shape[1] or t.shape[0] == 1), "rows of a CUDA matrix, the elements of a row adjacent"
+    assert like is None or t.device == like.device, "tensors on different devices"
+    assert dtype is None or t.dtype == dtype, "expected %s" % dtype
+
+
+def _ld(t):
+    """Distance of two rows (torch leaves the stride of a single row open)."""
+    return t.stride(0) if t.shape[0] > 1 else max(int(t.shape[1]), t.stride(0))
+
+
+def _check_vector(t, n, like, *dtypes):
+    assert t.is_cuda and t.device == like.device and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and \
+        t.dtype in dtypes, "a contiguous CUDA vector of %d %s" % (n, " or ".join(map(str, dtypes)))
+
+
+class _on_device_of:
+    """Makes the device of a tensor the current one, where it is not."""
+
+    def __init__(self, t):
+        import torch
+        self.guard = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+    def __enter__(self):
+        if self.guard:
+            self.guard.__enter__()
+
+    def __exit__(self, *a):
+        if self.guard:
+            self.guard.__exit__(*a)
+
+
+def policy_loss(logits, actions, logp_old, advantages, weights=None, logits_ref=None, logp_ref=None, clip=0.2,
+                kl_coef=0.0, entropy_coef=0.0, grad=True, stream=None) -> dict:
+    """accerl_policy_loss on CUDA rows of logits [T, A] (fp32, bf16 or fp16).
+
+    ``actions`` int32 or int64 [T]; ``logp_old``, ``advantages``, ``weights`` (None: 1 / T each), ``logp_ref`` fp32 [T];
+    ``logits_ref`` like ``logits``; ``clip`` a number or (low, high).  ``grad``: True for a new tensor, a tensor to write
+    (``logits`` itself among them), False for none.  Returns dict(stats [8], logp [T], kl [T], entropy [T], grad):
+    ``stats`` holds the loss, the weighted sums of the clipped objective, KL, entropy and clipped rows, the sum of
+    weights, the largest KL and the weighted sum of ratios.
+    """
+    import torch
+    low, high = clip if isinstance(clip, (tuple, list)) else (clip, clip)
+    code = _dtype_code(logits.dtype)
+    _check_rows(logits)
+    t, v = int(logits.shape[0]), int(logits.shape[1])
+    if logits_ref is not None:
+        _check_rows(logits_ref, logits, logits.dtype)
+        assert logits_ref.shape == logits.shape
+    _check_vector(actions, t, logits, torch.int32, torch.int64)
+    for x in (logp_old, advantages, weights, logp_ref):
+        if x is not None:
+            _check_vector(x, t, logits, torch.float32)
+    assert logp_old is not None and advantages is not None
+    dev = logits.device
+    if grad is True:
+        grad = torch.empty_strided(logits.shape, (_ld(logits), 1), dtype=logits.dtype, device=dev)
+    elif grad is False:
+        grad = None
+    if grad is not None:
+        _check_rows(grad, logits, logits.dtype)
+        assert grad.shape == logits.shape
+    f = torch.empty(8 + 5 * t, dtype=torch.float32, device=dev)
+    out = dict(stats=f[:8], logp=f[8 + 2 * t:8 + 3 * t], kl=f[8 + 3 * t:8 + 4 * t], entropy=f[8 + 4 * t:], grad=grad)
+    a = PolicyLossArgs(_ptr(logits), _ptr(logits_ref), _ptr(actions), _ptr(logp_old), _ptr(advantages), _ptr(logp_ref),
+                       _ptr(weights), _ld(logits), 0 if logits_ref is None else _ld(logits_ref),
+                       0 if grad is None else _ld(grad), t, v, code, int(actions.dtype == torch.int64), float(low),
+                       float(high), float(kl_coef), float(entropy_coef), _ptr(grad), _ptr(out["logp"]),
+                       _ptr(out["kl"]), _ptr(out["entropy"]), _ptr(f), _ptr(f[8:]))
+    with _on_device_of(logits):
+        _check(library().accerl_policy_loss(C.byref(a), _stream_of(logits, stream)))
     return out
 
 

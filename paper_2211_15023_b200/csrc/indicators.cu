@@ -10,6 +10,7 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
+#include "exp64.cuh"
 #include "internal.h"
 
 namespace accerl {
@@ -41,24 +42,6 @@ __device__ __forceinline__ float warp_maxf(float v)
 // the indicator runs at the Monitor's interval, not per environment step.  With e_i = exp(zo_i - mo),
 //   KL = sum_i e_i / so (zo_i - zs_i) - (lse_o - lse_s),
 // two exponentials an action instead of three, and identical rows give exactly 0.
-
-// exp(x) for x <= 0 by table and a short polynomial (Tang, "Table-driven implementation of the exponential
-// function", 1989): x = (64 m + j) ln2 / 64 + r, |r| <= ln2 / 128, exp(x) = 2^m 2^(j/64) (1 + r + ... + r^5 / 120);
-// the truncation is below 3e-17, the result within about one ulp.  `table` holds 2^(j/64).  It has half the
-// instructions of exp(), of which the rows kernel needs two per action (16 x 8192 rollouts of 18 actions,
-// V-trace and both launches of the KL, rows copied element by element as they were then: 27 us with exp(), 24.6 with this).
-__device__ __forceinline__ double exp_nonpositive(double x, const double *table)
-{
-    const double shift = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to an integer
-    const double t = fma(x, 92.332482616893656, shift), nf = t - shift;
-    const int n = __double2loint(t);
-    const double r = fma(nf, -3.623510646634843e-19, fma(nf, -0.010830424696249145, x));
-    const double p = fma(r * r, fma(r, fma(r, fma(r, 1.0 / 120.0, 1.0 / 24.0), 1.0 / 6.0), 0.5), r);
-    const double v = fma(table[n & 63], p, table[n & 63]);
-    const double y = __hiloint2double(__double2hiint(v) + ((n >> 6) << 20), __double2loint(v));
-    // What underflows is nothing beside the row's largest term; the last case is a NaN.
-    return x >= -708.0 ? y : x < 0.0 ? 0.0 : x;
-}
 
 // One row by one thread, V elements a load (then the row's address is a multiple of V elements and A one of V);
 // the elements are added in order whatever V is.
@@ -172,7 +155,7 @@ kl_rows_kernel(const float *__restrict__ zo, const float *__restrict__ zs, int B
     extern __shared__ __align__(16) float s_rows[];  // [2][kKlRows][pitch]
     __shared__ double s_table[64];
     if (STATS) cluster_started();
-    if (threadIdx.x < 64) s_table[threadIdx.x] = exp2((double)threadIdx.x * (1.0 / 64.0));
+    fill_exp_table(s_table);
     double sum = 0.0;
     float mx = -INFINITY;
     for (long long row0 = (long long)blockIdx.x * kKlRows; row0 < B; row0 += (long long)gridDim.x * kKlRows) {

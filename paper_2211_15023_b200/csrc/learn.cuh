@@ -1,0 +1,117 @@
+// What the Learner's operators share: element types, 16-byte pieces of rows, argument checks.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "internal.h"
+
+namespace accerl {
+
+inline int dtype_size(int dtype) { return dtype == ACCERL_F32 ? 4 : 2; }
+inline bool good_dtype(int dtype) { return dtype == ACCERL_F32 || dtype == ACCERL_BF16 || dtype == ACCERL_F16; }
+
+// Calls f with a value of the element type that `dtype` names.
+template <typename F>
+inline auto with_dtype(int dtype, F &&f)
+{
+    if (dtype == ACCERL_BF16) return f(__nv_bfloat16());
+    if (dtype == ACCERL_F16) return f(__half());
+    return f(float());
+}
+
+// 16 bytes of a row: kVec elements
+template <typename T>
+struct Row {
+    static constexpr int kVec = 16 / (int)sizeof(T);
+};
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+// two elements of a 32-bit word (one for float: `b` is not written)
+__device__ __forceinline__ void unpack_word(uint32_t w, float *v, const float *) { v[0] = __uint_as_float(w); }
+__device__ __forceinline__ void unpack_word(uint32_t w, float *v, const __nv_bfloat16 *)
+{
+    v[0] = __uint_as_float(w << 16);
+    v[1] = __uint_as_float(w & 0xffff0000u);
+}
+__device__ __forceinline__ void unpack_word(uint32_t w, float *v, const __half *)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    v[0] = f.x;
+    v[1] = f.y;
+}
+__device__ __forceinline__ uint32_t pack_word(const float *v, const float *) { return __float_as_uint(v[0]); }
+__device__ __forceinline__ uint32_t pack_word(const float *v, const __nv_bfloat16 *)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t pack_word(const float *v, const __half *)
+{
+    const __half2 h = __floats2half2_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4 &raw, float (&v)[Row<T>::kVec])
+{
+    constexpr int E = Row<T>::kVec / 4;
+    unpack_word(raw.x, v, (const T *)nullptr);
+    unpack_word(raw.y, v + E, (const T *)nullptr);
+    unpack_word(raw.z, v + 2 * E, (const T *)nullptr);
+    unpack_word(raw.w, v + 3 * E, (const T *)nullptr);
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float (&v)[Row<T>::kVec])
+{
+    constexpr int E = Row<T>::kVec / 4;
+    return make_uint4(pack_word(v, (const T *)nullptr), pack_word(v + E, (const T *)nullptr),
+                      pack_word(v + 2 * E, (const T *)nullptr), pack_word(v + 3 * E, (const T *)nullptr));
+}
+
+// Elements first .. first + kVec of a row of n, those outside it `fill`.  `whole`: the address of element `first` is
+// a multiple of 16 bytes, so that a piece inside the row is one load.
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const T *row, int first, int n, bool whole, float fill)
+{
+    constexpr int V = Row<T>::kVec;
+    if (whole && first >= 0 && first + V <= n) return __ldcs(reinterpret_cast<const uint4 *>(row + first));
+    float v[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = first + k >= 0 && first + k < n ? to_float(row[first + k]) : fill;
+    return pack<T>(v);
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T *row, int first, int n, bool whole, const float (&v)[Row<T>::kVec])
+{
+    constexpr int V = Row<T>::kVec;
+    if (whole && first >= 0 && first + V <= n) {
+        *reinterpret_cast<uint4 *>(row + first) = pack<T>(v);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        if (first + k >= 0 && first + k < n) row[first + k] = from_float<T>(v[k]);
+}
+
+// elements of type T by which an address lies behind a multiple of 16 bytes
+template <typename T>
+__device__ __forceinline__ int phase_of(const T *p)
+{
+    return (int)(((uintptr_t)p & 15) / sizeof(T));
+}
+
+}  // namespace accerl
