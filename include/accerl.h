@@ -495,6 +495,36 @@ typedef struct {
  */
 accerl_status accerl_policy_loss(const accerl_policy_loss_args *args, void *cuda_stream);
 
+/* Activations between the layers of a policy, for the checkpoints below */
+typedef enum { ACCERL_ACT_NONE = 0, ACCERL_ACT_RELU = 1, ACCERL_ACT_GELU = 2, ACCERL_ACT_SILU = 3 } accerl_activation;
+
+/*
+ * Activation checkpoints in 8 bits: what a layer's backward pass needs of its input, at a half (a quarter for fp32)
+ * of its size.  Every 32 values along a row (the last block of a row may be shorter) share a power of two: with
+ * e = max(1, biased exponent for which |q| <= 127 just holds) a value is kept as
+ *   q = rint(x / 2^(e - 127)),  |q| <= 127,   x^ = q 2^(e - 127),
+ * off by at most 2^-7 of the block's largest value (half a step of 2^-6).  x^ is a bf16 value, so the products of the
+ * backward pass that read it lose nothing further.  A block that holds an infinity or a NaN is kept as e = 255,
+ * q = 0, and all its values read back as NaN.
+ *   q   int8_t [rows][ld_q], e uint8_t [rows][ld_e]; with cols32 = cols rounded up to 32: ld_q >= cols32 and a
+ *       multiple of 16, ld_e >= cols32 / 32, q aligned to 16 bytes.  Columns cols .. cols32 of q are written as 0.
+ *
+ * accerl_ckpt_save          y = act(x) (y may be x itself, or NULL), and the checkpoint of x, in one pass
+ * accerl_ckpt_load          x = x^
+ * accerl_ckpt_act_backward  dx = dy act'(x^) (dx may be dy itself); relu'(0) = 0, GELU is x Phi(x)
+ * Results are computed in fp32 and rounded once to `dtype` (an accerl_dtype; the same for both arrays of a call).
+ * GELU's Phi has an absolute error below 3e-7.
+ * Asynchronous on `cuda_stream`, one launch.  Errors: INVALID_ARG, CUDA.
+ */
+accerl_status accerl_ckpt_save(const void *x_dev, int64_t ld_x, int32_t dtype, int64_t rows, int32_t cols, int32_t act,
+                               void *y_dev, int64_t ld_y, int8_t *q_dev, int64_t ld_q, uint8_t *e_dev, int64_t ld_e,
+                               void *cuda_stream);
+accerl_status accerl_ckpt_load(const int8_t *q_dev, int64_t ld_q, const uint8_t *e_dev, int64_t ld_e, int64_t rows,
+                               int32_t cols, void *x_dev, int64_t ld_x, int32_t dtype, void *cuda_stream);
+accerl_status accerl_ckpt_act_backward(const void *dy_dev, int64_t ld_dy, int32_t dtype, const int8_t *q_dev,
+                                       int64_t ld_q, const uint8_t *e_dev, int64_t ld_e, int64_t rows, int32_t cols,
+                                       int32_t act, void *dx_dev, int64_t ld_dx, void *cuda_stream);
+
 /*
  * Free the handle and its device memory.  Synchronises the device.  NULL is allowed.  Up to 512 MB of such
  * memory per process, and 64 MB of pinned host memory, stay with the library for the next policy (building one

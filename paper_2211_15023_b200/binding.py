@@ -86,6 +86,12 @@ def library() -> C.CDLL:
         lib.accerl_tc_probe_i8.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32, C.POINTER(f32), C.POINTER(f32)]
         lib.accerl_tc_probe_i8.restype = C.c_int
         lib.accerl_policy_loss.argtypes, lib.accerl_policy_loss.restype = [C.POINTER(PolicyLossArgs), vp], C.c_int
+        i64 = C.c_int64
+        lib.accerl_ckpt_save.argtypes = [vp, i64, i32, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp]
+        lib.accerl_ckpt_load.argtypes = [vp, i64, vp, i64, i64, i32, vp, i64, i32, vp]
+        lib.accerl_ckpt_act_backward.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i32, i32, vp, i64, vp]
+        for f in ("ckpt_save", "ckpt_load", "ckpt_act_backward"):
+            getattr(lib, "accerl_" + f).restype = C.c_int
         lib.accerl_policy_destroy.argtypes = [vp]
         lib.accerl_policy_destroy.restype = None
         lib.accerl_trim.argtypes, lib.accerl_trim.restype = [], None
@@ -324,6 +330,76 @@ def policy_loss(logits, actions, logp_old, advantages, weights=None, logits_ref=
                        _ptr(out["kl"]), _ptr(out["entropy"]), _ptr(f), _ptr(f[8:]))
     with _on_device_of(logits):
         _check(library().accerl_policy_loss(C.byref(a), _stream_of(logits, stream)))
+    return out
+
+
+_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def _check_ckpt(ckpt, rows, cols, like):
+    """(q int8 [rows, >= cols32], e uint8 [rows, >= cols32 / 32]) as ckpt_save makes them."""
+    import torch
+    q, e = ckpt
+    cols32 = -(-cols // 32) * 32
+    _check_rows(q, like, torch.int8)
+    _check_rows(e, like, torch.uint8)
+    assert q.shape[0] == e.shape[0] == rows and q.shape[1] >= cols32 and e.shape[1] >= cols32 // 32, \
+        "a checkpoint of %d rows of %d" % (rows, cols)
+    return q, e
+
+
+def ckpt_save(x, act="none", out=None, stream=None):
+    """accerl_ckpt_save of CUDA rows x [T, K] (fp32, bf16, fp16): returns (y, (q, e)) with y = act(x), act one of "none"
+    (y is x), "relu", "gelu", "silu".  ``out``: where to write y, x itself among the choices.  The checkpoint is
+    q int8 [T, K32], e uint8 [T, K32 / 32], K32 = K rounded up to 32."""
+    import torch
+    code = _dtype_code(x.dtype)
+    _check_rows(x)
+    t, k = int(x.shape[0]), int(x.shape[1])
+    k32 = -(-k // 32) * 32
+    q = torch.empty((t, k32), dtype=torch.int8, device=x.device)
+    e = torch.empty((t, k32 // 32), dtype=torch.uint8, device=x.device)
+    if out is not None:
+        _check_rows(out, x, x.dtype)
+        assert out.shape == x.shape
+    y = out if out is not None else x if act == "none" else torch.empty((t, k), dtype=x.dtype, device=x.device)
+    with _on_device_of(x):
+        _check(library().accerl_ckpt_save(_ptr(x), _ld(x), code, t, k, _ACTS[act],
+                                          None if act == "none" and out is None else _ptr(y), _ld(y), _ptr(q), k32, _ptr(e),
+                                          k32 // 32, _stream_of(x, stream)))
+    return y, (q, e)
+
+
+def ckpt_load(ckpt, cols, dtype, out=None, stream=None):
+    """accerl_ckpt_load: the values [T, cols] that a checkpoint stands for, in ``dtype`` (or into ``out``)."""
+    import torch
+    t = int(ckpt[0].shape[0])
+    if out is None:
+        out = torch.empty((t, cols), dtype=dtype, device=ckpt[0].device)
+    code = _dtype_code(out.dtype)
+    _check_rows(out)
+    assert out.dtype == dtype and tuple(out.shape) == (t, cols)
+    q, e = _check_ckpt(ckpt, t, cols, out)
+    with _on_device_of(out):
+        _check(library().accerl_ckpt_load(_ptr(q), _ld(q), _ptr(e), _ld(e), t, cols, _ptr(out), _ld(out), code,
+                                          _stream_of(out, stream)))
+    return out
+
+
+def ckpt_act_backward(dy, ckpt, act, out=None, stream=None):
+    """accerl_ckpt_act_backward: dx = dy act'(x^) for CUDA rows dy [T, K]; ``out`` may be dy."""
+    import torch
+    code = _dtype_code(dy.dtype)
+    _check_rows(dy)
+    t, k = int(dy.shape[0]), int(dy.shape[1])
+    q, e = _check_ckpt(ckpt, t, k, dy)
+    if out is None:
+        out = torch.empty((t, k), dtype=dy.dtype, device=dy.device)
+    _check_rows(out, dy, dy.dtype)
+    assert out.shape == dy.shape
+    with _on_device_of(dy):
+        _check(library().accerl_ckpt_act_backward(_ptr(dy), _ld(dy), code, _ptr(q), _ld(q), _ptr(e), _ld(e), t, k, _ACTS[act],
+                                                  _ptr(out), _ld(out), _stream_of(dy, stream)))
     return out
 
 

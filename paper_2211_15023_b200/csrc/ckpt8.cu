@@ -1,0 +1,291 @@
+// Activation checkpoints in 8 bits: kept beside the activation's forward pass, read back, and used in its backward pass.
+//
+// 32 values along a row share a power of two 2^E, the smallest with max |x| / 2^E < 127.5.  With bits the largest
+// magnitude's, that is E = exponent - 6, one more where the mantissa is at least 255/128 (its rounding would give
+// 128): E + 127 = ((bits + 0x10000) >> 23) - 6.  Dividing by a power of two is exact, so a value is rounded once, to
+// the integer, and q 2^E has at most 7 significant bits: every later product sees exactly what was kept.
+//
+// All three kernels move rows in pieces of 16 bytes of the activation's type (8 or 4 values; a block's 4 or 8 pieces
+// lie in neighbouring lanes) and are bound by HBM; what bounds the code is the instructions a value: at 5 bytes a value
+// (bf16 in and out, 8 bits kept) the memory leaves about 27 of them.  So the rounding is an addition of 1.5 2^23 that
+// leaves the integer in the low byte, bytes become floats by a byte permutation, and GELU's Phi takes the rational
+// approximation of Abramowitz and Stegun, "Handbook of Mathematical Functions", 7.1.26 (error of erf below 1.5e-7), whose
+// exponential the derivative shares.
+#include "learn.cuh"
+
+namespace accerl {
+
+namespace {
+
+constexpr int kThreads = 256, kAhead = 4, kUnit = kThreads * kAhead;  // pieces of a unit of work
+
+struct CkptArgs {
+    const void *in;  // x (save) or dy (backward)
+    void *out;       // y, x^ or dx; null: none
+    int8_t *q;
+    uint8_t *e;
+    long long ld_in, ld_out, ld_q, ld_e, rows, units;
+    int cols, pieces;    // pieces of a row, the last block's padding among them
+    int rows_per_unit;   // short rows: so many a unit; long ones: 1, and `segments` units a row
+    int segments;
+    unsigned magic;      // l / pieces = l * magic >> 20 for l < kUnit
+};
+
+enum { kSave, kLoad, kBackward };
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Phi(x) and exp(-x^2 / 2)
+__device__ __forceinline__ float normal_cdf(float x, float *density)
+{
+    const float u = fabsf(x) * 0.70710678f;
+    const float t = rcp(fmaf(0.3275911f, u, 1.f));
+    const float d = ex2(x * x * -0.72134752f);
+    float p = fmaf(t, 1.061405429f, -1.453152027f);
+    p = fmaf(t, p, 1.421413741f);
+    p = fmaf(t, p, -0.284496736f);
+    p = fmaf(t, p, 0.254829592f);
+    const float half = 0.5f * (p * t) * d;  // erfc(u) / 2
+    *density = d;
+    return x < 0.f ? half : 1.f - half;
+}
+
+template <int ACT>
+__device__ __forceinline__ float activation(float x)
+{
+    if constexpr (ACT == ACCERL_ACT_RELU) return x < 0.f ? 0.f : x;  // (NaN stays NaN)
+    if constexpr (ACT == ACCERL_ACT_GELU) {
+        float d;
+        return x * normal_cdf(x, &d);
+    }
+    if constexpr (ACT == ACCERL_ACT_SILU) return x * rcp(1.f + ex2(x * -1.44269504f));
+    return x;
+}
+template <int ACT>
+__device__ __forceinline__ float slope(float x)
+{
+    if constexpr (ACT == ACCERL_ACT_RELU) return x > 0.f ? 1.f : x <= 0.f ? 0.f : x;
+    if constexpr (ACT == ACCERL_ACT_GELU) {
+        float d;
+        const float cdf = normal_cdf(x, &d);
+        return fmaf(x * 0.39894228f, d, cdf);
+    }
+    if constexpr (ACT == ACCERL_ACT_SILU) {
+        const float s = rcp(1.f + ex2(x * -1.44269504f));
+        return s * fmaf(x, 1.f - s, 1.f);
+    }
+    return 1.f;
+}
+
+// byte k of a word of four int8, as a float
+__device__ __forceinline__ float byte_value(uint32_t flipped, int k)
+{
+    return __uint_as_float(__byte_perm(flipped, 0x4b000000u, 0x7440u | (unsigned)k)) - 8388736.f;  // 2^23 + 128
+}
+
+template <typename T, int MODE, int ACT>
+__global__ void __launch_bounds__(kThreads) ckpt_kernel(const __grid_constant__ CkptArgs p)
+{
+    constexpr int V = Row<T>::kVec, kWords = V / 4, kLanes = 32 / V;  // lanes of a block
+    for (long long unit = blockIdx.x; unit < p.units; unit += gridDim.x) {
+        const long long row0 = p.segments == 1 ? unit * p.rows_per_unit : unit / p.segments;
+        const int piece0 = p.segments == 1 ? 0 : (int)(unit - row0 * p.segments) * kUnit;
+        long long row[kAhead];
+        int at[kAhead];
+        bool live[kAhead];
+        uint4 raw[kAhead];
+        uint32_t code[kAhead][kWords];
+        uint32_t scale[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int l = i * kThreads + (int)threadIdx.x;
+            const int r = p.segments == 1 ? (int)((unsigned)l * p.magic >> 20) : 0;
+            const int piece = p.segments == 1 ? l - r * p.pieces : piece0 + l;
+            row[i] = row0 + r;
+            live[i] = r < p.rows_per_unit && row[i] < p.rows && piece < p.pieces;
+            at[i] = piece * V;
+            if constexpr (MODE != kLoad) {
+                const T *in = static_cast<const T *>(p.in) + row[i] * p.ld_in;
+                raw[i] = live[i] ? load_piece<T>(in, at[i], p.cols, phase_of(in) == 0, 0.f) : make_uint4(0, 0, 0, 0);
+            }
+            if constexpr (MODE != kSave) {
+#pragma unroll
+                for (int j = 0; j < kWords; ++j) code[i][j] = 0;
+                scale[i] = 0;
+                if (live[i]) {
+                    const int8_t *q = p.q + row[i] * p.ld_q + at[i];
+                    if constexpr (kWords == 2) {
+                        const uint2 c = __ldcs(reinterpret_cast<const uint2 *>(q));
+                        code[i][0] = c.x;
+                        code[i][1] = c.y;
+                    } else {
+                        code[i][0] = __ldcs(reinterpret_cast<const unsigned *>(q));
+                    }
+                    scale[i] = p.e[row[i] * p.ld_e + at[i] / 32];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            float v[V];
+            if constexpr (MODE == kSave) {
+                unpack<T>(raw[i], v);
+                uint32_t top = 0;
+#pragma unroll
+                for (int k = 0; k < V; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
+#pragma unroll
+                for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const bool broken = top >= 0x7f800000u;  // an infinity or a NaN
+                const int e = broken ? 255 : max((int)((top + 0x10000u) >> 23) - 6, 1);
+                const float inv = __uint_as_float((uint32_t)(254 - min(e, 253)) << 23);  // (e <= 249 for finite values)
+                uint32_t w[kWords];
+#pragma unroll
+                for (int j = 0; j < kWords; ++j) {
+                    uint32_t b[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(fmaf(v[4 * j + k], inv, 12582912.f));
+                    w[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+                    if (broken) w[j] = 0;
+                }
+                if (live[i]) {
+                    int8_t *q = p.q + row[i] * p.ld_q + at[i];
+                    if constexpr (kWords == 2) *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
+                    else *reinterpret_cast<uint32_t *>(q) = w[0];
+                    if (at[i] % 32 == 0) p.e[row[i] * p.ld_e + at[i] / 32] = (uint8_t)e;
+                }
+#pragma unroll
+                for (int k = 0; k < V; ++k) v[k] = activation<ACT>(v[k]);
+            } else {
+                float dy[V];
+                if constexpr (MODE == kBackward) unpack<T>(raw[i], dy);
+                const float s = __uint_as_float(scale[i] << 23);  // (255: infinity times the block's zeros, NaN)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float x = byte_value(code[i][k / 4] ^ 0x80808080u, k & 3) * s;
+                    v[k] = MODE == kBackward ? dy[k] * slope<ACT>(x) : x;
+                }
+            }
+            if (live[i] && p.out) {
+                T *out = static_cast<T *>(p.out) + row[i] * p.ld_out;
+                store_piece<T>(out, at[i], p.cols, phase_of(out) == 0, v);
+            }
+        }
+    }
+}
+
+template <int MODE>
+accerl_status launch(CkptArgs &p, int dtype, int act, void *cuda_stream)
+{
+    const int cols32 = (p.cols + 31) / 32 * 32;
+    p.pieces = cols32 * dtype_size(dtype) / 16;
+    if (p.pieces <= kUnit) {
+        p.rows_per_unit = kUnit / p.pieces;
+        p.segments = 1;
+        p.magic = ((1u << 20) + p.pieces - 1) / p.pieces;
+        p.units = (p.rows + p.rows_per_unit - 1) / p.rows_per_unit;
+    } else {
+        p.rows_per_unit = 1;
+        p.segments = (p.pieces + kUnit - 1) / kUnit;
+        p.magic = 0;
+        p.units = p.rows * p.segments;
+    }
+    const unsigned blocks = (unsigned)(p.units < (1LL << 30) ? p.units : (1LL << 30));
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    ACCERL_CUDA_TRY(with_dtype(dtype, [&](auto v) {
+        using T = decltype(v);
+        auto kernel = ckpt_kernel<T, MODE, ACCERL_ACT_NONE>;
+        if constexpr (MODE != kLoad) {
+            if (act == ACCERL_ACT_RELU) kernel = ckpt_kernel<T, MODE, ACCERL_ACT_RELU>;
+            if (act == ACCERL_ACT_GELU) kernel = ckpt_kernel<T, MODE, ACCERL_ACT_GELU>;
+            if (act == ACCERL_ACT_SILU) kernel = ckpt_kernel<T, MODE, ACCERL_ACT_SILU>;
+        }
+        kernel<<<blocks, kThreads, 0, st>>>(p);
+        return cudaGetLastError();
+    }));
+    return ACCERL_OK;
+}
+
+bool good_sizes(const char *who, long long rows, int cols, int dtype, int act)
+{
+    if (rows < 1 || cols < 1 || cols > (1 << 30) || rows > (1LL << 40) / cols) {
+        set_error("%s: rows and cols must be positive (cols at most 2^30, rows * cols at most 2^40)", who);
+        return false;
+    }
+    if (!good_dtype(dtype) || act < ACCERL_ACT_NONE || act > ACCERL_ACT_SILU) {
+        set_error("%s: unknown dtype %d or activation %d", who, dtype, act);
+        return false;
+    }
+    return true;
+}
+
+bool good_rows(const char *who, const char *name, const void *p, long long ld, int cols, int dtype)
+{
+    if (!p || ld < cols || ((uintptr_t)p & (dtype_size(dtype) - 1))) {
+        set_error("%s: %s is null, misaligned or its rows are closer than cols", who, name);
+        return false;
+    }
+    return true;
+}
+
+bool good_ckpt(const char *who, const void *q, long long ld_q, const void *e, long long ld_e, int cols)
+{
+    const int cols32 = (cols + 31) / 32 * 32;
+    if (!q || !e || ((uintptr_t)q & 15) || ld_q < cols32 || ld_q % 16 || ld_e < cols32 / 32) {
+        set_error("%s: a checkpoint's q needs 16-byte alignment, ld_q >= %d (a multiple of 16) and ld_e >= %d", who, cols32,
+                  cols32 / 32);
+        return false;
+    }
+    return true;
+}
+
+}  // namespace
+
+}  // namespace accerl
+
+using namespace accerl;
+
+extern "C" accerl_status accerl_ckpt_save(const void *x, int64_t ld_x, int32_t dtype, int64_t rows, int32_t cols,
+                                          int32_t act, void *y, int64_t ld_y, int8_t *q, int64_t ld_q, uint8_t *e,
+                                          int64_t ld_e, void *cuda_stream)
+{
+    const char *who = "ckpt_save";
+    if (!good_sizes(who, rows, cols, dtype, act) || !good_rows(who, "x", x, ld_x, cols, dtype) ||
+        (y && !good_rows(who, "y", y, ld_y, cols, dtype)) || !good_ckpt(who, q, ld_q, e, ld_e, cols))
+        return ACCERL_ERR_INVALID_ARG;
+    CkptArgs p{x, y, q, e, ld_x, ld_y, ld_q, ld_e, rows, 0, cols, 0, 0, 0, 0};
+    return launch<kSave>(p, dtype, act, cuda_stream);
+}
+
+extern "C" accerl_status accerl_ckpt_load(const int8_t *q, int64_t ld_q, const uint8_t *e, int64_t ld_e, int64_t rows,
+                                          int32_t cols, void *x, int64_t ld_x, int32_t dtype, void *cuda_stream)
+{
+    const char *who = "ckpt_load";
+    if (!good_sizes(who, rows, cols, dtype, ACCERL_ACT_NONE) || !good_rows(who, "x", x, ld_x, cols, dtype) ||
+        !good_ckpt(who, q, ld_q, e, ld_e, cols))
+        return ACCERL_ERR_INVALID_ARG;
+    CkptArgs p{nullptr, x, const_cast<int8_t *>(q), const_cast<uint8_t *>(e), 0, ld_x, ld_q, ld_e, rows, 0, cols, 0, 0, 0, 0};
+    return launch<kLoad>(p, dtype, ACCERL_ACT_NONE, cuda_stream);
+}
+
+extern "C" accerl_status accerl_ckpt_act_backward(const void *dy, int64_t ld_dy, int32_t dtype, const int8_t *q,
+                                                  int64_t ld_q, const uint8_t *e, int64_t ld_e, int64_t rows,
+                                                  int32_t cols, int32_t act, void *dx, int64_t ld_dx, void *cuda_stream)
+{
+    const char *who = "ckpt_act_backward";
+    if (!good_sizes(who, rows, cols, dtype, act) || !good_rows(who, "dy", dy, ld_dy, cols, dtype) ||
+        !good_rows(who, "dx", dx, ld_dx, cols, dtype) || !good_ckpt(who, q, ld_q, e, ld_e, cols))
+        return ACCERL_ERR_INVALID_ARG;
+    CkptArgs p{dy, dx, const_cast<int8_t *>(q), const_cast<uint8_t *>(e), ld_dy, ld_dx, ld_q, ld_e, rows, 0, cols, 0, 0, 0, 0};
+    return launch<kBackward>(p, dtype, act, cuda_stream);
+}

@@ -56,3 +56,46 @@ def test_tensors_a_kernel_cannot_read_raise(P):
                  lambda: P.policy_loss(z.int(), a, f, f)):
         with pytest.raises(AssertionError):
             call()
+
+
+def save_args(**change):
+    a = dict(x=AT, ld_x=40, dtype=0, rows=2, cols=40, act=1, y=AT, ld_y=40, q=AT, ld_q=64, e=AT, ld_e=2, stream=None)
+    a.update(change)
+    return a
+
+
+BAD_CKPT = [dict(q=None), dict(e=None), dict(q=AT + 8), dict(ld_q=63), dict(ld_q=72), dict(ld_q=48), dict(ld_e=1), dict(rows=0),
+            dict(cols=0), dict(rows=1 << 40), dict(dtype=3), dict(dtype=-1)]
+
+
+@pytest.mark.parametrize("change", BAD_CKPT + [dict(x=None), dict(x=AT + 2), dict(dtype=1, x=AT + 1), dict(ld_x=39),
+                                               dict(ld_y=39), dict(y=AT + 1), dict(act=4), dict(act=-1)])
+def test_ckpt_save_refuses(lib, change):
+    assert lib.accerl_ckpt_save(*save_args(**change).values()) == INVALID
+    assert lib.accerl_last_error().startswith(b"ckpt_save")
+
+
+@pytest.mark.parametrize("change", BAD_CKPT + [dict(x=None), dict(x=AT + 2), dict(ld_x=39)])
+def test_ckpt_load_refuses(lib, change):
+    a = save_args(**change)
+    args = [a[k] for k in ("q", "ld_q", "e", "ld_e", "rows", "cols", "x", "ld_x", "dtype", "stream")]
+    assert lib.accerl_ckpt_load(*args) == INVALID
+    assert lib.accerl_last_error().startswith(b"ckpt_load")
+
+
+@pytest.mark.parametrize("change", BAD_CKPT + [dict(x=None), dict(x=AT + 2), dict(ld_x=39), dict(y=None), dict(ld_y=39),
+                                               dict(act=4)])
+def test_ckpt_act_backward_refuses(lib, change):
+    a = save_args(**change)
+    args = [a[k] for k in ("x", "ld_x", "dtype", "q", "ld_q", "e", "ld_e", "rows", "cols", "act", "y", "ld_y", "stream")]
+    assert lib.accerl_ckpt_act_backward(*args) == INVALID
+    assert lib.accerl_last_error().startswith(b"ckpt_act_backward")
+
+
+def test_checkpoint_tensors_a_kernel_cannot_read_raise(P):
+    x = torch.zeros((4, 40))
+    ckpt = torch.zeros((4, 64), dtype=torch.int8), torch.zeros((4, 2), dtype=torch.uint8)
+    for call in (lambda: P.ckpt_save(x), lambda: P.ckpt_save(x.double()), lambda: P.ckpt_load(ckpt, 40, torch.float32),
+                 lambda: P.ckpt_act_backward(x, ckpt, "relu")):
+        with pytest.raises(AssertionError):
+            call()
