@@ -495,6 +495,54 @@ typedef struct {
  */
 accerl_status accerl_policy_loss(const accerl_policy_loss_args *args, void *cuda_stream);
 
+/*
+ * int8 rows with a scale each: s[t] = max_k |x[t][k]| / 127 and q = rint(x / s) in [-127, 127], both divisions
+ * rounded to fp32, ties to even.  Rows of activations are tokens, rows of weights ([out][in]) are channels.  A row of
+ * zeros has s = 0 and q = 0; one that holds an infinity or a NaN has s = NaN and q = 0 (what is computed from it is NaN).
+ *   q   int8_t [rows][ld_q]: ld_q >= cols, a multiple of 16, q aligned to 16 bytes (as the products below read it)
+ * Asynchronous on `cuda_stream`, one launch.  Errors: INVALID_ARG, CUDA.
+ */
+accerl_status accerl_quant_rows(const void *x_dev, int64_t ld_x, int32_t dtype, int64_t rows, int32_t cols, int8_t *q_dev,
+                                int64_t ld_q, float *scale_dev, void *cuda_stream);
+
+/*
+ * A layer of int8 weights on activations that are quantised per token, on the tensor cores:
+ *   acc = sum_k q[t][k] w[n][k]                                  int32, exact
+ *   y[t][n] = fmaf((float)acc, x_scale[t] * w_scale[n], bias[n])  the scales' product rounded once
+ *   (relu: y = max(y, 0)), rounded once to y_dtype.
+ * x is fp32, bf16 or fp16, quantised as accerl_quant_rows does, or (x_dtype ACCERL_I8) is that call's result.
+ */
+enum { ACCERL_I8 = 3 }; /* x_dtype of accerl_linear_i8_args besides the accerl_dtypes */
+typedef struct {
+    const void *x;         /* [tokens][k]; ACCERL_I8: aligned to 16 bytes, ld_x a multiple of 16 */
+    const float *x_scale;  /* [tokens], ACCERL_I8 only (else NULL) */
+    const int8_t *w;       /* [n][k], values in [-127, 127]; aligned to 16 bytes, ld_w a multiple of 16 */
+    const float *w_scale;  /* [n] */
+    const float *bias;     /* [n] or NULL */
+    void *y;               /* [tokens][n] */
+    void *workspace;       /* accerl_linear_i8_workspace bytes, 256-byte aligned; ACCERL_I8: not used */
+    int64_t ld_x, ld_w, ld_y, workspace_bytes;
+    int32_t tokens, n, k;  /* k at most 131072 */
+    int32_t x_dtype, y_dtype, relu;
+} accerl_linear_i8_args;
+
+/* bytes of accerl_linear_i8's workspace (the quantised activations) */
+int64_t accerl_linear_i8_workspace(int32_t tokens, int32_t k, int32_t x_dtype);
+
+/*
+ * Asynchronous on `cuda_stream`, one launch for ACCERL_I8, else two.  The workspace is the call's until the stream has
+ * passed it: calls that may run at the same time (two streams, two captured graphs) need one each.
+ * Errors: INVALID_ARG, UNSUPPORTED (no tensor-memory device), CUDA; a bounded wait on the device that gave up is
+ * reported by accerl_device_check.
+ */
+accerl_status accerl_linear_i8(const accerl_linear_i8_args *args, void *cuda_stream);
+
+/*
+ * Waits for the current device and reports whether a bounded device-side wait of the Learner's operators gave up
+ * since the last such call (ACCERL_ERR_TIMEOUT: results since then are not to be used).
+ */
+accerl_status accerl_device_check(void);
+
 /* Activations between the layers of a policy, for the checkpoints below */
 typedef enum { ACCERL_ACT_NONE = 0, ACCERL_ACT_RELU = 1, ACCERL_ACT_GELU = 2, ACCERL_ACT_SILU = 3 } accerl_activation;
 

@@ -92,6 +92,10 @@ def library() -> C.CDLL:
         lib.accerl_ckpt_act_backward.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i32, i32, vp, i64, vp]
         for f in ("ckpt_save", "ckpt_load", "ckpt_act_backward"):
             getattr(lib, "accerl_" + f).restype = C.c_int
+        lib.accerl_quant_rows.argtypes, lib.accerl_quant_rows.restype = [vp, i64, i32, i64, i32, vp, i64, vp, vp], C.c_int
+        lib.accerl_linear_i8.argtypes, lib.accerl_linear_i8.restype = [C.POINTER(LinearI8Args), vp], C.c_int
+        lib.accerl_linear_i8_workspace.argtypes, lib.accerl_linear_i8_workspace.restype = [i32, i32, i32], i64
+        lib.accerl_device_check.argtypes, lib.accerl_device_check.restype = [], C.c_int
         lib.accerl_policy_destroy.argtypes = [vp]
         lib.accerl_policy_destroy.restype = None
         lib.accerl_trim.argtypes, lib.accerl_trim.restype = [], None
@@ -401,6 +405,76 @@ def ckpt_act_backward(dy, ckpt, act, out=None, stream=None):
         _check(library().accerl_ckpt_act_backward(_ptr(dy), _ld(dy), code, _ptr(q), _ld(q), _ptr(e), _ld(e), t, k, _ACTS[act],
                                                   _ptr(out), _ld(out), _stream_of(dy, stream)))
     return out
+
+
+class LinearI8Args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "x_scale", "w", "w_scale", "bias", "y", "workspace")] + \
+        [(n, C.c_int64) for n in ("ld_x", "ld_w", "ld_y", "workspace_bytes")] + \
+        [(n, C.c_int32) for n in ("tokens", "n", "k", "x_dtype", "y_dtype", "relu")]
+
+
+def quant_rows(x, stream=None):
+    """accerl_quant_rows of CUDA rows x [T, K] (fp32, bf16, fp16): (q int8 [T, K], scale fp32 [T]), one scale a row: the
+    tokens of a batch of activations, or the channels of weights [out, in].  The rows of q start at multiples of 16
+    bytes (its row stride is K rounded up to 16), as linear_i8 reads them."""
+    import torch
+    code = _dtype_code(x.dtype)
+    _check_rows(x)
+    t, k = int(x.shape[0]), int(x.shape[1])
+    k16 = -(-k // 16) * 16
+    q = torch.empty((t, k16), dtype=torch.int8, device=x.device)
+    scale = torch.empty(t, dtype=torch.float32, device=x.device)
+    with _on_device_of(x):
+        _check(library().accerl_quant_rows(_ptr(x), _ld(x), code, t, k, _ptr(q), k16, _ptr(scale), _stream_of(x, stream)))
+    return q[:, :k], scale
+
+
+def _check_q_rows(q, scale, like):
+    import torch
+    _check_rows(q, like, torch.int8)
+    _check_vector(scale, int(q.shape[0]), like, torch.float32)
+    assert (q.stride(0) % 16 == 0 or q.shape[0] == 1) and q.data_ptr() % 16 == 0, "rows of q at multiples of 16 bytes (quant_rows)"
+
+
+def _ld16(q):
+    return q.stride(0) if q.shape[0] > 1 else -(-max(int(q.shape[1]), q.stride(0)) // 16) * 16
+
+
+def linear_i8(x, weight, bias=None, relu=False, out_dtype=None, out=None, stream=None):
+    """accerl_linear_i8: y [T, N] = (x quantised per token) times weight = (q int8 [N, K], scale fp32 [N]) as quant_rows
+    makes it of [N, K], plus ``bias`` fp32 [N], through a ReLU where asked.  x is CUDA rows [T, K] (fp32, bf16, fp16),
+    or a pair (q, scale) of quant_rows; y has x's type (fp32 for a pair) or ``out_dtype``, or is ``out``."""
+    import torch
+    wq, ws = weight
+    given = isinstance(x, (tuple, list))
+    xq, xs = x if given else (x, None)
+    code = 3 if given else _dtype_code(xq.dtype)
+    if given:
+        _check_q_rows(xq, xs, xq)
+    else:
+        _check_rows(xq)
+    _check_q_rows(wq, ws, xq)
+    t, k, n = int(xq.shape[0]), int(xq.shape[1]), int(wq.shape[0])
+    assert wq.shape[1] == k, "weights of rows of %d for tokens of %d" % (wq.shape[1], k)
+    if bias is not None:
+        _check_vector(bias, n, xq, torch.float32)
+    if out is None:
+        out = torch.empty((t, n), dtype=out_dtype or (torch.float32 if given else xq.dtype), device=xq.device)
+    _check_rows(out, xq)
+    assert tuple(out.shape) == (t, n) and (out_dtype is None or out.dtype == out_dtype)
+    lib = library()
+    need = lib.accerl_linear_i8_workspace(t, k, code)
+    ws_mem = torch.empty(need, dtype=torch.uint8, device=xq.device) if need else None
+    a = LinearI8Args(_ptr(xq), _ptr(xs), _ptr(wq), _ptr(ws), _ptr(bias), _ptr(out), _ptr(ws_mem),
+                     _ld16(xq) if given else _ld(xq), _ld16(wq), _ld(out), need, t, n, k, code, _dtype_code(out.dtype), int(relu))
+    with _on_device_of(xq):
+        _check(lib.accerl_linear_i8(C.byref(a), _stream_of(xq, stream)))
+    return out
+
+
+def device_check():
+    """accerl_device_check: waits for the current device; raises if a bounded wait of these operators gave up."""
+    _check(library().accerl_device_check())
 
 
 class Policy:

@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kThreads) ckpt_kernel(const __grid_constant__ 
             at[i] = piece * V;
             if constexpr (MODE != kLoad) {
                 const T *in = static_cast<const T *>(p.in) + row[i] * p.ld_in;
-                raw[i] = live[i] ? load_piece<T>(in, at[i], p.cols, phase_of(in) == 0, 0.f) : make_uint4(0, 0, 0, 0);
+                raw[i] = live[i] ? load_piece<T>(in, at[i], p.cols, 0.f) : make_uint4(0, 0, 0, 0);
             }
             if constexpr (MODE != kSave) {
 #pragma unroll
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads) ckpt_kernel(const __grid_constant__ 
             }
             if (live[i] && p.out) {
                 T *out = static_cast<T *>(p.out) + row[i] * p.ld_out;
-                store_piece<T>(out, at[i], p.cols, phase_of(out) == 0, v);
+                store_piece<T>(out, at[i], p.cols, v);
             }
         }
     }

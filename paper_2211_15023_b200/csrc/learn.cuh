@@ -82,24 +82,66 @@ __device__ __forceinline__ uint4 pack(const float (&v)[Row<T>::kVec])
                       pack_word(v + 2 * E, (const T *)nullptr), pack_word(v + 3 * E, (const T *)nullptr));
 }
 
-// Elements first .. first + kVec of a row of n, those outside it `fill`.  `whole`: the address of element `first` is
-// a multiple of 16 bytes, so that a piece inside the row is one load.
-template <typename T>
-__device__ __forceinline__ uint4 load_piece(const T *row, int first, int n, bool whole, float fill)
+// 16 bytes at any multiple of the element's size.  Off a multiple of 16 they go by 32-bit words, off a multiple of 4 (the
+// 16-bit types only) with the halves put together from neighbouring words: a warp's accesses then touch the same lines
+// four or five times, which L1 serves at about the rate of HBM; element by element it would be eight times.  (A word is
+// read whole where one of its halves is wanted: it lies in the same 4 bytes of the same allocation.)
+__device__ __forceinline__ uint4 load16(const void *p)
+{
+    const uintptr_t a = (uintptr_t)p;
+    if ((a & 15) == 0) return __ldcs(static_cast<const uint4 *>(p));
+    const uint32_t *w = reinterpret_cast<const uint32_t *>(a & ~(uintptr_t)3);
+    uint4 v = make_uint4(w[0], w[1], w[2], w[3]);
+    if (a & 2) {
+        v.x = __funnelshift_r(v.x, v.y, 16);
+        v.y = __funnelshift_r(v.y, v.z, 16);
+        v.z = __funnelshift_r(v.z, v.w, 16);
+        v.w = __funnelshift_r(v.w, w[4], 16);
+    }
+    return v;
+}
+__device__ __forceinline__ void store16(void *p, const uint4 &v)
+{
+    const uintptr_t a = (uintptr_t)p;
+    if ((a & 15) == 0) {
+        *static_cast<uint4 *>(p) = v;
+        return;
+    }
+    if (a & 2) {
+        *static_cast<uint16_t *>(p) = (uint16_t)v.x;
+        uint32_t *w = reinterpret_cast<uint32_t *>(a + 2);
+        w[0] = __funnelshift_r(v.x, v.y, 16);
+        w[1] = __funnelshift_r(v.y, v.z, 16);
+        w[2] = __funnelshift_r(v.z, v.w, 16);
+        *reinterpret_cast<uint16_t *>(a + 14) = (uint16_t)(v.w >> 16);
+        return;
+    }
+    uint32_t *w = static_cast<uint32_t *>(p);
+    w[0] = v.x;
+    w[1] = v.y;
+    w[2] = v.z;
+    w[3] = v.w;
+}
+
+// Elements first .. first + kVec of a row of n, those outside it `fill`.  ALIGNED: the address of element `first` is a
+// multiple of 16 bytes.
+template <typename T, bool ALIGNED = false>
+__device__ __forceinline__ uint4 load_piece(const T *row, int first, int n, float fill)
 {
     constexpr int V = Row<T>::kVec;
-    if (whole && first >= 0 && first + V <= n) return __ldcs(reinterpret_cast<const uint4 *>(row + first));
+    if (first >= 0 && first + V <= n)
+        return ALIGNED ? __ldcs(reinterpret_cast<const uint4 *>(row + first)) : load16(row + first);
     float v[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) v[k] = first + k >= 0 && first + k < n ? to_float(row[first + k]) : fill;
     return pack<T>(v);
 }
 template <typename T>
-__device__ __forceinline__ void store_piece(T *row, int first, int n, bool whole, const float (&v)[Row<T>::kVec])
+__device__ __forceinline__ void store_piece(T *row, int first, int n, const float (&v)[Row<T>::kVec])
 {
     constexpr int V = Row<T>::kVec;
-    if (whole && first >= 0 && first + V <= n) {
-        *reinterpret_cast<uint4 *>(row + first) = pack<T>(v);
+    if (first >= 0 && first + V <= n) {
+        store16(row + first, pack<T>(v));
         return;
     }
 #pragma unroll

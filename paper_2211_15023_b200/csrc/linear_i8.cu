@@ -1,0 +1,435 @@
+// int8 layers on activations that are quantised per token (one scale a token, one a channel).
+//
+// quant_rows_kernel: a warp or a CTA per row finds max |x| and rounds the row to int8; bound by HBM (or by the latency
+// of one row).  A row stays in registers between its maximum and its rounding.  q = rint(x / s) is a division rounded
+// to fp32; it is computed as x * (1 / s) and the division is done only where that product lies so near to a tie that
+// its error (below 127 * 2^-22) could matter.
+//
+// linear_few_kernel: the product.  Channels are the M of the tensor-core instructions and tokens their N, so that one
+// token needs no more than 16 columns and the weights, which bound the few-token case, stream through shared memory
+// once.  K is split over the CTAs of a cluster until the chip is covered; their int32 partial sums are added
+// through distributed shared memory (integers: any order gives the same bits).
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "learn.cuh"
+#include "tc_image.cuh"
+
+namespace accerl {
+
+namespace {
+
+__device__ int g_status;  // of this file's bounded waits
+
+// ------------------------------------------------------------------------------------------- quantisation
+struct QuantArgs {
+    const void *x;
+    int8_t *q;
+    float *scale;
+    long long ld_x, ld_q, rows;
+    int cols;
+};
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// four values to four int8; `exact`: the scale's reciprocal is not to be trusted
+__device__ __forceinline__ uint32_t quantised4(const float *v, float s, float inv, bool exact)
+{
+    float q[4], d = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float t = v[k] * inv;
+        q[k] = rintf(t);
+        d = fmaxf(d, fabsf(t - q[k]));
+    }
+    if (exact || d > 0.49996f) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = fminf(fmaxf(rintf(__fdiv_rn(v[k], s)), -127.f), 127.f);
+    }
+    uint32_t b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(q[k] + 12582912.f);  // the integer in the low byte
+    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+}
+
+template <typename T>
+__device__ __forceinline__ void quantise_piece(const QuantArgs &p, int8_t *q_row, int first, const uint4 &raw, float s, float inv,
+                                               bool exact, bool zero)
+{
+    constexpr int V = Row<T>::kVec;
+    if (first >= p.cols) return;
+    float v[V];
+    unpack<T>(raw, v);
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) w[j] = zero ? 0u : quantised4(v + 4 * j, s, inv, exact);
+    if (first + V <= p.cols) {
+        if constexpr (V == 8) *reinterpret_cast<uint2 *>(q_row + first) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t *>(q_row + first) = w[0];
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (first + k < p.cols) q_row[first + k] = (int8_t)(w[k / 4] >> 8 * (k & 3));
+    }
+}
+
+// WARP: a warp per row, four rows a CTA; else a CTA per row.  NV pieces of 16 bytes a thread stay in registers; a row
+// that has more (LOOP) is read twice.
+template <typename T, int NV, bool WARP, bool LOOP>
+__global__ void __launch_bounds__(WARP ? 128 : 1024) quant_rows_kernel(const __grid_constant__ QuantArgs p)
+{
+    constexpr int V = Row<T>::kVec;
+    __shared__ uint32_t s_top[32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long row = WARP ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
+    if (WARP && row >= p.rows) return;
+    const T *x = static_cast<const T *>(p.x) + row * p.ld_x;
+    int8_t *q = p.q + row * p.ld_q;
+    const int lanes = WARP ? 32 : (int)blockDim.x, step = lanes * V, first = (WARP ? lane : (int)threadIdx.x) * V;
+    uint4 raw[NV];
+    uint32_t top = 0;
+    auto take = [&](const uint4 &piece) {
+        float v[V];
+        unpack<T>(piece, v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) top = max(top, magnitude(v[k]));
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) raw[i] = load_piece<T>(x, first + i * step, p.cols, 0.f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) take(raw[i]);
+    if constexpr (LOOP)
+        for (int at = first + NV * step; at < p.cols; at += step) take(load_piece<T>(x, at, p.cols, 0.f));
+    top = __reduce_max_sync(0xffffffffu, top);
+    if constexpr (!WARP) {
+        if (lane == 0) s_top[warp] = top;
+        __syncthreads();
+        top = __reduce_max_sync(0xffffffffu, lane < lanes / 32 ? s_top[lane] : 0u);
+    }
+    const bool broken = top >= 0x7f800000u;
+    const float s = broken ? NAN : __fdiv_rn(__uint_as_float(top), 127.f);
+    const bool zero = broken || s == 0.f, exact = s < 1e-30f;  // (tiny scales: 1 / s may overflow, s itself be coarse)
+    const float inv = zero || exact ? 0.f : __fdiv_rn(1.f, s);
+    if (first == 0) p.scale[row] = s;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) quantise_piece<T>(p, q, first + i * step, raw[i], s, inv, exact, zero);
+    if constexpr (LOOP)
+        for (int at = first + NV * step; at < p.cols; at += step)
+            quantise_piece<T>(p, q, at, load_piece<T>(x, at, p.cols, 0.f), s, inv, exact, zero);
+}
+
+template <typename T>
+cudaError_t launch_quant(const QuantArgs &p, cudaStream_t st)
+{
+    const long long pieces = ((long long)p.cols + Row<T>::kVec - 1) / Row<T>::kVec;
+    if (pieces <= 32 * 4) {
+        quant_rows_kernel<T, 4, true, false><<<(unsigned)((p.rows + 3) / 4), 128, 0, st>>>(p);
+        return cudaGetLastError();
+    }
+    int threads = 128;
+    while (threads < 1024 && threads * 4 < pieces) threads *= 2;
+    if (threads * 4 >= pieces) quant_rows_kernel<T, 4, false, false><<<(unsigned)p.rows, threads, 0, st>>>(p);
+    else quant_rows_kernel<T, 4, false, true><<<(unsigned)p.rows, threads, 0, st>>>(p);
+    return cudaGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------ product
+struct LinearArgs {
+    const float *x_scale, *w_scale, *bias;
+    void *y;
+    long long ld_y;
+    int tokens, n, k, y_dtype, relu;
+    int chunks;  // of 128 bytes along K
+    int stages;
+};
+
+__device__ __forceinline__ void store_y(const LinearArgs &p, int t, int n, float v)
+{
+    const long long at = (long long)t * p.ld_y + n;
+    if (p.y_dtype == ACCERL_F32) static_cast<float *>(p.y)[at] = v;
+    else if (p.y_dtype == ACCERL_BF16) static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
+    else static_cast<__half *>(p.y)[at] = __float2half_rn(v);
+}
+
+constexpr int kFewThreads = 192, kMaxStages = 8;
+
+// One tile of 128 channels x NT tokens; the CTAs of a cluster share its K.
+// Warps 0..3 drain the accumulator (and finish), warp 4 loads, warp 5 issues the tensor-core instructions.
+template <int NT>
+__global__ void __launch_bounds__(kFewThreads)
+linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                  const __grid_constant__ LinearArgs p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ struct {
+        uint64_t full[kMaxStages], empty[kMaxStages], acc;
+        uint32_t tmem;
+        int abort_flag;
+    } bars;
+    namespace cg = cooperative_groups;
+    constexpr int kStage = 128 * 128 + NT * 128, kCols = NT < 32 ? 32 : NT;
+    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t base = smem_u32(smem), full0 = smem_u32(&bars.full[0]), empty0 = smem_u32(&bars.empty[0]);
+    const int warp = threadIdx.x >> 5;
+    const int share = (int)cg::this_cluster().num_blocks(), rank = (int)cg::this_cluster().block_rank();
+    const int n0 = (int)(blockIdx.x / (unsigned)share) * 128, t0 = (int)blockIdx.y * NT;
+    const int c0 = (int)((long long)p.chunks * rank / share), c1 = (int)((long long)p.chunks * (rank + 1) / share);
+    volatile int *abort_flag = &bars.abort_flag;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(full0 + 8 * s, 1);
+            mbar_init(empty0 + 8 * s, 1);
+        }
+        mbar_init(smem_u32(&bars.acc), 1);
+        bars.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async();
+    }
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"((uint32_t)kCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = bars.tmem;
+
+    if (warp == 4) {
+        // weights are not the previous launch's (the quantiser's) doing: the first stages' are on their way before it ends
+        const int early = min(p.stages, c1 - c0);
+        if (elect_one()) {
+            for (int i = 0; i < early; ++i) {
+                mbar_expect_tx(full0 + 8 * i, kStage);
+                tma_load_2d(base + i * kStage, &map_w, (c0 + i) * 128, n0, full0 + 8 * i);
+            }
+        }
+        __syncwarp();
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        bool ok = true;
+        for (int i = 0; i < c1 - c0 && ok; ++i) {
+            const int s = i % p.stages;
+            if (i >= p.stages) ok = mbar_wait(empty0 + 8 * s, (uint32_t)((i / p.stages - 1) & 1), abort_flag, &g_status, 1);
+            if (ok && elect_one()) {
+                const uint32_t at = base + s * kStage;
+                if (i >= early) {
+                    mbar_expect_tx(full0 + 8 * s, kStage);
+                    tma_load_2d(at, &map_w, (c0 + i) * 128, n0, full0 + 8 * s);
+                }
+                tma_load_2d(at + 128 * 128, &map_x, (c0 + i) * 128, t0, full0 + 8 * s);
+            }
+            __syncwarp();
+        }
+    } else if (warp == 5) {
+        bool ok = true;
+        for (int i = 0; i < c1 - c0 && ok; ++i) {
+            const int s = i % p.stages;
+            ok = mbar_wait(full0 + 8 * s, (uint32_t)((i / p.stages) & 1), abort_flag, &g_status, 8);
+            fence_after();
+            if (ok && elect_one()) {
+                const uint64_t a = make_desc(base + s * kStage, 128), b = make_desc(base + s * kStage + 128 * 128, 128);
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) mma_i8(tmem, a + 2 * ks, b + 2 * ks, idesc_for(NT), (uint32_t)(i | ks));
+                mma_commit(empty0 + 8 * s);
+                if (i == c1 - c0 - 1) mma_commit(smem_u32(&bars.acc));
+            }
+            __syncwarp();
+        }
+    } else {
+        mbar_wait(smem_u32(&bars.acc), 0, abort_flag, &g_status, 16);
+        fence_after();
+    }
+    const int n = n0 + (int)threadIdx.x;  // (the first 128 threads)
+    const bool mine = threadIdx.x < 128 && n < p.n;
+    float ws = 0.f, bias = 0.f;
+    if (mine) {
+        ws = p.w_scale[n];
+        bias = p.bias ? p.bias[n] : 0.f;
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the tokens' scales are the quantiser's
+    auto finish = [&](int t, int acc) {
+        if (!mine || t >= p.tokens) return;
+        float v = fmaf((float)acc, p.x_scale[t] * ws, bias);
+        if (p.relu && v < 0.f) v = 0.f;
+        store_y(p, t, n, v);
+    };
+    int *part = reinterpret_cast<int *>(smem);  // [NT][128]: every operand has been read
+    if (warp < 4) {
+#pragma unroll
+        for (int j = 0; j < NT / 16; ++j) {
+            int acc[16];
+            tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + 16 * j, acc);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (share == 1) finish(t0 + 16 * j + i, acc[i]);
+                else part[(16 * j + i) * 128 + threadIdx.x] = acc[i];
+            }
+        }
+        fence_before();
+    }
+    if (share > 1) {
+        cg::this_cluster().sync();
+        if (threadIdx.x < 128) {
+            const int have = min(NT, p.tokens - t0);
+            for (int t = rank; t < have; t += share) {
+                int acc = 0;
+                for (int r = 0; r < share; ++r) acc += *cg::this_cluster().map_shared_rank(&part[t * 128 + threadIdx.x], r);
+                finish(t0 + t, acc);
+            }
+        }
+        cg::this_cluster().sync();
+    }
+    if (*abort_flag)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
+    __syncthreads();
+    if (warp == 5)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kCols) : "memory");
+}
+
+template <int NT>
+accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArgs &p, int sm_count, bool after_quant, cudaStream_t st)
+{
+    constexpr int kStage = 128 * 128 + NT * 128;
+    p.stages = std::min(kMaxStages, 110 * 1024 / kStage);
+    const size_t smem = 1024 + (size_t)p.stages * kStage;
+    const int tiles = (p.n + 127) / 128, token_tiles = (p.tokens + NT - 1) / NT;
+    int share = 1;
+    while (share < 8 && (long long)tiles * token_tiles * share < sm_count && p.chunks >= 4 * share) share *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)share;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)(tiles * share), (unsigned)token_tiles);
+    cfg.blockDim = dim3(kFewThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = after_quant ? 2 : 1;
+    ACCERL_CUDA_TRY(allow_smem((const void *)linear_few_kernel<NT>, smem));
+    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_few_kernel<NT>, mw, mx, p));
+    return ACCERL_OK;
+}
+
+bool good_quant(const char *who, const void *x, long long ld_x, int dtype, long long rows, int cols)
+{
+    if (rows < 1 || cols < 1 || cols > (1 << 30) || rows > (1LL << 31) - 1 || rows > (1LL << 40) / cols) {
+        set_error("%s: rows and columns must be positive (rows below 2^31, columns at most 2^30, together at most 2^40)", who);
+        return false;
+    }
+    if (!good_dtype(dtype) || !x || ((uintptr_t)x & (dtype_size(dtype) - 1)) || ld_x < cols) {
+        set_error("%s: unknown dtype, or x is null, misaligned or its rows are closer than their length", who);
+        return false;
+    }
+    return true;
+}
+
+}  // namespace
+
+cudaError_t linear_status(int *out)  // (clears it)
+{
+    cudaError_t e = cudaMemcpyFromSymbol(out, g_status, sizeof(int));
+    const int zero = 0;
+    if (e == cudaSuccess && *out) e = cudaMemcpyToSymbol(g_status, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace accerl
+
+using namespace accerl;
+
+extern "C" accerl_status accerl_quant_rows(const void *x, int64_t ld_x, int32_t dtype, int64_t rows, int32_t cols, int8_t *q,
+                                           int64_t ld_q, float *scale, void *cuda_stream)
+{
+    if (!good_quant("quant_rows", x, ld_x, dtype, rows, cols)) return ACCERL_ERR_INVALID_ARG;
+    if (!q || !scale || ((uintptr_t)q & 15) || ((uintptr_t)scale & 3) || ld_q < cols || ld_q % 16) {
+        set_error("quant_rows: q needs 16-byte alignment and ld_q >= cols (a multiple of 16), scale 4-byte alignment");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    const QuantArgs p{x, q, scale, ld_x, ld_q, rows, cols};
+    ACCERL_CUDA_TRY(with_dtype(dtype, [&](auto v) { return launch_quant<decltype(v)>(p, (cudaStream_t)cuda_stream); }));
+    return ACCERL_OK;
+}
+
+static int64_t quantised_bytes(int64_t tokens, int64_t k) { return (tokens * ((k + 15) / 16 * 16) + 255) / 256 * 256; }
+
+extern "C" int64_t accerl_linear_i8_workspace(int32_t tokens, int32_t k, int32_t x_dtype)
+{
+    if (x_dtype == ACCERL_I8 || tokens < 1 || k < 1) return 0;
+    return quantised_bytes(tokens, k) + (4LL * tokens + 255) / 256 * 256;
+}
+
+extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *cuda_stream)
+{
+    if (!a || !a->x || !a->w || !a->w_scale || !a->y) {
+        set_error("linear_i8: null argument");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    if (a->tokens < 1 || a->n < 1 || a->k < 1 || a->k > 131072) {
+        set_error("linear_i8: tokens, n and k must be positive, k at most 131072 (an int32 sum of products of 127)");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    const bool given = a->x_dtype == ACCERL_I8;
+    if (given ? (!a->x_scale || ((uintptr_t)a->x & 15) || a->ld_x < a->k || a->ld_x % 16 || ((uintptr_t)a->x_scale & 3))
+              : a->x_scale != nullptr) {
+        set_error("linear_i8: int8 x needs x_scale, 16-byte alignment and ld_x >= k (a multiple of 16); other x takes no x_scale");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    if (!given && !good_quant("linear_i8", a->x, a->ld_x, a->x_dtype, a->tokens, a->k)) return ACCERL_ERR_INVALID_ARG;
+    if (((uintptr_t)a->w & 15) || a->ld_w < a->k || a->ld_w % 16 || (((uintptr_t)a->w_scale | (uintptr_t)a->bias) & 3)) {
+        set_error("linear_i8: w needs 16-byte alignment and ld_w >= k (a multiple of 16), scales and bias 4-byte alignment");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    if (!good_dtype(a->y_dtype) || ((uintptr_t)a->y & (dtype_size(a->y_dtype) - 1)) || a->ld_y < a->n) {
+        set_error("linear_i8: y has an unknown dtype, is misaligned or its rows are closer than n");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    const int64_t need = accerl_linear_i8_workspace(a->tokens, a->k, a->x_dtype);
+    if (need && (!a->workspace || ((uintptr_t)a->workspace & 255) || a->workspace_bytes < need)) {
+        set_error("linear_i8: the workspace needs %lld bytes, aligned to 256", (long long)need);
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    int device = 0, sm_count = 0;
+    ACCERL_CUDA_TRY(cudaGetDevice(&device));
+    ACCERL_CUDA_TRY(cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device));
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const void *xq = a->x;
+    const float *xs = a->x_scale;
+    int64_t ld_xq = a->ld_x;
+    CUtensorMap mw, mx;
+    if (!given) {
+        ld_xq = (a->k + 15) / 16 * 16;
+        xq = a->workspace;
+        xs = reinterpret_cast<const float *>(static_cast<char *>(a->workspace) + quantised_bytes(a->tokens, a->k));
+    }
+    const int nt = a->tokens <= 16 ? 16 : a->tokens <= 32 ? 32 : a->tokens <= 64 ? 64 : 128;
+    accerl_status s = tc_make_map(&mw, a->w, a->n, a->k, a->ld_w, 128, 128);
+    if (s == ACCERL_OK) s = tc_make_map(&mx, xq, a->tokens, a->k, ld_xq, nt, 128);
+    if (s != ACCERL_OK) return s;
+    if (!given) {
+        const QuantArgs q{a->x, static_cast<int8_t *>(a->workspace), const_cast<float *>(xs), a->ld_x, ld_xq, a->tokens, a->k};
+        ACCERL_CUDA_TRY(with_dtype(a->x_dtype, [&](auto v) { return launch_quant<decltype(v)>(q, st); }));
+    }
+    LinearArgs p{xs, a->w_scale, a->bias, a->y, a->ld_y, a->tokens, a->n, a->k, a->y_dtype, a->relu != 0, (a->k + 127) / 128, 0};
+    return nt == 16   ? launch_few<16>(mw, mx, p, sm_count, !given, st)
+           : nt == 32 ? launch_few<32>(mw, mx, p, sm_count, !given, st)
+           : nt == 64 ? launch_few<64>(mw, mx, p, sm_count, !given, st)
+                      : launch_few<128>(mw, mx, p, sm_count, !given, st);
+}
+
+extern "C" accerl_status accerl_device_check(void)
+{
+    ACCERL_CUDA_TRY(cudaDeviceSynchronize());
+    int st = 0;
+    ACCERL_CUDA_TRY(linear_status(&st));
+    if (st) {
+        set_error("a bounded device-side wait gave up (status 0x%x)", st);
+        return ACCERL_ERR_TIMEOUT;
+    }
+    return ACCERL_OK;
+}

@@ -265,26 +265,23 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) loss_rows_kernel(const __gri
     const T *z_row = static_cast<const T *>(p.logits) + row * p.ld;
     const T *r_row = REF ? static_cast<const T *>(p.ref) + row * p.ld_ref : z_row;
     T *g_row = p.grad ? static_cast<T *>(p.grad) + row * p.ld_grad : nullptr;
-    // Pieces start at multiples of 16 bytes of the logits; an array that lies otherwise goes element by element (the
-    // sums, their order among them, do not depend on it).
-    const int phase = phase_of(z_row);
-    const bool whole_r = phase == phase_of(r_row), whole_g = g_row && phase == phase_of(g_row);
-    const int first = first_lane * V - phase, step = lanes * V;
+    // pieces start at multiples of 16 bytes of the logits (the other arrays may lie otherwise)
+    const int first = first_lane * V - phase_of(z_row), step = lanes * V;
     if (w == 0.f) {
         if (!WARP) asm volatile("barrier.cluster.wait;" ::: "memory");
         if (first_lane == 0) skip_row(p, row);
         if (g_row) {
             const float zero[V] = {};
 #pragma unroll
-            for (int i = 0; i < NV; ++i) store_piece<T>(g_row, first + i * step, p.A, whole_g, zero);
+            for (int i = 0; i < NV; ++i) store_piece<T>(g_row, first + i * step, p.A, zero);
         }
         return;
     }
     uint4 raw[NV], raw_r[REF ? NV : 1];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        raw[i] = load_piece<T>(z_row, first + i * step, p.A, true, -INFINITY);
-        if constexpr (REF) raw_r[i] = load_piece<T>(r_row, first + i * step, p.A, whole_r, -INFINITY);
+        raw[i] = load_piece<T, true>(z_row, first + i * step, p.A, -INFINITY);
+        if constexpr (REF) raw_r[i] = load_piece<T>(r_row, first + i * step, p.A, -INFINITY);
     }
     const long long a = action_of(p, row);
     const bool known = a >= 0 && a < p.A;
@@ -392,7 +389,7 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) loss_rows_kernel(const __gri
 #pragma unroll
             for (int k = 0; k < V; ++k) g[k] = 0.f;
         }
-        store_piece<T>(g_row, at, p.A, whole_g, g);
+        store_piece<T>(g_row, at, p.A, g);
     }
 }
 

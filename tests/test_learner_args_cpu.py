@@ -99,3 +99,49 @@ def test_checkpoint_tensors_a_kernel_cannot_read_raise(P):
                  lambda: P.ckpt_act_backward(x, ckpt, "relu")):
         with pytest.raises(AssertionError):
             call()
+
+
+@pytest.mark.parametrize("change", [dict(x=None), dict(q=None), dict(scale=None), dict(x=AT + 2), dict(dtype=1, x=AT + 1),
+                                    dict(ld_x=39), dict(q=AT + 8), dict(ld_q=47), dict(ld_q=32), dict(rows=0), dict(cols=0),
+                                    dict(rows=1 << 31), dict(rows=1 << 41), dict(dtype=3), dict(scale=AT + 2)])
+def test_quant_rows_refuses(lib, change):
+    a = dict(x=AT, ld_x=40, dtype=0, rows=2, cols=40, q=AT, ld_q=48, scale=AT, stream=None)
+    a.update(change)
+    assert lib.accerl_quant_rows(*a.values()) == INVALID
+    assert lib.accerl_last_error().startswith(b"quant_rows")
+
+
+def linear_args(**change):
+    from paper_2211_15023_b200.binding import LinearI8Args
+    a = dict(x=AT, w=AT, w_scale=AT, y=AT, workspace=AT, ld_x=40, ld_w=48, ld_y=8, workspace_bytes=1 << 20, tokens=2, n=8,
+             k=40, x_dtype=0, y_dtype=0)
+    a.update(change)
+    return LinearI8Args(**a)
+
+
+I8 = dict(x_dtype=3, x_scale=AT, ld_x=48, workspace=None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(x=None), dict(w=None), dict(w_scale=None), dict(y=None), dict(workspace=None), dict(workspace=AT + 128),
+    dict(workspace_bytes=0), dict(tokens=0), dict(n=0), dict(k=0), dict(k=131073, ld_x=131073, ld_w=131088), dict(ld_x=39),
+    dict(ld_w=47), dict(ld_w=32), dict(w=AT + 8), dict(ld_y=7), dict(y=AT + 2), dict(y_dtype=3), dict(x_dtype=4),
+    dict(x_scale=AT), dict(bias=AT + 1), dict(w_scale=AT + 2), dict(I8, x_scale=None), dict(I8, x=AT + 8), dict(I8, ld_x=40),
+    dict(I8, ld_x=32)])
+def test_linear_i8_refuses(lib, change):
+    assert lib.accerl_linear_i8(C.byref(linear_args(**change)), None) == INVALID
+    assert lib.accerl_last_error().startswith(b"linear_i8")
+
+
+def test_linear_i8_needs_no_workspace_for_quantised_tokens(lib):
+    assert lib.accerl_linear_i8(None, None) == INVALID
+    assert lib.accerl_linear_i8_workspace(5, 40, 3) == 0 and lib.accerl_linear_i8_workspace(5, 40, 1) == 256 + 256
+    assert lib.accerl_linear_i8_workspace(1 << 20, 1 << 16, 0) == (1 << 36) + (1 << 22)
+
+
+def test_int8_tensors_a_kernel_cannot_read_raise(P):
+    x, q, s = torch.zeros((4, 40)), torch.zeros((8, 48), dtype=torch.int8)[:, :40], torch.zeros(8)
+    for call in (lambda: P.quant_rows(x), lambda: P.linear_i8(x, (q, s)), lambda: P.linear_i8((q, s), (q, s)),
+                 lambda: P.linear_i8(x.double(), (q, s))):
+        with pytest.raises(AssertionError):
+            call()
