@@ -496,6 +496,35 @@ typedef struct {
 accerl_status accerl_policy_loss(const accerl_policy_loss_args *args, void *cuda_stream);
 
 /*
+ * Gradient of a layer's weights from the checkpoint of its input, on the tensor cores:
+ *   dw[n][k] = sum_t dy[t][n] x^[t][k],   db[n] = sum_t dy[t][n]
+ * with products of the exact 16-bit values and sums in fp32, in an order that depends on the sizes alone (the same
+ * call gives the same bits), rounded once to out_dtype.  `accumulate`: added to what dw and db hold (out_dtype
+ * ACCERL_F32 only), as a sum over micro-batches needs it.  With ACCERL_F16 gradients x^ is taken as fp16: beyond its
+ * range it is infinite.  Needs bf16 or fp16 dy.
+ */
+typedef struct {
+    const void *dy;   /* [tokens][n] of dy_dtype (ACCERL_BF16 or ACCERL_F16) */
+    const int8_t *q;  /* checkpoint of the layer's input, [tokens][k] as accerl_ckpt_save writes it */
+    const uint8_t *e;
+    void *dw;         /* [n][k] of out_dtype (ACCERL_F32 or dy_dtype) */
+    void *db;         /* [n] of out_dtype, or NULL */
+    void *workspace;  /* accerl_ckpt_weight_grad_workspace bytes, 256-byte aligned; may be NULL where that is 0 */
+    int64_t ld_dy, ld_q, ld_e, ld_dw, workspace_bytes;
+    int32_t tokens, n, k;
+    int32_t dy_dtype, out_dtype, accumulate;
+} accerl_weight_grad_args;
+
+/* bytes of the workspace: 0 where dy is aligned to 16 bytes with ld_dy a multiple of 8, else a copy of dy that is */
+int64_t accerl_ckpt_weight_grad_workspace(const accerl_weight_grad_args *args);
+
+/*
+ * Asynchronous on `cuda_stream`, one launch (two with a workspace).  Errors: INVALID_ARG, UNSUPPORTED (fp32 dy), CUDA; a
+ * bounded wait on the device that gave up is reported by accerl_device_check.
+ */
+accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *args, void *cuda_stream);
+
+/*
  * int8 rows with a scale each: s[t] = max_k |x[t][k]| / 127 and q = rint(x / s) in [-127, 127], both divisions
  * rounded to fp32, ties to even.  Rows of activations are tokens, rows of weights ([out][in]) are channels.  A row of
  * zeros has s = 0 and q = 0; one that holds an infinity or a NaN has s = NaN and q = 0 (what is computed from it is NaN).

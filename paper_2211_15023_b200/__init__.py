@@ -7,6 +7,6 @@ is no CPU fallback -- importing :class:`Policy` without the built library
 raises.
 """
 from .binding import (AccerlError, Policy, act_mixed, ckpt_act_backward, ckpt_load, ckpt_save,  # noqa: F401
-                      device_check, kl, library, library_path, linear_i8, policy_loss, quant_rows,
+                      ckpt_weight_grad, device_check, kl, library, library_path, linear_i8, policy_loss, quant_rows,
                       tc_probe_i8, trim, vtrace, FLAG_FORCE_GENERIC, FLAG_KEEP_ACTIVATIONS, FLAG_TAP_FUSED,
                       FLAG_VALUE_HEAD, FLAG_TEST_NO_FASTDIV, FLAG_TEST_NO_AFFINE)

@@ -96,6 +96,10 @@ def library() -> C.CDLL:
         lib.accerl_linear_i8.argtypes, lib.accerl_linear_i8.restype = [C.POINTER(LinearI8Args), vp], C.c_int
         lib.accerl_linear_i8_workspace.argtypes, lib.accerl_linear_i8_workspace.restype = [i32, i32, i32], i64
         lib.accerl_device_check.argtypes, lib.accerl_device_check.restype = [], C.c_int
+        lib.accerl_ckpt_weight_grad.argtypes = [C.POINTER(WeightGradArgs), vp]
+        lib.accerl_ckpt_weight_grad.restype = C.c_int
+        lib.accerl_ckpt_weight_grad_workspace.argtypes = [C.POINTER(WeightGradArgs)]
+        lib.accerl_ckpt_weight_grad_workspace.restype = i64
         lib.accerl_policy_destroy.argtypes = [vp]
         lib.accerl_policy_destroy.restype = None
         lib.accerl_trim.argtypes, lib.accerl_trim.restype = [], None
@@ -405,6 +409,42 @@ def ckpt_act_backward(dy, ckpt, act, out=None, stream=None):
         _check(library().accerl_ckpt_act_backward(_ptr(dy), _ld(dy), code, _ptr(q), _ld(q), _ptr(e), _ld(e), t, k, _ACTS[act],
                                                   _ptr(out), _ld(out), _stream_of(dy, stream)))
     return out
+
+
+class WeightGradArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dy", "q", "e", "dw", "db", "workspace")] + \
+        [(n, C.c_int64) for n in ("ld_dy", "ld_q", "ld_e", "ld_dw", "workspace_bytes")] + \
+        [(n, C.c_int32) for n in ("tokens", "n", "k", "dy_dtype", "out_dtype", "accumulate")]
+
+
+def ckpt_weight_grad(dy, ckpt, cols, out_dtype=None, bias=True, out=None, accumulate=False, stream=None):
+    """accerl_ckpt_weight_grad: (dw [N, K], db [N] or None) from CUDA rows dy [T, N] (bf16 or fp16) and the checkpoint of
+    the layer's input [T, K = cols].  ``out_dtype`` fp32 or dy's type (the default); ``out`` = (dw, db) to write, or with
+    ``accumulate`` (fp32) to add to; db None leaves it out, as does ``bias`` False."""
+    import torch
+    code = _dtype_code(dy.dtype)
+    _check_rows(dy)
+    t, n, k = int(dy.shape[0]), int(dy.shape[1]), int(cols)
+    q, e = _check_ckpt(ckpt, t, k, dy)
+    assert out is not None or not accumulate, "accumulate adds to `out`"
+    if out is None:
+        dt = out_dtype or dy.dtype
+        out = (torch.empty((n, k), dtype=dt, device=dy.device), torch.empty(n, dtype=dt, device=dy.device) if bias else None)
+    dw, db = out
+    _check_rows(dw, dy)
+    assert tuple(dw.shape) == (n, k) and (out_dtype is None or dw.dtype == out_dtype)
+    if db is not None:
+        _check_vector(db, n, dy, dw.dtype)
+    a = WeightGradArgs(_ptr(dy), _ptr(q), _ptr(e), _ptr(dw), _ptr(db), None, _ld(dy), _ld(q), _ld(e), _ld(dw), 0, t, n, k,
+                       code, _dtype_code(dw.dtype), int(accumulate))
+    lib = library()
+    need = lib.accerl_ckpt_weight_grad_workspace(C.byref(a))
+    if need:
+        mem = torch.empty(need, dtype=torch.uint8, device=dy.device)
+        a.workspace, a.workspace_bytes = _ptr(mem), need
+    with _on_device_of(dy):
+        _check(lib.accerl_ckpt_weight_grad(C.byref(a), _stream_of(dy, stream)))
+    return dw, db
 
 
 class LinearI8Args(C.Structure):

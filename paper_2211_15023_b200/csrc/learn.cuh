@@ -22,6 +22,10 @@ inline auto with_dtype(int dtype, F &&f)
     return f(float());
 }
 
+// status words of the bounded waits of linear_i8.cu and weight_grad.cu on the current device; reading clears them
+cudaError_t linear_status(int *out);
+cudaError_t weight_grad_status(int *out);
+
 // 16 bytes of a row: kVec elements
 template <typename T>
 struct Row {

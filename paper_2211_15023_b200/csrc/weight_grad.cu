@@ -1,0 +1,474 @@
+// Gradient of a layer's weights from the 8-bit checkpoint of its input:  dw[n][k] = sum_t dy[t][n] x^[t][k].
+//
+// A bf16 (fp16) product on the tensor cores whose one operand is decoded on the way: x^ = q 2^E has 7 significant bits,
+// so it is exact in either type, and the gradient carries no error beside the checkpoint's own and the fp32 sums'.
+// Both operands lie in memory with the summed index (tokens) outermost, which the tensor cores take as it is (MN-major).
+//
+// x^ is the M operand (128 values of k a tile), dy the N operand (up to 256 channels): a decoded value then meets 256
+// others, and a warp's 32 accumulator lanes are neighbours in a row of dw.  Per stage of 64 tokens the TMA fetches 8 KB of
+// codes and 32 KB of dy; eight warps turn the codes into 16 KB of operand (one block of 32 values a thread: a byte
+// permutation, a subtraction and a multiplication for every two); one thread issues the four instructions of the
+// stage; four warps write the previous tile out meanwhile (two accumulators of 256 columns fill tensor memory).
+// Where the tiles do not cover the chip the tokens are split over a cluster, whose CTAs add their parts through
+// distributed shared memory in a fixed order.  db is a tile of its own whose decoded operand is all ones.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "learn.cuh"
+#include "tc_image.cuh"
+
+namespace accerl {
+
+namespace {
+
+__device__ int g_status;  // of this file's bounded waits
+
+constexpr int kTileK = 128, kTokens = 64;        // values of k a tile, tokens a stage
+constexpr int kRaw = 4, kDec = 3, kDy = 4;       // stages of the three rings
+constexpr int kRawBytes = kTokens * kTileK, kDecBytes = 2 * kRawBytes;
+constexpr int kConvWarps = 8, kThreads = 32 * (4 + kConvWarps + 4);
+
+struct GradArgs {
+    const uint8_t *e;
+    void *dw, *db;
+    long long ld_e, ld_dw;
+    int tokens, n, k, out_dtype, accumulate;
+    int n_tile, n_tiles, k_tiles, tiles;  // tiles: those of db included
+    int cols32;
+};
+
+__device__ __forceinline__ void mma_f16(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// 64 columns of the M or N index (128 bytes) by rows of tokens, 128-byte swizzle: groups of 8 tokens lie 1024 bytes
+// apart, blocks of 64 columns a whole block of kTokens rows
+__device__ __forceinline__ uint64_t mn_desc(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)((kTokens * 128) >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+           (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+// two bytes of `w` (selected) as two bf16 integers: with 0x43 above them the low seven bits read 128 + value, the sign
+// bit alone 128 or 256
+template <typename T>
+struct Decode;
+template <>
+struct Decode<__nv_bfloat16> {
+    __nv_bfloat162 s;
+    __device__ __forceinline__ explicit Decode(int e)
+    {
+        const uint32_t b = (uint32_t)e << 7;  // 2^(e - 127); 255: infinity, times the block's zeros NaN
+        const uint32_t two = b | b << 16;
+        s = *reinterpret_cast<const __nv_bfloat162 *>(&two);
+    }
+    __device__ __forceinline__ uint32_t pair(uint32_t w, uint32_t sel) const
+    {
+        const uint32_t t = __byte_perm(w, 0x43434343u, sel), a = t & 0xff7fff7fu, c = t & 0xff80ff80u;
+        const __nv_bfloat162 q = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&c));
+        const __nv_bfloat162 v = __hmul2(q, s);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+    static constexpr uint32_t kOnes = 0x3f803f80u;
+};
+template <>
+struct Decode<__half> {
+    __half2 s1, s2;  // 2^E in two factors, each a half (E goes beyond its range on both sides)
+    __device__ __forceinline__ explicit Decode(int e)
+    {
+        const int E = e - 127, a = min(max(E, -14), 15), b = max(min(E - a, 1), -24);
+        const float f1 = e == 255 ? NAN : __uint_as_float((uint32_t)(a + 127) << 23), f2 = __uint_as_float((uint32_t)(b + 127) << 23);
+        s1 = __float2half2_rn(f1);
+        s2 = __float2half2_rn(f2);
+    }
+    __device__ __forceinline__ uint32_t pair(uint32_t w, uint32_t sel) const
+    {
+        const uint32_t t = __byte_perm(w ^ 0x80808080u, 0x64646464u, sel);  // 1024 + 128 + value
+        const __half2 q = __hsub2(*reinterpret_cast<const __half2 *>(&t), __float2half2_rn(1152.f));
+        const __half2 v = __hmul2(__hmul2(q, s1), s2);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+    static constexpr uint32_t kOnes = 0x3c003c00u;
+};
+
+struct __align__(8) GradBars {
+    uint64_t raw_full[kRaw], raw_empty[kRaw], dec_full[kDec], dec_empty[kDec], dy_full[kDy], dy_empty[kDy], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int abort_flag;
+};
+
+// position in a ring and its phase
+template <int N>
+struct Ring {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++slot == N) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+__device__ __forceinline__ float load_out(const GradArgs &p, const void *base, long long at)
+{
+    return p.out_dtype == ACCERL_F32 ? static_cast<const float *>(base)[at] : 0.f;
+}
+__device__ __forceinline__ void store_out(const GradArgs &p, void *base, long long at, float v)
+{
+    if (p.out_dtype == ACCERL_F32) static_cast<float *>(base)[at] = v;
+    else if (p.out_dtype == ACCERL_BF16) static_cast<__nv_bfloat16 *>(base)[at] = __float2bfloat16_rn(v);
+    else static_cast<__half *>(base)[at] = __float2half_rn(v);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_dy,
+                   const __grid_constant__ GradArgs p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ GradBars bars;
+    namespace cg = cooperative_groups;
+    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const int dy_bytes = p.n_tile * 2 * kTokens;
+    const uint32_t raw0 = smem_u32(smem), dec0 = raw0 + kRaw * kRawBytes, dy0 = dec0 + kDec * kDecBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int share = (int)cg::this_cluster().num_blocks(), rank = (int)cg::this_cluster().block_rank();
+    const int stages_all = (p.tokens + kTokens - 1) / kTokens;
+    const int g0 = (int)((long long)stages_all * rank / share), g1 = (int)((long long)stages_all * (rank + 1) / share);
+    const int first = (int)(blockIdx.x / (unsigned)share), stride = (int)(gridDim.x / (unsigned)share);
+    volatile int *abort_flag = &bars.abort_flag;
+    auto bar = [](uint64_t &b) { return smem_u32(&b); };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kRaw; ++i) {
+            mbar_init(bar(bars.raw_full[i]), 1);
+            mbar_init(bar(bars.raw_empty[i]), kConvWarps);
+        }
+        for (int i = 0; i < kDec; ++i) {
+            mbar_init(bar(bars.dec_full[i]), kConvWarps);
+            mbar_init(bar(bars.dec_empty[i]), 1);
+        }
+        for (int i = 0; i < kDy; ++i) {
+            mbar_init(bar(bars.dy_full[i]), 1);
+            mbar_init(bar(bars.dy_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(bars.acc_full[i]), 1);
+            mbar_init(bar(bars.acc_empty[i]), 4);
+        }
+        bars.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = bars.tmem;
+    bool ok = true;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------------------------- loads
+        Ring<kRaw> r;
+        Ring<kDy> d;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * p.n_tile;
+            for (int g = g0; g < g1 && ok; ++g) {
+                if (kt < p.k_tiles) {
+                    ok = mbar_wait(bar(bars.raw_empty[r.slot]), r.phase ^ 1, abort_flag, &g_status, 1);
+                    if (ok && elect_one()) {
+                        mbar_expect_tx(bar(bars.raw_full[r.slot]), kRawBytes);
+                        tma_load_2d(raw0 + r.slot * kRawBytes, &map_q, kt * kTileK, g * kTokens, bar(bars.raw_full[r.slot]));
+                    }
+                    __syncwarp();
+                    r.next();
+                }
+                if (ok) ok = mbar_wait(bar(bars.dy_empty[d.slot]), d.phase ^ 1, abort_flag, &g_status, 2);
+                if (ok && elect_one()) {
+                    mbar_expect_tx(bar(bars.dy_full[d.slot]), (uint32_t)dy_bytes);
+                    for (int b = 0; b < p.n_tile / 64; ++b)
+                        tma_load_2d(dy0 + d.slot * dy_bytes + b * kTokens * 128, &map_dy, (n0 + 64 * b) * 2, g * kTokens, bar(bars.dy_full[d.slot]));
+                }
+                __syncwarp();
+                d.next();
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------------------ tensor core
+        constexpr uint32_t kType = std::is_same<T, __half>::value ? 0u : 1u;
+        const uint32_t idesc = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(p.n_tile >> 3) << 17) |
+                               ((uint32_t)(kTileK >> 4) << 24);
+        Ring<kDec> c;
+        Ring<kDy> d;
+        Ring<2> a;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            ok = mbar_wait(bar(bars.acc_empty[a.slot]), a.phase ^ 1, abort_flag, &g_status, 4);
+            fence_after();
+            for (int g = g0; g < g1 && ok; ++g) {
+                ok = mbar_wait(bar(bars.dec_full[c.slot]), c.phase, abort_flag, &g_status, 8);
+                if (ok) ok = mbar_wait(bar(bars.dy_full[d.slot]), d.phase, abort_flag, &g_status, 8);
+                fence_after();
+                if (ok && elect_one()) {
+                    const uint64_t ad = mn_desc(dec0 + c.slot * kDecBytes), bd = mn_desc(dy0 + d.slot * dy_bytes);
+#pragma unroll
+                    for (int ks = 0; ks < kTokens / 16; ++ks)
+                        mma_f16(tmem + 256 * a.slot, ad + ks * (2048 >> 4), bd + ks * (2048 >> 4), idesc, (uint32_t)((g - g0) | ks));
+                    mma_commit(bar(bars.dec_empty[c.slot]));
+                    mma_commit(bar(bars.dy_empty[d.slot]));
+                    if (g == g1 - 1) mma_commit(bar(bars.acc_full[a.slot]));
+                }
+                __syncwarp();
+                c.next();
+                d.next();
+            }
+            a.next();
+        }
+    } else if (warp >= 4 && warp < 4 + kConvWarps) {
+        // ------------------------------------------------------------------------------------ decoding
+        const int w = warp - 4, b = w & 3, t = (w >> 2) * 32 + lane;  // block of 32 values, token of the stage
+        Ring<kRaw> r;
+        Ring<kDec> c;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int kt = u / p.n_tiles;
+            const int col = kt * kTileK + 32 * b;
+            const uint8_t *e_col = p.e + col / 32;
+            const bool in = kt < p.k_tiles && col < p.cols32;
+            auto exponent = [&](int g) { return in && g < g1 && g * kTokens + t < p.tokens ? (int)__ldg(e_col + (long long)(g * kTokens + t) * p.ld_e) : 127; };
+            int e_next = exponent(g0);
+            for (int g = g0; g < g1 && ok; ++g) {
+                const int e = e_next;
+                e_next = exponent(g + 1);
+                uint32_t q[8] = {};
+                if (kt < p.k_tiles) {
+                    ok = mbar_wait(bar(bars.raw_full[r.slot]), r.phase, abort_flag, &g_status, 16);
+                    const uint32_t row = raw0 + r.slot * kRawBytes + t * 128;
+                    const uint4 lo = lds16(row + (((2 * b) ^ (t & 7)) << 4)), hi = lds16(row + (((2 * b + 1) ^ (t & 7)) << 4));
+                    q[0] = lo.x, q[1] = lo.y, q[2] = lo.z, q[3] = lo.w, q[4] = hi.x, q[5] = hi.y, q[6] = hi.z, q[7] = hi.w;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(bars.raw_empty[r.slot]));
+                    r.next();
+                }
+                if (ok) ok = mbar_wait(bar(bars.dec_empty[c.slot]), c.phase ^ 1, abort_flag, &g_status, 32);
+                ok = __all_sync(0xffffffffu, ok);
+                const uint32_t out = dec0 + c.slot * kDecBytes + (b >> 1) * (kTokens * 128) + t * 128;
+                const Decode<T> dec(e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint4 v;
+                    if (kt < p.k_tiles) {
+                        v.x = dec.pair(q[2 * i], 0x4140);
+                        v.y = dec.pair(q[2 * i], 0x4342);
+                        v.z = dec.pair(q[2 * i + 1], 0x4140);
+                        v.w = dec.pair(q[2 * i + 1], 0x4342);
+                    } else {
+                        v.x = v.y = v.z = v.w = Decode<T>::kOnes;
+                    }
+                    sts16(out + ((((b & 1) * 4 + i) ^ (t & 7)) << 4), v);
+                }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(bars.dec_full[c.slot]));
+                c.next();
+            }
+        }
+    } else if (warp >= 4 + kConvWarps) {
+        // ---------------------------------------------------------------------------------------- out
+        const int q = warp & 3;
+        const int kl = 32 * q + lane;
+        Ring<2> a;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * p.n_tile;
+            ok = mbar_wait(bar(bars.acc_full[a.slot]), a.phase, abort_flag, &g_status, 64);
+            fence_after();
+            const bool sums = kt == p.k_tiles;  // db: every row of the accumulator is the same
+            const int k = kt * kTileK + kl;
+            const int n_end = min(p.n_tile, p.n - n0);
+            float *part = reinterpret_cast<float *>(smem);  // [n_tile][128] of this CTA (share > 1: the rings are done with)
+            for (int j = 0; j < p.n_tile; j += 32) {
+                int raw[32];
+                tmem_ld32(tmem + 256 * a.slot + ((uint32_t)(q * 32) << 16) + j, raw);
+                tmem_wait_ld();
+                if (share > 1) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) part[(j + i) * 128 + kl] = __int_as_float(raw[i]);
+                } else if (sums ? kl == 0 : k < p.k) {
+                    void *base = sums ? p.db : p.dw;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        if (j + i >= n_end) break;
+                        const long long at = sums ? n0 + j + i : (long long)(n0 + j + i) * p.ld_dw + k;
+                        float v = __int_as_float(raw[i]);
+                        if (p.accumulate) v += load_out(p, base, at);
+                        store_out(p, base, at, v);
+                    }
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(bars.acc_empty[a.slot]));
+            a.next();
+        }
+    }
+    if (share > 1) {  // one tile a cluster
+        cg::this_cluster().sync();
+        if (warp >= 4 + kConvWarps && first < p.tiles) {
+            const int kt = first / p.n_tiles, n0 = (first - kt * p.n_tiles) * p.n_tile;
+            const int kl = (int)threadIdx.x - 32 * (4 + kConvWarps);
+            const bool sums = kt == p.k_tiles;
+            const int k = kt * kTileK + kl, n_end = min(p.n_tile, p.n - n0);
+            float *part = reinterpret_cast<float *>(smem);
+            if (sums ? kl == 0 : k < p.k)
+                for (int j = rank; j < n_end; j += share) {
+                    float v = 0.f;
+                    for (int i = 0; i < share; ++i) v += *cg::this_cluster().map_shared_rank(&part[j * 128 + kl], i);
+                    void *base = sums ? p.db : p.dw;
+                    const long long at = sums ? n0 + j : (long long)(n0 + j) * p.ld_dw + k;
+                    if (p.accumulate) v += load_out(p, base, at);
+                    store_out(p, base, at, v);
+                }
+        }
+        cg::this_cluster().sync();
+    }
+    if (*abort_flag)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
+    fence_before();
+    __syncthreads();
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// dy at rows of a multiple of 16 bytes, for the TMA
+__global__ void __launch_bounds__(256) realign_kernel(const uint16_t *__restrict__ src, long long ld_src, uint16_t *__restrict__ dst, int ld_dst,
+                                                      int tokens, int n)
+{
+    for (long long t = blockIdx.y; t < tokens; t += gridDim.y)
+        for (int i = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 8; i < n; i += (int)(gridDim.x * blockDim.x) * 8) {
+            const uint4 v = load_piece<__half>(reinterpret_cast<const __half *>(src + t * ld_src), i, n, 0.f);
+            *reinterpret_cast<uint4 *>(dst + t * ld_dst + i) = v;
+        }
+}
+
+int padded_n(int n) { return (n + 7) / 8 * 8; }
+
+}  // namespace
+
+cudaError_t weight_grad_status(int *out)  // (clears it)
+{
+    cudaError_t e = cudaMemcpyFromSymbol(out, g_status, sizeof(int));
+    const int zero = 0;
+    if (e == cudaSuccess && *out) e = cudaMemcpyToSymbol(g_status, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace accerl
+
+using namespace accerl;
+
+static bool dy_aligned(const accerl_weight_grad_args *a) { return !((uintptr_t)a->dy & 15) && a->ld_dy % 8 == 0; }
+
+extern "C" int64_t accerl_ckpt_weight_grad_workspace(const accerl_weight_grad_args *a)
+{
+    if (!a || a->tokens < 1 || a->n < 1 || dy_aligned(a)) return 0;
+    return (2LL * a->tokens * padded_n(a->n) + 255) / 256 * 256;
+}
+
+extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *a, void *cuda_stream)
+{
+    if (!a || !a->dy || !a->q || !a->e || !a->dw) {
+        set_error("ckpt_weight_grad: null argument");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    if (a->tokens < 1 || a->n < 1 || a->k < 1 || a->k > (1 << 27) || a->n > (1 << 27) || (long long)a->n * a->k > (1LL << 40)) {
+        set_error("ckpt_weight_grad: tokens, n and k must be positive, n and k at most 2^27, n * k at most 2^40");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    if (a->dy_dtype == ACCERL_F32) {
+        set_error("ckpt_weight_grad: dy must be bf16 or fp16");
+        return ACCERL_ERR_UNSUPPORTED;
+    }
+    if (!good_dtype(a->dy_dtype) || (a->out_dtype != ACCERL_F32 && a->out_dtype != a->dy_dtype) ||
+        (a->accumulate && a->out_dtype != ACCERL_F32)) {
+        set_error("ckpt_weight_grad: dy is bf16 or fp16, dw and db fp32 or dy's type (fp32 to accumulate)");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    const int cols32 = (a->k + 31) / 32 * 32, es = dtype_size(a->out_dtype);
+    if (((uintptr_t)a->q & 15) || a->ld_q < cols32 || a->ld_q % 16 || a->ld_e < cols32 / 32) {
+        set_error("ckpt_weight_grad: a checkpoint's q needs 16-byte alignment, ld_q >= %d (a multiple of 16) and ld_e >= %d", cols32, cols32 / 32);
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    if (((uintptr_t)a->dy & 1) || a->ld_dy < a->n || a->ld_dw < a->k || (((uintptr_t)a->dw | (uintptr_t)a->db) & (es - 1))) {
+        set_error("ckpt_weight_grad: dy, dw or db is misaligned, or rows are closer than their length");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    const int64_t need = accerl_ckpt_weight_grad_workspace(a);
+    if (need && (!a->workspace || ((uintptr_t)a->workspace & 255) || a->workspace_bytes < need)) {
+        set_error("ckpt_weight_grad: the workspace needs %lld bytes, aligned to 256", (long long)need);
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    int device = 0, sm_count = 0;
+    ACCERL_CUDA_TRY(cudaGetDevice(&device));
+    ACCERL_CUDA_TRY(cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device));
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const void *dy = need ? a->workspace : a->dy;
+    const long long ld_dy = need ? padded_n(a->n) : a->ld_dy;
+    CUtensorMap mq, md;
+    accerl_status s = tc_make_map(&mq, a->q, a->tokens, cols32, a->ld_q, kTokens, 128);
+    if (s == ACCERL_OK) s = tc_make_map(&md, dy, a->tokens, 2 * a->n, 2 * ld_dy, kTokens, 128);
+    if (s != ACCERL_OK) return s;
+    if (need) {
+        const dim3 grid((unsigned)std::min((a->n + 2047) / 2048, 1024), (unsigned)std::min(a->tokens, 65535));
+        realign_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(a->dy), a->ld_dy, static_cast<uint16_t *>(a->workspace),
+                                             padded_n(a->n), a->tokens, a->n);
+        ACCERL_CUDA_TRY(cudaGetLastError());
+    }
+    GradArgs p;
+    p.e = a->e;
+    p.dw = a->dw;
+    p.db = a->db;
+    p.ld_e = a->ld_e;
+    p.ld_dw = a->ld_dw;
+    p.tokens = a->tokens;
+    p.n = a->n;
+    p.k = a->k;
+    p.out_dtype = a->out_dtype;
+    p.accumulate = a->accumulate != 0;
+    p.n_tile = std::min(256, (a->n + 63) / 64 * 64);
+    p.n_tiles = (a->n + p.n_tile - 1) / p.n_tile;
+    p.k_tiles = (a->k + kTileK - 1) / kTileK;
+    p.cols32 = cols32;
+    const long long tiles = (long long)p.n_tiles * (p.k_tiles + (a->db ? 1 : 0));
+    if (tiles > (1 << 30)) {
+        set_error("ckpt_weight_grad: n * k is too large");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    p.tiles = (int)tiles;
+    const int stages = (a->tokens + kTokens - 1) / kTokens;
+    int share = 1;
+    while (share < 8 && 2LL * share * p.tiles <= sm_count && stages >= 4 * share) share *= 2;
+    const unsigned grid = share > 1 ? (unsigned)(p.tiles * share) : (unsigned)std::min(p.tiles, sm_count);
+    const size_t smem = 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens;
+    const auto kernel = a->dy_dtype == ACCERL_F16 ? weight_grad_kernel<__half> : weight_grad_kernel<__nv_bfloat16>;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)share;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    ACCERL_CUDA_TRY(allow_smem((const void *)kernel, smem));
+    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, mq, md, p));
+    return ACCERL_OK;
+}

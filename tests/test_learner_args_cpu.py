@@ -145,3 +145,31 @@ def test_int8_tensors_a_kernel_cannot_read_raise(P):
                  lambda: P.linear_i8(x.double(), (q, s))):
         with pytest.raises(AssertionError):
             call()
+
+
+def grad_args(**change):
+    from paper_2211_15023_b200.binding import WeightGradArgs
+    a = dict(dy=AT, q=AT, e=AT, dw=AT, db=AT, ld_dy=16, ld_q=64, ld_e=2, ld_dw=40, tokens=4, n=16, k=40, dy_dtype=1,
+             out_dtype=0)
+    a.update(change)
+    return WeightGradArgs(**a)
+
+
+@pytest.mark.parametrize("change", [
+    dict(dy=None), dict(q=None), dict(e=None), dict(dw=None), dict(tokens=0), dict(n=0), dict(k=0), dict(dy_dtype=3),
+    dict(out_dtype=2), dict(out_dtype=1, accumulate=1), dict(q=AT + 8), dict(ld_q=63), dict(ld_q=72), dict(ld_e=1),
+    dict(dy=AT + 1), dict(ld_dy=15), dict(ld_dw=39), dict(dw=AT + 2), dict(db=AT + 2), dict(ld_dy=17), dict(dy=AT + 2),
+    dict(ld_dy=17, workspace=AT, workspace_bytes=64), dict(ld_dy=17, workspace=AT + 16, workspace_bytes=1 << 20),
+    dict(n=1 << 27, ld_dy=1 << 27, k=1 << 27, ld_q=1 << 27, ld_e=1 << 22, ld_dw=1 << 27)])
+def test_ckpt_weight_grad_refuses(lib, change):
+    assert lib.accerl_ckpt_weight_grad(C.byref(grad_args(**change)), None) == INVALID
+    assert lib.accerl_last_error().startswith(b"ckpt_weight_grad")
+
+
+def test_ckpt_weight_grad_workspace_and_types(lib):
+    assert lib.accerl_ckpt_weight_grad(None, None) == INVALID
+    assert lib.accerl_ckpt_weight_grad(C.byref(grad_args(dy_dtype=0)), None) == 2  # fp32 gradients: unsupported
+    assert lib.accerl_ckpt_weight_grad_workspace(None) == 0
+    assert lib.accerl_ckpt_weight_grad_workspace(C.byref(grad_args())) == 0
+    assert lib.accerl_ckpt_weight_grad_workspace(C.byref(grad_args(n=15, ld_dy=15))) == 256  # 4 rows of 16 16-bit values
+    assert lib.accerl_ckpt_weight_grad_workspace(C.byref(grad_args(dy=AT + 2, tokens=1 << 20, n=1 << 14, ld_dy=1 << 14))) == 1 << 35
