@@ -22,7 +22,8 @@ inline auto with_dtype(int dtype, F &&f)
     return f(float());
 }
 
-// status words of the bounded waits of linear_i8.cu and weight_grad.cu on the current device; reading clears them
+// status words of the bounded waits of the Learner's files on the current device; reading clears them
+cudaError_t policy_loss_status(int *out);
 cudaError_t linear_status(int *out);
 cudaError_t weight_grad_status(int *out);
 

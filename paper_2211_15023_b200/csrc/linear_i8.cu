@@ -425,11 +425,13 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
 extern "C" accerl_status accerl_device_check(void)
 {
     ACCERL_CUDA_TRY(cudaDeviceSynchronize());
-    int linear = 0, grad = 0;
+    int linear = 0, grad = 0, loss = 0;
     ACCERL_CUDA_TRY(linear_status(&linear));
     ACCERL_CUDA_TRY(weight_grad_status(&grad));
-    if (linear || grad) {
-        set_error("a bounded device-side wait gave up (linear_i8 0x%x, ckpt_weight_grad 0x%x)", linear, grad);
+    ACCERL_CUDA_TRY(policy_loss_status(&loss));
+    if (linear || grad || loss) {
+        set_error("a bounded device-side wait gave up (linear_i8 0x%x, ckpt_weight_grad 0x%x, policy_loss 0x%x)", linear, grad,
+                  loss);
         return ACCERL_ERR_TIMEOUT;
     }
     return ACCERL_OK;

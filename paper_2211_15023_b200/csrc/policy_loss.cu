@@ -13,12 +13,18 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "exp64.cuh"
 #include "learn.cuh"
+#include "tc_ptx.cuh"
 
 namespace accerl {
 
 namespace {
+
+__device__ int g_status;  // of this file's bounded waits
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
@@ -29,6 +35,7 @@ struct LossArgs {
     const float *logp_old, *advantages, *logp_ref, *weights;
     long long ld, ld_ref, ld_grad;
     int rows, A, actions64;
+    int part_pieces;  // long rows: room of a CTA's part, in pieces
     float clip_low, clip_high, kl_coef, entropy_coef;
     void *grad;
     float *logp, *kl, *entropy, *terms;
@@ -195,202 +202,450 @@ __global__ void __launch_bounds__(128) loss_narrow_kernel(const __grid_constant_
 }
 
 // -------------------------------------------------------------------------------------------- long rows
-struct Partial {  // of one warp or more: maxima, sums relative to them
-    float c, so, st, cr, ss, sd;
+__device__ __forceinline__ float max_nan(float a, float b)  // a NaN wins
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
+    } else if constexpr (std::is_same<T, __half>::value) {
+        const __half2 m = __hmax2_nan(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    } else {
+        const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t min_words(uint32_t a, uint32_t b)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __float_as_uint(fminf(__uint_as_float(a), __uint_as_float(b)));
+    } else if constexpr (std::is_same<T, __half>::value) {
+        const __half2 m = __hmin2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    } else {
+        const __nv_bfloat162 m = __hmin2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+}
+// What -inf is taken for (finite, so that its probability of 0 times its logarithm is 0), as a word of one or two
+// elements; a row or part of a row with nothing above it is looked at again, see `low_part`.
+template <typename T>
+__device__ __forceinline__ uint32_t low_word()
+{
+    const float v[2] = {sizeof(T) == 2 && std::is_same<T, __half>::value ? -65504.f : -1e30f,
+                        sizeof(T) == 2 && std::is_same<T, __half>::value ? -65504.f : -1e30f};
+    return pack_word(v, (const T *)nullptr);
+}
+template <typename T>
+__device__ __forceinline__ float word_max(uint32_t w)
+{
+    float v[2];
+    unpack_word(w, v, (const T *)nullptr);
+    return sizeof(T) == 4 ? v[0] : max_nan(v[0], v[1]);
+}
+template <typename T>
+__device__ __forceinline__ float word_min(uint32_t w)
+{
+    float v[2];
+    unpack_word(w, v, (const T *)nullptr);
+    return sizeof(T) == 4 ? v[0] : fminf(v[0], v[1]);
+}
+__device__ __forceinline__ uint32_t *words(uint4 &v) { return reinterpret_cast<uint32_t *>(&v); }
+
+// Gradient coefficients of a row for sums relative to maxima C and CR:  w p_v (base + kl_coef delta_v + entropy_coef lp_v)
+// = e_v (k0 + kt t_v - kr t'_v), logarithms in base 2; and what the action's logit gets on top.
+struct RowCoef {
+    float c, cr, k0, kt, kr, at_a;
 };
-__device__ __forceinline__ Partial shuffled(const Partial &a, int o)
+template <bool REF>
+__device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, float w, bool known, float za, double C, double CR, double so,
+                                            double st, double ss, double sd, bool writer)
 {
-    Partial b;
-    b.c = __shfl_xor_sync(0xffffffffu, a.c, o);
-    b.so = __shfl_xor_sync(0xffffffffu, a.so, o);
-    b.st = __shfl_xor_sync(0xffffffffu, a.st, o);
-    b.cr = __shfl_xor_sync(0xffffffffu, a.cr, o);
-    b.ss = __shfl_xor_sync(0xffffffffu, a.ss, o);
-    b.sd = __shfl_xor_sync(0xffffffffu, a.sd, o);
-    return b;
-}
-// sums of `a` relative to the maxima c and cr (those of a part without any element are -inf, its sums 0)
-__device__ __forceinline__ void rebase(Partial &a, float c, float cr)
-{
-    const float d = a.so != 0.f ? (a.c - c) * kLog2e : 0.f, dr = a.ss != 0.f ? (a.cr - cr) * kLog2e : 0.f;
-    const float f = exp2f(d), fr = exp2f(dr);
-    a.st = f * (a.st + d * a.so);
-    a.sd = f * (a.sd + (d - dr) * a.so);
-    a.so *= f;
-    a.ss *= fr;
-    a.c = c;
-    a.cr = cr;
-}
-__device__ __forceinline__ Partial warp_merged(Partial a)
-{
-    float c = a.c, cr = a.cr;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, o));
-        cr = fmaxf(cr, __shfl_xor_sync(0xffffffffu, cr, o));
-    }
-    rebase(a, c, cr);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const Partial b = shuffled(a, o);
-        a.so += b.so;
-        a.st += b.st;
-        a.ss += b.ss;
-        a.sd += b.sd;
-    }
-    return a;
+    const bool empty = known && C == -INFINITY;
+    const double lso = log2(so), lsr = REF ? log2(ss) : 0.0;
+    const double kl = REF ? kLn2 * (sd / so - (lso - lsr)) : 0.0, H = kLn2 * (lso - st / so);
+    const double logp = empty ? (double)-INFINITY : known ? ((double)za - C) - kLn2 * lso : (double)NAN;
+    const RowResult f = finish_row(p, row, logp, kl, H, empty, writer);
+    const double scale = (double)w / so, kk = REF ? (double)p.kl_coef * kLn2 : 0.0, ke = (double)p.entropy_coef * kLn2;
+    RowCoef r;
+    r.c = (float)C;
+    r.cr = (float)CR;
+    r.k0 = empty ? 0.f : (float)(scale * (f.base - ke * lso - (kk != 0.0 ? kk * (lso - lsr) : 0.0)));
+    r.kt = empty ? 0.f : (float)(scale * (ke + kk));
+    r.kr = empty ? 0.f : (float)(scale * kk);
+    r.at_a = empty ? 0.f : (float)((double)w * f.slope);
+    return r;
 }
 
-constexpr int kMaxCluster = 16, kMaxWarps = 16;
+// t of a piece's logits kept relative to `base`, when the row's maximum is c (a part far below the rest: its probabilities
+// are 0, their logarithms kept finite)
+__device__ __forceinline__ float shift_of(float base, float c) { return c == -INFINITY ? 0.f : max_nan((base - c) * kLog2e, -1e30f); }
 
-// WARP: a warp per row, four rows a CTA; else the CTAs of a cluster share a row.  A thread holds NV pieces of 16 bytes
-// (and as many of the reference's).
-template <typename T, bool REF, int NV, bool WARP>
-__global__ void __launch_bounds__(WARP ? 128 : 512) loss_rows_kernel(const __grid_constant__ LossArgs p)
+template <typename T, bool REF>
+__device__ __forceinline__ void add_sums(const uint4 &raw, const uint4 &raw_r, float nc, float ncr, float &so, float &st, float &ss, float &sd)
 {
     constexpr int V = Row<T>::kVec;
-    __shared__ Partial parts[WARP ? 1 : kMaxCluster * kMaxWarps];
-    namespace cg = cooperative_groups;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int share = 1, rank = 0;  // CTAs of the row
-    if constexpr (!WARP) {
-        share = (int)cg::this_cluster().num_blocks();
-        rank = (int)cg::this_cluster().block_rank();
-        asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+    float z[V], zr[V];
+    unpack<T>(raw, z);
+    if constexpr (REF) unpack<T>(raw_r, zr);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const float t = fmaf(z[k], kLog2e, nc), e = exp2_fast(t);
+        so += e;
+        st = fmaf(e, t, st);
+        if constexpr (REF) {
+            const float tr = fmaf(zr[k], kLog2e, ncr);
+            ss += exp2_fast(tr);
+            sd = fmaf(e, t - tr, sd);
+        }
     }
-    const long long row = WARP ? (long long)blockIdx.x * 4 + warp : (long long)(blockIdx.x / (unsigned)share);
-    if (WARP && row >= p.rows) return;
-    const int lanes = WARP ? 32 : (int)blockDim.x * share, first_lane = WARP ? lane : rank * (int)blockDim.x + (int)threadIdx.x;
+}
+
+template <typename T, bool REF>
+__device__ __forceinline__ void put_gradient(const LossArgs &p, T *g_row, int at, int a, const uint4 &raw, const uint4 &raw_r, const RowCoef &f,
+                                             float sh, float shr)
+{
+    constexpr int V = Row<T>::kVec;
+    float z[V], zr[V], g[V];
+    unpack<T>(raw, z);
+    if constexpr (REF) unpack<T>(raw_r, zr);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const float t = fmaf(z[k], kLog2e, sh), e = exp2_fast(t);
+        float b = fmaf(f.kt, t, f.k0);
+        if constexpr (REF) b = fmaf(-f.kr, fmaf(zr[k], kLog2e, shr), b);
+        g[k] = e * b;
+    }
+    if ((unsigned)(a - at) < (unsigned)V) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (at + k == a) g[k] += f.at_a;
+    }
+    store_piece<T>(g_row, at, p.A, g);
+}
+
+// is there a probability of the policy where the reference has none?  (elements lane, lane + step ... of the row's part)
+template <typename T>
+__device__ __forceinline__ bool without_q(const T *z_row, const T *r_row, int begin, int end, int step, float c)
+{
+    bool found = false;
+    for (int v = begin; v < end; v += step)
+        if (to_float(r_row[v]) == -INFINITY && to_float(z_row[v]) != -INFINITY && exp2_fast((to_float(z_row[v]) - c) * kLog2e) != 0.f)
+            found = true;
+    return found;
+}
+
+// Rows of up to 128 pieces of 16 bytes: a warp per row, the row in its registers.
+constexpr int kWarpPieces = 4;
+template <typename T, bool REF>
+__global__ void __launch_bounds__(128, 4) loss_warp_kernel(const __grid_constant__ LossArgs p)
+{
+    constexpr int V = Row<T>::kVec, NV = kWarpPieces;
+    const int lane = threadIdx.x & 31;
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row >= p.rows) return;
     const float w = weight_of(p, row);
     const T *z_row = static_cast<const T *>(p.logits) + row * p.ld;
     const T *r_row = REF ? static_cast<const T *>(p.ref) + row * p.ld_ref : z_row;
     T *g_row = p.grad ? static_cast<T *>(p.grad) + row * p.ld_grad : nullptr;
-    // pieces start at multiples of 16 bytes of the logits (the other arrays may lie otherwise)
-    const int first = first_lane * V - phase_of(z_row), step = lanes * V;
+    const int first = lane * V - phase_of(z_row), step = 32 * V;
     if (w == 0.f) {
-        if (!WARP) asm volatile("barrier.cluster.wait;" ::: "memory");
-        if (first_lane == 0) skip_row(p, row);
-        if (g_row) {
-            const float zero[V] = {};
-#pragma unroll
+        if (lane == 0) skip_row(p, row);
+        const float zero[V] = {};
+        if (g_row)
             for (int i = 0; i < NV; ++i) store_piece<T>(g_row, first + i * step, p.A, zero);
-        }
         return;
     }
-    uint4 raw[NV], raw_r[REF ? NV : 1];
+    uint4 raw[NV], raw_r[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         raw[i] = load_piece<T, true>(z_row, first + i * step, p.A, -INFINITY);
         if constexpr (REF) raw_r[i] = load_piece<T>(r_row, first + i * step, p.A, -INFINITY);
+        else raw_r[i] = raw[i];
     }
-    const long long a = action_of(p, row);
-    const bool known = a >= 0 && a < p.A;
-    const float za = known ? to_float(z_row[a]) : NAN;
-
-    Partial s;
-    float m = -INFINITY, mr = -INFINITY;
+    const long long wanted = action_of(p, row);
+    const int a = wanted >= 0 && wanted < p.A ? (int)wanted : -1;
+    const float za = a >= 0 ? to_float(z_row[a]) : NAN;
+    const uint32_t low_w = low_word<T>();
+    float low[2];
+    unpack_word(low_w, low, (const T *)nullptr);
+    // the maximum; -inf raised to the low value; pieces are relative to `base` (0 but where all lies at that value or below)
+    auto prepare = [&](uint4 (&x)[NV], const T *x_row, float &base) {
+        uint32_t m = low_w;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        float z[V];
-        unpack<T>(raw[i], z);
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int k = 0; k < V; ++k) m = fmaxf(m, z[k]);
-        if constexpr (REF) {
-            unpack<T>(raw_r[i], z);
+            for (int j = 0; j < 4; ++j) {
+                words(x[i])[j] = max_words<T>(words(x[i])[j], low_w);
+                m = max_words<T>(m, words(x[i])[j]);
+            }
+        float c = word_max<T>(m);
 #pragma unroll
-            for (int k = 0; k < V; ++k) mr = fmaxf(mr, z[k]);
-        }
-    }
+        for (int o = 16; o > 0; o >>= 1) c = max_nan(c, __shfl_xor_sync(0xffffffffu, c, o));
+        base = 0.f;
+        if (c <= low[0]) {
+            c = -INFINITY;
+            for (int v = lane; v < p.A; v += 32) c = fmaxf(c, to_float(x_row[v]));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if (REF) mr = fmaxf(mr, __shfl_xor_sync(0xffffffffu, mr, o));
-    }
-    s.c = m;
-    s.cr = mr;
-    {
-        const float c = m == -INFINITY ? 0.f : m, cr = mr == -INFINITY ? 0.f : mr;
-        s.so = s.st = s.ss = s.sd = 0.f;
+            for (int o = 16; o > 0; o >>= 1) c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, o));
+            if (c != -INFINITY) {
+                base = c;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float z[V], zr[V];
-            unpack<T>(raw[i], z);
-            if constexpr (REF) unpack<T>(raw_r[i], zr);
+                for (int i = 0; i < NV; ++i) {
+                    float z[V];
+                    x[i] = load_piece<T>(x_row, first + i * step, p.A, -INFINITY);
+                    unpack<T>(x[i], z);
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float t = (z[k] - c) * kLog2e, e = exp2_fast(t);
-                s.so += e;
-                s.st += e != 0.f ? e * t : 0.f;
-                if constexpr (REF) {
-                    const float tr = (zr[k] - cr) * kLog2e;
-                    s.ss += exp2_fast(tr);
-                    s.sd += e != 0.f ? e * (t - tr) : 0.f;
+                    for (int k = 0; k < V; ++k) z[k] = fmaxf(z[k] - c, low[0]);
+                    x[i] = pack<T>(z);
                 }
             }
         }
+        return c;
+    };
+    bool holes = false;
+    if constexpr (REF) {
+        uint32_t least = raw_r[0].x;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) least = min_words<T>(least, words(raw_r[i])[j]);
+        holes = word_min<T>(least) == -INFINITY;
     }
-    s = warp_merged(s);
-    if constexpr (!WARP) {
-        asm volatile("barrier.cluster.wait;" ::: "memory");  // every CTA of the cluster has started
-        const int warps = (int)blockDim.x >> 5, total = warps * share;
-        if (lane < share) *cg::this_cluster().map_shared_rank(&parts[rank * warps + warp], lane) = s;
-        cg::this_cluster().sync();
-        Partial mine;
-        mine.c = mine.cr = -INFINITY;
-        for (int i = lane; i < total; i += 32) {
-            mine.c = fmaxf(mine.c, parts[i].c);
-            mine.cr = fmaxf(mine.cr, parts[i].cr);
+    float base, base_r = 0.f;
+    const float C = prepare(raw, z_row, base);
+    float CR = -INFINITY;
+    if constexpr (REF) CR = prepare(raw_r, r_row, base_r);
+    float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f;
+    float sh = shift_of(base, C), shr = shift_of(base_r, CR);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) add_sums<T, REF>(raw[i], raw_r[i], sh, shr, so, st, ss, sd);
+    if (REF && __any_sync(0xffffffffu, holes) && without_q(z_row, r_row, lane, p.A, 32, C)) sd = INFINITY;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        so += __shfl_xor_sync(0xffffffffu, so, o);
+        st += __shfl_xor_sync(0xffffffffu, st, o);
+        if (REF) {
+            ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            sd += __shfl_xor_sync(0xffffffffu, sd, o);
         }
-        mine.so = mine.st = mine.ss = mine.sd = 0.f;
-        for (int i = lane; i < total; i += 32) {
-            Partial b = parts[i];
-            rebase(b, mine.c, mine.cr);
-            mine.so += b.so;
-            mine.st += b.st;
-            mine.ss += b.ss;
-            mine.sd += b.sd;
-        }
-        s = warp_merged(mine);
     }
-    const bool empty = known && s.so == 0.f;
-    const float c = s.c == -INFINITY ? 0.f : s.c, cr = s.cr == -INFINITY ? 0.f : s.cr;
-    const float inv = 1.f / s.so, lso = log2f(s.so), lsr = REF ? log2f(s.ss) : 0.f;
-    const double kl = REF ? kLn2 * ((double)s.sd / (double)s.so - (double)log2f(s.so / s.ss)) : 0.0;
-    const double H = kLn2 * ((double)lso - (double)s.st / (double)s.so);
-    const double logp = empty ? (double)-INFINITY : kLn2 * ((double)((za - c) * kLog2e) - (double)lso);
-    const RowResult f = finish_row(p, row, logp, kl, H, empty, first_lane == 0);
+    const RowCoef f = row_coef<REF>(p, row, w, a >= 0, za, C, CR, so, st, CR == -INFINITY ? 0.0 : (double)ss, sd, lane == 0);
     if (!g_row) return;
-    // p_v (base + kl_coef delta_v + entropy_coef lp_v) with the logarithms in base 2
-    const float kk = REF ? (float)(p.kl_coef * kLn2) : 0.f, ke = (float)(p.entropy_coef * kLn2);
-    const float wi = w * inv;
-    const float k0 = (float)(f.base - (double)ke * lso - (kk != 0.f ? (double)kk * ((double)lso - lsr) : 0.0));
-    const float at_a = (float)((double)w * f.slope);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = first + i * step;
-        float z[V], zr[V], g[V];
-        unpack<T>(raw[i], z);
-        if constexpr (REF) unpack<T>(raw_r[i], zr);
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const float t = (z[k] - c) * kLog2e, e = exp2_fast(t);
-            float b = fmaf(ke, t, k0);
-            if constexpr (REF) {
-                if (kk != 0.f) b = fmaf(kk, t - (zr[k] - cr) * kLog2e, b);
-            }
-            g[k] = e != 0.f ? e * wi * b : 0.f;
-        }
-        if (a >= at && a < at + V) {
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (at + k == a) g[k] += at_a;
-        }
-        if (empty) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) g[k] = 0.f;
-        }
-        store_piece<T>(g_row, at, p.A, g);
+    for (int i = 0; i < NV; ++i) put_gradient<T, REF>(p, g_row, first + i * step, a, raw[i], raw_r[i], f, sh, shr);
+}
+
+struct Partial {  // of one CTA: maxima, and sums relative to them
+    double so, st, ss, sd;
+    float c, cr;
+};
+
+// Longer rows: the CTAs of a cluster share a row (one CTA up to 72 KB of it, the reference's included), each keeps its part in
+// shared memory from one read of it to the gradient.  Bulk copies bring it in; what is not whole 16 bytes, or lies otherwise
+// to 16 bytes than the logits do, goes through registers.  Three or four CTAs fit an SM: while one waits for its part or
+// for its cluster, the others compute and write.  What bounds it beside HBM is the instructions a logit (14, 25 with a
+// reference row, where memory leaves 22 and 33): so -inf is made finite and the maximum found two 16-bit logits at a
+// time, t is one multiply-add of the logit, and what depends on the row only is worked out, in double, by one warp.
+// Sums of a thread are float (some 50 terms), from there on double.
+constexpr int kMaxCluster = 16, kRowThreads = 512;
+template <typename T, bool REF>
+__global__ void __launch_bounds__(kRowThreads, 2) loss_rows_kernel(const __grid_constant__ LossArgs p)
+{
+    constexpr int V = Row<T>::kVec;
+    extern __shared__ __align__(128) uint4 s_piece[];  // [REF ? 2 : 1][pieces of a part]
+    __shared__ Partial parts[kMaxCluster];
+    __shared__ double s_sum[kRowThreads / 32][4];
+    __shared__ float s_max[2][kRowThreads / 32];
+    __shared__ RowCoef s_row;
+    __shared__ uint64_t s_bar;
+    __shared__ int s_abort;
+    namespace cg = cooperative_groups;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
+    const int share = (int)cg::this_cluster().num_blocks(), rank = (int)cg::this_cluster().block_rank();
+    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+    const long long row = (long long)(blockIdx.x / (unsigned)share);
+    const float w = weight_of(p, row);
+    const T *z_row = static_cast<const T *>(p.logits) + row * p.ld;
+    const T *r_row = REF ? static_cast<const T *>(p.ref) + row * p.ld_ref : z_row;
+    T *g_row = p.grad ? static_cast<T *>(p.grad) + row * p.ld_grad : nullptr;
+    // pieces start at multiples of 16 bytes of the logits
+    const int phase = phase_of(z_row), pieces = (phase + p.A + V - 1) / V;
+    const int j0 = (int)((long long)pieces * rank / share), n = (int)((long long)pieces * (rank + 1) / share) - j0;
+    const int first = j0 * V - phase;  // element of the part's first piece
+    if (w == 0.f) {
+        asm volatile("barrier.cluster.wait;" ::: "memory");
+        if (rank == 0 && threadIdx.x == 0) skip_row(p, row);
+        const float zero[V] = {};
+        if (g_row)
+            for (int j = threadIdx.x; j < n; j += blockDim.x) store_piece<T>(g_row, first + j * V, p.A, zero);
+        return;
     }
+    uint4 *z_s = s_piece, *r_s = s_piece + (REF ? p.part_pieces : 0);
+    const bool alike = phase_of(r_row) == phase;
+    const int whole0 = first < 0 ? 1 : 0, whole1 = first + n * V > p.A ? n - 1 : n;  // whole pieces of the part
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        mbar_init(smem_u32(&s_bar), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        const uint32_t bytes = whole1 > whole0 ? (uint32_t)(whole1 - whole0) * 16u : 0u;
+        mbar_expect_tx(smem_u32(&s_bar), bytes * (REF && alike ? 2u : 1u));
+        if (bytes) {
+            bulk_load(smem_u32(z_s + whole0), z_row + first + whole0 * V, bytes, smem_u32(&s_bar));
+            if (REF && alike) bulk_load(smem_u32(r_s + whole0), r_row + first + whole0 * V, bytes, smem_u32(&s_bar));
+        }
+    }
+    if (threadIdx.x < 2) {  // the part's ends
+        const int j = threadIdx.x == 0 ? 0 : n - 1;
+        if (n > 0 && (j < whole0 || j >= whole1)) {
+            z_s[j] = load_piece<T>(z_row, first + j * V, p.A, -INFINITY);
+            if (REF && alike) r_s[j] = load_piece<T>(r_row, first + j * V, p.A, -INFINITY);
+        }
+    }
+    if (REF && !alike)
+        for (int j = threadIdx.x; j < n; j += blockDim.x) r_s[j] = load_piece<T>(r_row, first + j * V, p.A, -INFINITY);
+    const long long wanted = action_of(p, row);
+    const int a = wanted >= 0 && wanted < p.A ? (int)wanted : -1;
+    const float za = a >= 0 ? to_float(z_row[a]) : NAN;  // (`grad` may be `logits`: read before the barriers below)
+    __syncthreads();
+    mbar_wait(smem_u32(&s_bar), 0, &s_abort, &g_status, 1);
+
+    const uint32_t low_w = low_word<T>();
+    float low[2];
+    unpack_word(low_w, low, (const T *)nullptr);
+    // a pass of the part: -inf raised to the low value, the maximum; in every thread of the CTA
+    auto prepare = [&](uint4 *x_s, int which) {
+        uint32_t m = low_w, least = low_w;
+        for (int j = threadIdx.x; j < n; j += blockDim.x) {
+            uint4 v = x_s[j];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (which) least = min_words<T>(least, words(v)[i]);
+                words(v)[i] = max_words<T>(words(v)[i], low_w);
+                m = max_words<T>(m, words(v)[i]);
+            }
+            x_s[j] = v;
+        }
+        float c = word_max<T>(m);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) c = max_nan(c, __shfl_xor_sync(0xffffffffu, c, o));
+        if (lane == 0) s_max[which][warp] = c;
+        return which && word_min<T>(least) == -INFINITY;
+    };
+    auto block_max = [&](int which) {
+        float c = s_max[which][0];
+        for (int i = 1; i < warps; ++i) c = max_nan(c, s_max[which][i]);
+        return c;
+    };
+    // a part with nothing above the low value: read again, relative to its own maximum (returned; -inf: no logit)
+    auto low_part = [&](uint4 *x_s, const T *x_row, int which) {
+        float c = -INFINITY;
+        for (int v = max(first, 0) + (int)threadIdx.x; v < min(first + n * V, p.A); v += blockDim.x) c = fmaxf(c, to_float(x_row[v]));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, o));
+        __syncthreads();
+        if (lane == 0) s_max[which][warp] = c;
+        __syncthreads();
+        c = block_max(which);
+        if (c != -INFINITY)
+            for (int j = threadIdx.x; j < n; j += blockDim.x) {
+                float z[V];
+                unpack<T>(load_piece<T>(x_row, first + j * V, p.A, -INFINITY), z);
+#pragma unroll
+                for (int k = 0; k < V; ++k) z[k] = fmaxf(z[k] - c, low[0]);
+                x_s[j] = pack<T>(z);
+            }
+        return c;
+    };
+    bool holes = false;
+    prepare(z_s, 0);
+    if (REF) holes = prepare(r_s, 1);
+    holes = __syncthreads_or(holes);
+    float c = block_max(0), cr = REF ? block_max(1) : -INFINITY, base = 0.f, base_r = 0.f;
+    if (c <= low[0]) {
+        c = low_part(z_s, z_row, 0);
+        base = c == -INFINITY ? 0.f : c;
+    }
+    if (REF && cr <= low[0]) {
+        cr = low_part(r_s, r_row, 1);
+        base_r = cr == -INFINITY ? 0.f : cr;
+    }
+    float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f;
+    {
+        const float sh = shift_of(base, c), shr = shift_of(base_r, cr);
+#pragma unroll 2
+        for (int j = threadIdx.x; j < n; j += blockDim.x) add_sums<T, REF>(z_s[j], r_s[j], sh, shr, so, st, ss, sd);
+    }
+    if (holes && without_q(z_row, r_row, max(first, 0) + (int)threadIdx.x, min(first + n * V, p.A), (int)blockDim.x, c)) sd = INFINITY;
+    double sums[4] = {so, st, ss, sd};
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < (REF ? 4 : 2); ++i) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], o);
+    if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_sum[warp][i] = sums[i];
+    __syncthreads();
+    asm volatile("barrier.cluster.wait;" ::: "memory");  // every CTA of the cluster has started
+    if (warp == 0) {
+        Partial mine;
+        double v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = lane < warps ? s_sum[lane][i] : 0.0;
+#pragma unroll
+            for (int o = kRowThreads / 64; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        }
+        mine.so = c == -INFINITY ? 0.0 : v[0];
+        mine.st = c == -INFINITY ? 0.0 : v[1];
+        mine.ss = cr == -INFINITY ? 0.0 : v[2];
+        mine.sd = c == -INFINITY ? 0.0 : v[3];
+        mine.c = c;
+        mine.cr = cr;
+        if (lane < share) *cg::this_cluster().map_shared_rank(&parts[rank], lane) = mine;
+    }
+    cg::this_cluster().sync();
+    if (warp == 0) {
+        Partial b = parts[lane < share ? lane : 0];
+        if (lane >= share) {
+            b.so = b.st = b.ss = b.sd = 0.0;
+            b.c = b.cr = -INFINITY;
+        }
+        float C = b.c, CR = b.cr;
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+            C = max_nan(C, __shfl_xor_sync(0xffffffffu, C, o));
+            CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
+        }
+        // a part's sums, relative to the row's maxima
+        const double d = b.so != 0.0 ? ((double)b.c - (double)C) * (double)kLog2e : 0.0;
+        const double dr = b.ss != 0.0 ? ((double)b.cr - (double)CR) * (double)kLog2e : 0.0;
+        const double f = exp2(d);
+        double v[4] = {f * b.so, f != 0.0 ? f * (b.st + d * b.so) : 0.0, exp2(dr) * b.ss, f != 0.0 ? f * (b.sd + (d - dr) * b.so) : 0.0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int o = kMaxCluster / 2; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        const RowCoef r = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], rank == 0 && lane == 0);
+        if (lane == 0) s_row = r;
+    }
+    __syncthreads();
+    if (g_row) {
+        const RowCoef f = s_row;
+        const float sh = shift_of(base, f.c), shr = shift_of(base_r, f.cr);
+#pragma unroll 2
+        for (int j = threadIdx.x; j < n; j += blockDim.x) put_gradient<T, REF>(p, g_row, first + j * V, a, z_s[j], r_s[j], f, sh, shr);
+    }
+    if (s_abort)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
 }
 
 // -------------------------------------------------------------------------------------- sums over rows
@@ -487,26 +742,26 @@ cudaError_t launch_narrow(const LossArgs &p, cudaStream_t st)
 }
 
 template <typename T, bool REF>
-cudaError_t launch_rows(const LossArgs &p, cudaStream_t st)
+cudaError_t launch_rows(LossArgs &p, int sm_count, cudaStream_t st)
 {
     constexpr int V = Row<T>::kVec;
     const int pieces = (p.A + V - 1 + V - 1) / V;  // a row may start up to V - 1 elements behind a multiple of 16 bytes
-    if (pieces <= 32 * 8) {
-        const unsigned blocks = (unsigned)(((long long)p.rows + 3) / 4);
-        if (pieces <= 32 * 4) loss_rows_kernel<T, REF, 4, true><<<blocks, 128, 0, st>>>(p);
-        else loss_rows_kernel<T, REF, 8, true><<<blocks, 128, 0, st>>>(p);
+    if (pieces <= 32 * kWarpPieces) {
+        loss_warp_kernel<T, REF><<<(unsigned)(((long long)p.rows + 3) / 4), 128, 0, st>>>(p);
         return cudaGetLastError();
     }
-    int threads = 128, share = 1;
-    while (threads < 512 && threads * 4 < pieces) threads *= 2;
-    while (share < 8 && threads * 4 * share < pieces) share *= 2;
-    const bool eight = threads * 4 * share < pieces;
-    if (threads * 8 * share < pieces) share *= 2;
-    const auto kernel = eight ? loss_rows_kernel<T, REF, 8, false> : loss_rows_kernel<T, REF, 4, false>;
-    if (share > 8) {
-        const cudaError_t e = cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-    }
+    // As few CTAs a row as keep three of them on an SM; more where the rows alone do not cover the chip.
+    const int most = 72 * 1024 / (REF ? 32 : 16);
+    int share = 1;
+    while (share < kMaxCluster && share * most < pieces) share *= 2;
+    while (share < 8 && (long long)p.rows * share < sm_count && pieces >= share * 256) share *= 2;
+    p.part_pieces = (pieces + share - 1) / share + 1;
+    const size_t smem = (size_t)p.part_pieces * (REF ? 32 : 16);
+    const int threads = std::min(kRowThreads, (p.part_pieces + 63) / 64 * 32);
+    const auto kernel = loss_rows_kernel<T, REF>;
+    cudaError_t e = allow_smem((const void *)kernel, smem);
+    if (e == cudaSuccess && share > 8) e = cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -514,6 +769,7 @@ cudaError_t launch_rows(const LossArgs &p, cudaStream_t st)
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)((long long)p.rows * share));
     cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
@@ -521,6 +777,18 @@ cudaError_t launch_rows(const LossArgs &p, cudaStream_t st)
 }
 
 }  // namespace
+
+}  // namespace accerl
+
+namespace accerl {
+
+cudaError_t policy_loss_status(int *out)  // (clears it)
+{
+    cudaError_t e = cudaMemcpyFromSymbol(out, g_status, sizeof(int));
+    const int zero = 0;
+    if (e == cudaSuccess && *out) e = cudaMemcpyToSymbol(g_status, &zero, sizeof(int));
+    return e;
+}
 
 }  // namespace accerl
 
@@ -585,11 +853,15 @@ extern "C" accerl_status accerl_policy_loss(const accerl_policy_loss_args *a, vo
     p.kl = a->kl;
     p.entropy = a->entropy;
     p.terms = a->terms;
+    p.part_pieces = 0;
+    int device = 0, sm_count = 0;
+    ACCERL_CUDA_TRY(cudaGetDevice(&device));
+    ACCERL_CUDA_TRY(cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     ACCERL_CUDA_TRY(with_dtype(a->dtype, [&](auto v) {
         using T = decltype(v);
         if (p.A <= kNarrow) return p.ref ? launch_narrow<T, true>(p, st) : launch_narrow<T, false>(p, st);
-        return p.ref ? launch_rows<T, true>(p, st) : launch_rows<T, false>(p, st);
+        return p.ref ? launch_rows<T, true>(p, sm_count, st) : launch_rows<T, false>(p, sm_count, st);
     }));
     const unsigned ctas = p.rows <= 8192 ? 1 : kStatsCluster;
     cudaLaunchConfig_t cfg = {};
