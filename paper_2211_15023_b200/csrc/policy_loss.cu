@@ -58,42 +58,50 @@ __device__ __forceinline__ float weight_of(const LossArgs &p, long long row)
     return p.weights ? p.weights[row] : (float)(1.0 / (double)p.rows);
 }
 
+__device__ __forceinline__ double exp_of(double x) { return exp(x); }
+__device__ __forceinline__ float exp_of(float x) { return expf(x); }
+__device__ __forceinline__ double expm1_of(double x) { return expm1(x); }
+__device__ __forceinline__ float expm1_of(float x) { return expm1f(x); }
+
 // What a row's sums make of it: its outputs, and the gradient's coefficients (natural logarithms: delta_v = log p_v -
 // log q_v, lp_v = log p_v):  d loss / d z_v = w p_v (base + kl_coef delta_v + entropy_coef lp_v) + w slope [v = a].
+// R: double for narrow rows; float for long ones, where this is a chain of instructions that a whole CTA waits for
+// (the difference of two log-probabilities is taken in double all the same).
+template <typename R>
 struct RowResult {
-    double base, slope;
+    R base, slope;
 };
-__device__ __forceinline__ RowResult finish_row(const LossArgs &p, long long row, double logp, double kl_full, double H,
-                                                bool empty, bool writer)
+template <typename R>
+__device__ __forceinline__ RowResult<R> finish_row(const LossArgs &p, long long row, double logp, R kl_full, R H, bool empty, bool writer)
 {
-    double kl = kl_full, slope = 0.0, pg = 0.0, r = 0.0;
+    R kl = kl_full, slope = 0, pg = 0, r = 0;
+    bool inside = true;
     if (empty) {
-        kl = H = 0.0;
+        kl = H = 0;
     } else {
-        const double adv = (double)p.advantages[row];
-        r = exp(logp - (double)p.logp_old[row]);
-        const double lo = 1.0 - (double)p.clip_low, hi = 1.0 + (double)p.clip_high;
-        const double rc = r < lo ? lo : r > hi ? hi : r;  // (a NaN stays one)
-        const double plain = r * adv, clipped = rc * adv;
-        const bool inside = !(plain > clipped);
+        const R adv = (R)p.advantages[row];
+        r = exp_of((R)(logp - (double)p.logp_old[row]));
+        const R lo = (R)1 - (R)p.clip_low, hi = (R)1 + (R)p.clip_high;
+        const R rc = r < lo ? lo : r > hi ? hi : r;  // (a NaN stays one)
+        const R plain = r * adv, clipped = rc * adv;
+        inside = !(plain > clipped);
         pg = -(inside ? plain : clipped);
-        slope = inside ? -plain : 0.0;
+        slope = inside ? -plain : (R)0;
         if (p.logp_ref) {
-            const double d = (double)p.logp_ref[row] - logp, e = expm1(d);
+            const R d = (R)((double)p.logp_ref[row] - logp), e = expm1_of(d);
             kl = e - d;
-            slope -= (double)p.kl_coef * e;
+            slope -= (R)p.kl_coef * e;
         }
-        if (writer && p.terms) *reinterpret_cast<float2 *>(p.terms + 2 * row) = make_float2((float)pg, inside ? (float)r : -(float)r);
     }
     if (writer) {
-        if (empty) *reinterpret_cast<float2 *>(p.terms + 2 * row) = make_float2(0.f, 0.f);
+        *reinterpret_cast<float2 *>(p.terms + 2 * row) = make_float2((float)pg, inside ? (float)r : -(float)r);
         p.logp[row] = (float)logp;
         p.kl[row] = (float)kl;
         p.entropy[row] = (float)H;
     }
-    RowResult o;
+    RowResult<R> o;
     o.slope = slope;
-    o.base = -slope + (double)p.entropy_coef * H - (p.ref && p.kl_coef != 0.f ? (double)p.kl_coef * kl : 0.0);
+    o.base = -slope + (R)p.entropy_coef * H - (p.ref && p.kl_coef != 0.f ? (R)p.kl_coef * kl : (R)0);
     return o;
 }
 
@@ -184,7 +192,7 @@ __global__ void __launch_bounds__(128) loss_narrow_kernel(const __grid_constant_
     const double logp = known ? ((double)za - mo) - lso : (double)NAN;
     const double kl = REF ? sd / so - (lso - lsr) : 0.0, H = lso - st / so;
     // (a row without a finite logit: log 0 everywhere, and no distribution to have a gradient)
-    const RowResult f = finish_row(p, row, empty && known ? -INFINITY : logp, kl, H, empty && known, lane == 0);
+    const RowResult<double> f = finish_row<double>(p, row, empty && known ? -INFINITY : logp, kl, H, empty && known, lane == 0);
     if (!p.grad) return;
 #pragma unroll
     for (int k = 0; k < kNarrowPer; ++k) {
@@ -264,23 +272,35 @@ __device__ __forceinline__ uint32_t *words(uint4 &v) { return reinterpret_cast<u
 struct RowCoef {
     float c, cr, k0, kt, kr, at_a;
 };
+// log2 of a positive sum: the exponent and the mantissa's logarithm apart, off by 1e-7 whatever its size
+__device__ __forceinline__ double log2_of(double x)
+{
+    const int hi = __double2hiint(x);
+    if (hi < 0x00100000 || hi >= 0x7ff00000) return (double)log2f((float)x);  // (0, infinity, NaN)
+    const double m = __hiloint2double((hi & 0x000fffff) | 0x3ff00000, __double2loint(x));
+    return (double)((hi >> 20) - 1023) + (double)log2f((float)m);
+}
+
 template <bool REF>
-__device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, float w, bool known, float za, double C, double CR, double so,
+__device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, float w, bool known, float za, float C, float CR, double so,
                                             double st, double ss, double sd, bool writer)
 {
     const bool empty = known && C == -INFINITY;
-    const double lso = log2(so), lsr = REF ? log2(ss) : 0.0;
-    const double kl = REF ? kLn2 * (sd / so - (lso - lsr)) : 0.0, H = kLn2 * (lso - st / so);
-    const double logp = empty ? (double)-INFINITY : known ? ((double)za - C) - kLn2 * lso : (double)NAN;
-    const RowResult f = finish_row(p, row, logp, kl, H, empty, writer);
-    const double scale = (double)w / so, kk = REF ? (double)p.kl_coef * kLn2 : 0.0, ke = (double)p.entropy_coef * kLn2;
+    const float fo = (float)so, fs = (float)ss, inv = 1.f / fo;
+    const double lso = log2_of(so);
+    // log2(S / S') from the difference of the sums where they are near each other
+    const float d = (float)(so - ss) / fs, ratio = REF ? (fabsf(d) < 0.5f ? log1pf(d) * kLog2e : (float)(lso - log2_of(ss))) : 0.f;
+    const float H = (float)kLn2 * (float)(lso - (double)((float)st * inv)), kl = REF ? (float)kLn2 * ((float)sd * inv - ratio) : 0.f;
+    const double logp = empty ? (double)-INFINITY : known ? ((double)za - (double)C) - kLn2 * lso : (double)NAN;
+    const RowResult<float> f = finish_row<float>(p, row, logp, kl, H, empty, writer);
+    const float scale = w * inv, kk = REF ? p.kl_coef * (float)kLn2 : 0.f, ke = p.entropy_coef * (float)kLn2;
     RowCoef r;
-    r.c = (float)C;
-    r.cr = (float)CR;
-    r.k0 = empty ? 0.f : (float)(scale * (f.base - ke * lso - (kk != 0.0 ? kk * (lso - lsr) : 0.0)));
-    r.kt = empty ? 0.f : (float)(scale * (ke + kk));
-    r.kr = empty ? 0.f : (float)(scale * kk);
-    r.at_a = empty ? 0.f : (float)((double)w * f.slope);
+    r.c = C;
+    r.cr = CR;
+    r.k0 = empty ? 0.f : scale * (f.base - ke * (float)lso - (kk != 0.f ? kk * ratio : 0.f));
+    r.kt = empty ? 0.f : scale * (ke + kk);
+    r.kr = empty ? 0.f : scale * kk;
+    r.at_a = empty ? 0.f : w * f.slope;
     return r;
 }
 
@@ -454,15 +474,15 @@ struct Partial {  // of one CTA: maxima, and sums relative to them
 // for its cluster, the others compute and write.  What bounds it beside HBM is the instructions a logit (14, 25 with a
 // reference row, where memory leaves 22 and 33): so -inf is made finite and the maximum found two 16-bit logits at a
 // time, t is one multiply-add of the logit, and what depends on the row only is worked out, in double, by one warp.
-// Sums of a thread are float (some 50 terms), from there on double.
-constexpr int kMaxCluster = 16, kRowThreads = 512;
+// Sums of a warp are float, from there on double.
+constexpr int kMaxCluster = 16, kRowThreads = 256;
 template <typename T, bool REF>
-__global__ void __launch_bounds__(kRowThreads, 2) loss_rows_kernel(const __grid_constant__ LossArgs p)
+__global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_constant__ LossArgs p)
 {
     constexpr int V = Row<T>::kVec;
     extern __shared__ __align__(128) uint4 s_piece[];  // [REF ? 2 : 1][pieces of a part]
     __shared__ Partial parts[kMaxCluster];
-    __shared__ double s_sum[kRowThreads / 32][4];
+    __shared__ float4 s_sum[kRowThreads / 32];
     __shared__ float s_max[2][kRowThreads / 32];
     __shared__ RowCoef s_row;
     __shared__ uint64_t s_bar;
@@ -491,6 +511,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) loss_rows_kernel(const __grid_
     uint4 *z_s = s_piece, *r_s = s_piece + (REF ? p.part_pieces : 0);
     const bool alike = phase_of(r_row) == phase;
     const int whole0 = first < 0 ? 1 : 0, whole1 = first + n * V > p.A ? n - 1 : n;  // whole pieces of the part
+    if (threadIdx.x < 2 * (kRowThreads / 32)) s_max[threadIdx.x / (kRowThreads / 32)][threadIdx.x % (kRowThreads / 32)] = -INFINITY;
     if (threadIdx.x == 0) {
         s_abort = 0;
         mbar_init(smem_u32(&s_bar), 1);
@@ -541,8 +562,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) loss_rows_kernel(const __grid_
         return which && word_min<T>(least) == -INFINITY;
     };
     auto block_max = [&](int which) {
-        float c = s_max[which][0];
-        for (int i = 1; i < warps; ++i) c = max_nan(c, s_max[which][i]);
+        float c = s_max[which][lane & (kRowThreads / 32 - 1)];
+#pragma unroll
+        for (int o = kRowThreads / 64; o > 0; o >>= 1) c = max_nan(c, __shfl_xor_sync(0xffffffffu, c, o));
         return c;
     };
     // a part with nothing above the low value: read again, relative to its own maximum (returned; -inf: no logit)
@@ -585,25 +607,22 @@ __global__ void __launch_bounds__(kRowThreads, 2) loss_rows_kernel(const __grid_
         for (int j = threadIdx.x; j < n; j += blockDim.x) add_sums<T, REF>(z_s[j], r_s[j], sh, shr, so, st, ss, sd);
     }
     if (holes && without_q(z_row, r_row, max(first, 0) + (int)threadIdx.x, min(first + n * V, p.A), (int)blockDim.x, c)) sd = INFINITY;
-    double sums[4] = {so, st, ss, sd};
+    float sums[4] = {so, st, ss, sd};
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
         for (int i = 0; i < (REF ? 4 : 2); ++i) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], o);
-    if (lane == 0)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s_sum[warp][i] = sums[i];
+    if (lane == 0) s_sum[warp] = make_float4(sums[0], sums[1], sums[2], sums[3]);
     __syncthreads();
     asm volatile("barrier.cluster.wait;" ::: "memory");  // every CTA of the cluster has started
     if (warp == 0) {
         Partial mine;
-        double v[4];
+        const float4 part = lane < warps ? s_sum[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+        double v[4] = {part.x, part.y, part.z, part.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = lane < warps ? s_sum[lane][i] : 0.0;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int o = kRowThreads / 64; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        }
         mine.so = c == -INFINITY ? 0.0 : v[0];
         mine.st = c == -INFINITY ? 0.0 : v[1];
         mine.ss = cr == -INFINITY ? 0.0 : v[2];
@@ -626,10 +645,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) loss_rows_kernel(const __grid_
             CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
         }
         // a part's sums, relative to the row's maxima
-        const double d = b.so != 0.0 ? ((double)b.c - (double)C) * (double)kLog2e : 0.0;
-        const double dr = b.ss != 0.0 ? ((double)b.cr - (double)CR) * (double)kLog2e : 0.0;
-        const double f = exp2(d);
-        double v[4] = {f * b.so, f != 0.0 ? f * (b.st + d * b.so) : 0.0, exp2(dr) * b.ss, f != 0.0 ? f * (b.sd + (d - dr) * b.so) : 0.0};
+        const float d = b.so != 0.0 ? (b.c - C) * kLog2e : 0.f, dr = b.ss != 0.0 ? (b.cr - CR) * kLog2e : 0.f;
+        const double f = (double)exp2f(d), df = (double)d, dd = (double)(d - dr);
+        double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, (double)exp2f(dr) * b.ss, f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -750,7 +768,7 @@ cudaError_t launch_rows(LossArgs &p, int sm_count, cudaStream_t st)
         loss_warp_kernel<T, REF><<<(unsigned)(((long long)p.rows + 3) / 4), 128, 0, st>>>(p);
         return cudaGetLastError();
     }
-    // As few CTAs a row as keep three of them on an SM; more where the rows alone do not cover the chip.
+    // As few CTAs a row as keep three of them on an SM (72 KB each); more where the rows alone do not cover the chip.
     const int most = 72 * 1024 / (REF ? 32 : 16);
     int share = 1;
     while (share < kMaxCluster && share * most < pieces) share *= 2;
