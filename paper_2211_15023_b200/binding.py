@@ -308,8 +308,12 @@ def policy_loss(logits, actions, logp_old, advantages, weights=None, logits_ref=
     ``stats`` holds the loss, the weighted sums of the clipped objective, KL, entropy and clipped rows, the sum of
     weights, the largest KL and the weighted sum of ratios.
     """
-    import torch
     low, high = clip if isinstance(clip, (tuple, list)) else (clip, clip)
+    r = (_CALLS or _calls()).policy_loss(logits, actions, logp_old, advantages, weights, logits_ref, logp_ref, low, high,
+                                         kl_coef, entropy_coef, grad, stream)
+    if r is not None:
+        return _done(r)
+    import torch
     code = _dtype_code(logits.dtype)
     _check_rows(logits)
     t, v = int(logits.shape[0]), int(logits.shape[1])
@@ -360,6 +364,10 @@ def ckpt_save(x, act="none", out=None, stream=None):
     """accerl_ckpt_save of CUDA rows x [T, K] (fp32, bf16, fp16): returns (y, (q, e)) with y = act(x), act one of "none"
     (y is x), "relu", "gelu", "silu".  ``out``: where to write y, x itself among the choices.  The checkpoint is
     q int8 [T, K32], e uint8 [T, K32 / 32], K32 = K rounded up to 32."""
+    if out is None:
+        r = (_CALLS or _calls()).ckpt_save(x, _ACTS[act], stream)
+        if r is not None:
+            return _done(r)
     import torch
     code = _dtype_code(x.dtype)
     _check_rows(x)
@@ -380,6 +388,10 @@ def ckpt_save(x, act="none", out=None, stream=None):
 
 def ckpt_load(ckpt, cols, dtype, out=None, stream=None):
     """accerl_ckpt_load: the values [T, cols] that a checkpoint stands for, in ``dtype`` (or into ``out``)."""
+    if out is None:
+        r = (_CALLS or _calls()).ckpt_load(ckpt, cols, dtype, stream)
+        if r is not None:
+            return _done(r)
     import torch
     t = int(ckpt[0].shape[0])
     if out is None:
@@ -396,6 +408,10 @@ def ckpt_load(ckpt, cols, dtype, out=None, stream=None):
 
 def ckpt_act_backward(dy, ckpt, act, out=None, stream=None):
     """accerl_ckpt_act_backward: dx = dy act'(x^) for CUDA rows dy [T, K]; ``out`` may be dy."""
+    if out is None:
+        r = (_CALLS or _calls()).ckpt_act_backward(dy, ckpt, _ACTS[act], stream)
+        if r is not None:
+            return _done(r)
     import torch
     code = _dtype_code(dy.dtype)
     _check_rows(dy)
@@ -421,6 +437,10 @@ def ckpt_weight_grad(dy, ckpt, cols, out_dtype=None, bias=True, out=None, accumu
     """accerl_ckpt_weight_grad: (dw [N, K], db [N] or None) from CUDA rows dy [T, N] (bf16 or fp16) and the checkpoint of
     the layer's input [T, K = cols].  ``out_dtype`` fp32 or dy's type (the default); ``out`` = (dw, db) to write, or with
     ``accumulate`` (fp32) to add to; db None leaves it out, as does ``bias`` False."""
+    if out is None and not accumulate:
+        r = (_CALLS or _calls()).ckpt_weight_grad(dy, ckpt, cols, out_dtype, bias, stream)
+        if r is not None:
+            return _done(r)
     import torch
     code = _dtype_code(dy.dtype)
     _check_rows(dy)
@@ -457,6 +477,9 @@ def quant_rows(x, stream=None):
     """accerl_quant_rows of CUDA rows x [T, K] (fp32, bf16, fp16): (q int8 [T, K], scale fp32 [T]), one scale a row: the
     tokens of a batch of activations, or the channels of weights [out, in].  The rows of q start at multiples of 16
     bytes (its row stride is K rounded up to 16), as linear_i8 reads them."""
+    r = (_CALLS or _calls()).quant_rows(x, stream)
+    if r is not None:
+        return _done(r)
     import torch
     code = _dtype_code(x.dtype)
     _check_rows(x)
@@ -484,8 +507,12 @@ def linear_i8(x, weight, bias=None, relu=False, out_dtype=None, out=None, stream
     """accerl_linear_i8: y [T, N] = (x quantised per token) times weight = (q int8 [N, K], scale fp32 [N]) as quant_rows
     makes it of [N, K], plus ``bias`` fp32 [N], through a ReLU where asked.  x is CUDA rows [T, K] (fp32, bf16, fp16),
     or a pair (q, scale) of quant_rows; y has x's type (fp32 for a pair) or ``out_dtype``, or is ``out``."""
-    import torch
     wq, ws = weight
+    if out is None:
+        r = (_CALLS or _calls()).linear_i8(x, wq, ws, bias, relu, out_dtype, stream)
+        if r is not None:
+            return _done(r)
+    import torch
     given = isinstance(x, (tuple, list))
     xq, xs = x if given else (x, None)
     code = 3 if given else _dtype_code(xq.dtype)
