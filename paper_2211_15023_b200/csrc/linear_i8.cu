@@ -316,6 +316,184 @@ accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArg
     return ACCERL_OK;
 }
 
+// Many tokens: pairs of CTAs on tiles of 256 channels x 256 tokens, persistent.  A CTA holds 128 channels and 128 tokens of a
+// stage (32 KB for 128 bytes of K) and 128 of the accumulator's rows: an instruction of the pair reads 8 KB of operands per
+// SM in 128 cycles, half of what a single CTA's 128 x 256 tile would.  Two accumulators fill tensor memory, so that four
+// warps write a tile out while the next one is computed.
+constexpr int kPairTile = 256, kPairStages = 6, kPairStage = 2 * 128 * 128, kPairThreads = 192;
+constexpr int kGroup = 8;  // token tiles whose channel tiles are walked together: their operands stay in L2
+
+__device__ __forceinline__ void pair_tile(const LinearArgs &p, int tile, int *channel, int *token)
+{
+    const int ct = (p.n + kPairTile - 1) / kPairTile, tt = (p.tokens + kPairTile - 1) / kPairTile;
+    const int group = tile / (ct * kGroup), rest = tile - group * ct * kGroup, rows = min(kGroup, tt - group * kGroup);
+    *token = (group * kGroup + rest % rows) * kPairTile;
+    *channel = rest / rows * kPairTile;
+}
+
+__global__ void __launch_bounds__(kPairThreads, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                   const __grid_constant__ LinearArgs p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ struct {
+        uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2];
+        uint32_t tmem;
+        int abort_flag;
+    } bars;
+    __shared__ float4 s_scale[4][8];
+    namespace cg = cooperative_groups;
+    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t base = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cg::this_cluster().block_rank();
+    const int tiles = ((p.n + kPairTile - 1) / kPairTile) * ((p.tokens + kPairTile - 1) / kPairTile);
+    const int first = (int)blockIdx.x >> 1, stride = (int)gridDim.x >> 1;
+    volatile int *abort_flag = &bars.abort_flag;
+    auto bar = [](uint64_t &b) { return smem_u32(&b); };
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kPairStages; ++s) {
+            mbar_init(bar(bars.full[s]), 1);   // the first CTA's counts the loads of both
+            mbar_init(bar(bars.empty[s]), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(bar(bars.acc_full[a]), 1);
+            mbar_init(bar(bars.acc_empty[a]), 8);  // the first CTA's: four warps of each
+        }
+        bars.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async();
+    }
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    cg::this_cluster().sync();
+    fence_after();
+    const uint32_t tmem = bars.tmem;
+    bool ok = true;
+
+    if (warp == 4) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        int s = 0;
+        uint32_t phase = 0;
+        for (int u = first; u < tiles && ok; u += stride) {
+            int n0, t0;
+            pair_tile(p, u, &n0, &t0);
+            for (int c = 0; c < p.chunks && ok; ++c) {
+                ok = mbar_wait(bar(bars.empty[s]), phase ^ 1, abort_flag, &g_status, 1);
+                if (ok && elect_one()) {
+                    const uint32_t full = peer_addr(bar(bars.full[s]), 0);
+                    if (rank == 0) mbar_expect_tx(bar(bars.full[s]), 2 * kPairStage);
+                    tma_load_2d_pair(base + s * kPairStage, &map_w, c * 128, n0 + 128 * rank, full);
+                    tma_load_2d_pair(base + s * kPairStage + 128 * 128, &map_x, c * 128, t0 + 128 * rank, full);
+                }
+                __syncwarp();
+                if (++s == kPairStages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+    } else if (warp == 5 && rank == 0) {
+        constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+        int s = 0, a = 0;
+        uint32_t phase = 0, aphase = 0;
+        for (int u = first; u < tiles && ok; u += stride) {
+            ok = mbar_wait(bar(bars.acc_empty[a]), aphase ^ 1, abort_flag, &g_status, 4);
+            fence_after();
+            for (int c = 0; c < p.chunks && ok; ++c) {
+                ok = mbar_wait(bar(bars.full[s]), phase, abort_flag, &g_status, 8);
+                fence_after();
+                if (ok && elect_one()) {
+                    const uint64_t ad = make_desc(base + s * kPairStage, 128), bd = make_desc(base + s * kPairStage + 128 * 128, 128);
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks) mma_i8_pair(tmem + 256 * a, ad + 2 * ks, bd + 2 * ks, idesc, (uint32_t)(c | ks));
+                    mma_commit_pair(bar(bars.empty[s]));
+                    if (c == p.chunks - 1) mma_commit_pair(bar(bars.acc_full[a]));
+                }
+                __syncwarp();
+                if (++s == kPairStages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            }
+            if ((a ^= 1) == 0) aphase ^= 1;
+        }
+    } else if (warp < 4) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");  // the tokens' scales are the quantiser's
+        int a = 0;
+        uint32_t aphase = 0;
+        for (int u = first; u < tiles && ok; u += stride) {
+            int n0, t0;
+            pair_tile(p, u, &n0, &t0);
+            const int n = n0 + 128 * rank + 32 * warp + lane;
+            const bool mine = n < p.n;
+            const float ws = mine ? p.w_scale[n] : 0.f, bias = mine && p.bias ? p.bias[n] : 0.f;
+            ok = mbar_wait(bar(bars.acc_full[a]), aphase, abort_flag, &g_status, 16);
+            fence_after();
+            const int have = min(kPairTile, p.tokens - t0);
+            for (int j = 0; j < have; j += 32) {
+                int acc[32];
+                tmem_ld32(tmem + 256 * a + ((uint32_t)(warp * 32) << 16) + j, acc);
+                __syncwarp();
+                reinterpret_cast<float *>(s_scale[warp])[lane] = t0 + j + lane < p.tokens ? __ldg(p.x_scale + t0 + j + lane) : 0.f;
+                __syncwarp();
+                tmem_wait_ld();
+                if (mine) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 xs = s_scale[warp][i / 4];
+                        const float sc[4] = {xs.x, xs.y, xs.z, xs.w};
+#pragma unroll
+                        for (int l = 0; l < 4; ++l) {
+                            float v = fmaf((float)acc[i + l], sc[l] * ws, bias);
+                            if (p.relu && v < 0.f) v = 0.f;
+                            if (j + i + l < have) store_y(p, t0 + j + i + l, n, v);
+                        }
+                    }
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(peer_addr(bar(bars.acc_empty[a]), 0));
+            if ((a ^= 1) == 0) aphase ^= 1;
+        }
+    }
+    if (*abort_flag)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    cg::this_cluster().sync();  // no barrier of a CTA is signalled once it has gone
+    if (warp == 5)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+accerl_status launch_pair(const CUtensorMap &mw, const CUtensorMap &mx, const LinearArgs &p, int sm_count, bool after_quant, cudaStream_t st)
+{
+    const size_t smem = 1024 + (size_t)kPairStages * kPairStage;
+    const long long tiles = ((p.n + kPairTile - 1LL) / kPairTile) * ((p.tokens + kPairTile - 1LL) / kPairTile);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(2u * (unsigned)std::min<long long>(tiles, sm_count / 2));
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = after_quant ? 2 : 1;
+    ACCERL_CUDA_TRY(allow_smem((const void *)linear_pair_kernel, smem));
+    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_pair_kernel, mw, mx, p));
+    return ACCERL_OK;
+}
+
 bool good_quant(const char *who, const void *x, long long ld_x, int dtype, long long rows, int cols)
 {
     if (rows < 1 || cols < 1 || cols > (1 << 30) || rows > (1LL << 31) - 1 || rows > (1LL << 40) / cols) {
@@ -370,6 +548,10 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
         set_error("linear_i8: null argument");
         return ACCERL_ERR_INVALID_ARG;
     }
+    if ((a->n + 255LL) / 256 * ((a->tokens + 255LL) / 256) > (1 << 30)) {
+        set_error("linear_i8: tokens * n is too large");
+        return ACCERL_ERR_INVALID_ARG;
+    }
     if (a->tokens < 1 || a->n < 1 || a->k < 1 || a->k > 131072) {
         set_error("linear_i8: tokens, n and k must be positive, k at most 131072 (an int32 sum of products of 127)");
         return ACCERL_ERR_INVALID_ARG;
@@ -407,6 +589,8 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
         xq = a->workspace;
         xs = reinterpret_cast<const float *>(static_cast<char *>(a->workspace) + quantised_bytes(a->tokens, a->k));
     }
+    const long long pair_tiles = ((a->n + kPairTile - 1LL) / kPairTile) * ((a->tokens + kPairTile - 1LL) / kPairTile);
+    const bool pair = a->tokens > 256 && 4 * pair_tiles >= sm_count;
     const int nt = a->tokens <= 16 ? 16 : a->tokens <= 32 ? 32 : a->tokens <= 64 ? 64 : 128;
     accerl_status s = tc_make_map(&mw, a->w, a->n, a->k, a->ld_w, 128, 128);
     if (s == ACCERL_OK) s = tc_make_map(&mx, xq, a->tokens, a->k, ld_xq, nt, 128);
@@ -416,6 +600,7 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
         ACCERL_CUDA_TRY(with_dtype(a->x_dtype, [&](auto v) { return launch_quant<decltype(v)>(q, st); }));
     }
     LinearArgs p{xs, a->w_scale, a->bias, a->y, a->ld_y, a->tokens, a->n, a->k, a->y_dtype, a->relu != 0, (a->k + 127) / 128, 0};
+    if (pair) return launch_pair(mw, mx, p, sm_count, !given, st);
     return nt == 16   ? launch_few<16>(mw, mx, p, sm_count, !given, st)
            : nt == 32 ? launch_few<32>(mw, mx, p, sm_count, !given, st)
            : nt == 64 ? launch_few<64>(mw, mx, p, sm_count, !given, st)
