@@ -94,7 +94,8 @@ __device__ __forceinline__ float byte_value(uint32_t flipped, int k)
     return __uint_as_float(__byte_perm(flipped, 0x4b000000u, 0x7440u | (unsigned)k)) - 8388736.f;  // 2^23 + 128
 }
 
-template <typename T, int MODE, int ACT>
+// ALIGNED: the rows of both arrays start at multiples of 16 bytes
+template <typename T, int MODE, int ACT, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) ckpt_kernel(const __grid_constant__ CkptArgs p)
 {
     constexpr int V = Row<T>::kVec, kWords = V / 4, kLanes = 32 / V;  // lanes of a block
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) ckpt_kernel(const __grid_constant__ 
             at[i] = piece * V;
             if constexpr (MODE != kLoad) {
                 const T *in = static_cast<const T *>(p.in) + row[i] * p.ld_in;
-                raw[i] = live[i] ? load_piece<T>(in, at[i], p.cols, 0.f) : make_uint4(0, 0, 0, 0);
+                raw[i] = live[i] ? load_piece<T, ALIGNED>(in, at[i], p.cols, 0.f) : make_uint4(0, 0, 0, 0);
             }
             if constexpr (MODE != kSave) {
 #pragma unroll
@@ -178,10 +179,21 @@ __global__ void __launch_bounds__(kThreads) ckpt_kernel(const __grid_constant__ 
             }
             if (live[i] && p.out) {
                 T *out = static_cast<T *>(p.out) + row[i] * p.ld_out;
-                store_piece<T>(out, at[i], p.cols, v);
+                store_piece<T, ALIGNED>(out, at[i], p.cols, v);
             }
         }
     }
+}
+
+template <typename T, int MODE, bool ALIGNED>
+auto kernel_of(int act)
+{
+    if constexpr (MODE != kLoad) {
+        if (act == ACCERL_ACT_RELU) return ckpt_kernel<T, MODE, ACCERL_ACT_RELU, ALIGNED>;
+        if (act == ACCERL_ACT_GELU) return ckpt_kernel<T, MODE, ACCERL_ACT_GELU, ALIGNED>;
+        if (act == ACCERL_ACT_SILU) return ckpt_kernel<T, MODE, ACCERL_ACT_SILU, ALIGNED>;
+    }
+    return ckpt_kernel<T, MODE, ACCERL_ACT_NONE, ALIGNED>;
 }
 
 template <int MODE>
@@ -202,14 +214,10 @@ accerl_status launch(CkptArgs &p, int dtype, int act, void *cuda_stream)
     }
     const unsigned blocks = (unsigned)(p.units < (1LL << 30) ? p.units : (1LL << 30));
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    const bool aligned = (MODE == kLoad || rows_aligned(p.in, p.ld_in, dtype)) && (!p.out || rows_aligned(p.out, p.ld_out, dtype));
     ACCERL_CUDA_TRY(with_dtype(dtype, [&](auto v) {
         using T = decltype(v);
-        auto kernel = ckpt_kernel<T, MODE, ACCERL_ACT_NONE>;
-        if constexpr (MODE != kLoad) {
-            if (act == ACCERL_ACT_RELU) kernel = ckpt_kernel<T, MODE, ACCERL_ACT_RELU>;
-            if (act == ACCERL_ACT_GELU) kernel = ckpt_kernel<T, MODE, ACCERL_ACT_GELU>;
-            if (act == ACCERL_ACT_SILU) kernel = ckpt_kernel<T, MODE, ACCERL_ACT_SILU>;
-        }
+        const auto kernel = aligned ? kernel_of<T, MODE, true>(act) : kernel_of<T, MODE, false>(act);
         kernel<<<blocks, kThreads, 0, st>>>(p);
         return cudaGetLastError();
     }));

@@ -141,18 +141,22 @@ __device__ __forceinline__ uint4 load_piece(const T *row, int first, int n, floa
     for (int k = 0; k < V; ++k) v[k] = first + k >= 0 && first + k < n ? to_float(row[first + k]) : fill;
     return pack<T>(v);
 }
-template <typename T>
+template <typename T, bool ALIGNED = false>
 __device__ __forceinline__ void store_piece(T *row, int first, int n, const float (&v)[Row<T>::kVec])
 {
     constexpr int V = Row<T>::kVec;
     if (first >= 0 && first + V <= n) {
-        store16(row + first, pack<T>(v));
+        if (ALIGNED) *reinterpret_cast<uint4 *>(row + first) = pack<T>(v);
+        else store16(row + first, pack<T>(v));
         return;
     }
 #pragma unroll
     for (int k = 0; k < V; ++k)
         if (first + k >= 0 && first + k < n) row[first + k] = from_float<T>(v[k]);
 }
+
+// do all rows of an array start at multiples of 16 bytes?
+inline bool rows_aligned(const void *p, long long ld, int dtype) { return !(((uintptr_t)p | (uintptr_t)(ld * dtype_size(dtype))) & 15); }
 
 // elements of type T by which an address lies behind a multiple of 16 bytes
 template <typename T>

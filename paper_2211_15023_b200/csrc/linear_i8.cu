@@ -36,20 +36,21 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 // four values to four int8; `exact`: the scale's reciprocal is not to be trusted
 __device__ __forceinline__ uint32_t quantised4(const float *v, float s, float inv, bool exact)
 {
-    float q[4], d = 0.f;
+    const float magic = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer, in the low byte of the sum
+    float b4[4], d = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const float t = v[k] * inv;
-        q[k] = rintf(t);
-        d = fmaxf(d, fabsf(t - q[k]));
+        b4[k] = t + magic;
+        d = fmaxf(d, fabsf(t - (b4[k] - magic)));
     }
     if (exact || d > 0.49996f) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) q[k] = fminf(fmaxf(rintf(__fdiv_rn(v[k], s)), -127.f), 127.f);
+        for (int k = 0; k < 4; ++k) b4[k] = fminf(fmaxf(rintf(__fdiv_rn(v[k], s)), -127.f), 127.f) + magic;
     }
     uint32_t b[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(q[k] + 12582912.f);  // the integer in the low byte
+    for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(b4[k]);
     return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }
 
@@ -75,8 +76,8 @@ __device__ __forceinline__ void quantise_piece(const QuantArgs &p, int8_t *q_row
 }
 
 // WARP: a warp per row, four rows a CTA; else a CTA per row.  NV pieces of 16 bytes a thread stay in registers; a row
-// that has more (LOOP) is read twice.
-template <typename T, int NV, bool WARP, bool LOOP>
+// that has more (LOOP) is read twice.  ALIGNED: rows at multiples of 16 bytes.
+template <typename T, int NV, bool WARP, bool LOOP, bool ALIGNED>
 __global__ void __launch_bounds__(WARP ? 128 : 1024) quant_rows_kernel(const __grid_constant__ QuantArgs p)
 {
     constexpr int V = Row<T>::kVec;
@@ -97,11 +98,11 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) quant_rows_kernel(const __g
         for (int k = 0; k < V; ++k) top = max(top, magnitude(v[k]));
     };
 #pragma unroll
-    for (int i = 0; i < NV; ++i) raw[i] = load_piece<T>(x, first + i * step, p.cols, 0.f);
+    for (int i = 0; i < NV; ++i) raw[i] = load_piece<T, ALIGNED>(x, first + i * step, p.cols, 0.f);
 #pragma unroll
     for (int i = 0; i < NV; ++i) take(raw[i]);
     if constexpr (LOOP)
-        for (int at = first + NV * step; at < p.cols; at += step) take(load_piece<T>(x, at, p.cols, 0.f));
+        for (int at = first + NV * step; at < p.cols; at += step) take(load_piece<T, ALIGNED>(x, at, p.cols, 0.f));
     top = __reduce_max_sync(0xffffffffu, top);
     if constexpr (!WARP) {
         if (lane == 0) s_top[warp] = top;
@@ -117,22 +118,35 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) quant_rows_kernel(const __g
     for (int i = 0; i < NV; ++i) quantise_piece<T>(p, q, first + i * step, raw[i], s, inv, exact, zero);
     if constexpr (LOOP)
         for (int at = first + NV * step; at < p.cols; at += step)
-            quantise_piece<T>(p, q, at, load_piece<T>(x, at, p.cols, 0.f), s, inv, exact, zero);
+            quantise_piece<T>(p, q, at, load_piece<T, ALIGNED>(x, at, p.cols, 0.f), s, inv, exact, zero);
 }
 
-template <typename T>
-cudaError_t launch_quant(const QuantArgs &p, cudaStream_t st)
+template <typename T, bool ALIGNED>
+cudaError_t launch_quant(const QuantArgs &p, int sm_count, cudaStream_t st)
 {
     const long long pieces = ((long long)p.cols + Row<T>::kVec - 1) / Row<T>::kVec;
-    if (pieces <= 32 * 4) {
-        quant_rows_kernel<T, 4, true, false><<<(unsigned)((p.rows + 3) / 4), 128, 0, st>>>(p);
+    // Few rows: two pieces a thread, the shortest chain.  Many: eight, since what a thread does once for its row (two
+    // divisions, the reduction) is some hundred instructions.
+    const bool few = p.rows < 2 * sm_count;
+    if (!few && pieces <= 32 * 8) {
+        quant_rows_kernel<T, 8, true, false, ALIGNED><<<(unsigned)((p.rows + 3) / 4), 128, 0, st>>>(p);
         return cudaGetLastError();
     }
-    int threads = 128;
-    while (threads < 1024 && threads * 4 < pieces) threads *= 2;
-    if (threads * 4 >= pieces) quant_rows_kernel<T, 4, false, false><<<(unsigned)p.rows, threads, 0, st>>>(p);
-    else quant_rows_kernel<T, 4, false, true><<<(unsigned)p.rows, threads, 0, st>>>(p);
+    const long long want = few ? (pieces + 1) / 2 : (pieces + 7) / 8;
+    const int threads = (int)std::min<long long>(1024, (want + 31) / 32 * 32);
+    const auto kernel = threads * 2 >= pieces   ? quant_rows_kernel<T, 2, false, false, ALIGNED>
+                        : threads * 8 >= pieces ? quant_rows_kernel<T, 8, false, false, ALIGNED>
+                                                : quant_rows_kernel<T, 8, false, true, ALIGNED>;
+    kernel<<<(unsigned)p.rows, threads, 0, st>>>(p);
     return cudaGetLastError();
+}
+
+cudaError_t launch_quant(const QuantArgs &p, int dtype, int sm_count, cudaStream_t st)
+{
+    return with_dtype(dtype, [&](auto v) {
+        using T = decltype(v);
+        return rows_aligned(p.x, p.ld_x, dtype) ? launch_quant<T, true>(p, sm_count, st) : launch_quant<T, false>(p, sm_count, st);
+    });
 }
 
 // ------------------------------------------------------------------------------------------------ product
@@ -151,6 +165,13 @@ __device__ __forceinline__ void store_y(const LinearArgs &p, int t, int n, float
     if (p.y_dtype == ACCERL_F32) static_cast<float *>(p.y)[at] = v;
     else if (p.y_dtype == ACCERL_BF16) static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
     else static_cast<__half *>(p.y)[at] = __float2half_rn(v);
+}
+
+__device__ __forceinline__ float at_least(float v, float floor)  // (a NaN stays one)
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(v), "f"(floor));
+    return m;
 }
 
 constexpr int kFewThreads = 192, kMaxStages = 8;
@@ -251,9 +272,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the tokens' scales are the quantiser's
     auto finish = [&](int t, int acc) {
         if (!mine || t >= p.tokens) return;
-        float v = fmaf((float)acc, p.x_scale[t] * ws, bias);
-        if (p.relu && v < 0.f) v = 0.f;
-        store_y(p, t, n, v);
+        store_y(p, t, n, at_least(fmaf((float)acc, p.x_scale[t] * ws, bias), p.relu ? 0.f : -INFINITY));
     };
     int *part = reinterpret_cast<int *>(smem);  // [NT][128]: every operand has been read
     if (warp < 4) {
@@ -318,9 +337,10 @@ accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArg
 
 // Many tokens: pairs of CTAs on tiles of 256 channels x 256 tokens, persistent.  A CTA holds 128 channels and 128 tokens of a
 // stage (32 KB for 128 bytes of K) and 128 of the accumulator's rows: an instruction of the pair reads 8 KB of operands per
-// SM in 128 cycles, half of what a single CTA's 128 x 256 tile would.  Two accumulators fill tensor memory, so that four
-// warps write a tile out while the next one is computed.
-constexpr int kPairTile = 256, kPairStages = 6, kPairStage = 2 * 128 * 128, kPairThreads = 192;
+// SM in 128 cycles, half of what a single CTA's 128 x 256 tile would.  Two accumulators fill tensor memory, so that eight
+// warps (each 32 channels by 128 tokens, neighbouring lanes neighbours in a row of y) write a tile out while the next
+// one is computed; that takes some 8 instructions a value, and with four warps bounded the kernel.
+constexpr int kPairTile = 256, kPairStages = 6, kPairStage = 2 * 128 * 128, kPairOut = 8, kPairThreads = 32 * (kPairOut + 2);
 constexpr int kGroup = 8;  // token tiles whose channel tiles are walked together: their operands stay in L2
 
 __device__ __forceinline__ void pair_tile(const LinearArgs &p, int tile, int *channel, int *token)
@@ -331,6 +351,7 @@ __device__ __forceinline__ void pair_tile(const LinearArgs &p, int tile, int *ch
     *channel = rest / rows * kPairTile;
 }
 
+template <typename T>
 __global__ void __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                    const __grid_constant__ LinearArgs p)
@@ -341,7 +362,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         uint32_t tmem;
         int abort_flag;
     } bars;
-    __shared__ float4 s_scale[4][8];
+    __shared__ float4 s_scale[kPairOut][8];
     namespace cg = cooperative_groups;
     uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t base = smem_u32(smem);
@@ -358,13 +379,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(bar(bars.acc_full[a]), 1);
-            mbar_init(bar(bars.acc_empty[a]), 8);  // the first CTA's: four warps of each
+            mbar_init(bar(bars.acc_empty[a]), 2 * kPairOut);  // the first CTA's: the writing warps of both
         }
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
     }
-    if (warp == 5) {
+    if (warp == kPairOut + 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
@@ -375,7 +396,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     const uint32_t tmem = bars.tmem;
     bool ok = true;
 
-    if (warp == 4) {
+    if (warp == kPairOut) {
         asm volatile("griddepcontrol.wait;" ::: "memory");
         int s = 0;
         uint32_t phase = 0;
@@ -397,7 +418,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                 }
             }
         }
-    } else if (warp == 5 && rank == 0) {
+    } else if (warp == kPairOut + 1 && rank == 0) {
         constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
         int s = 0, a = 0;
         uint32_t phase = 0, aphase = 0;
@@ -422,37 +443,38 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
             }
             if ((a ^= 1) == 0) aphase ^= 1;
         }
-    } else if (warp < 4) {
+    } else if (warp < kPairOut) {
         asm volatile("griddepcontrol.wait;" ::: "memory");  // the tokens' scales are the quantiser's
+        const float floor = p.relu ? 0.f : -INFINITY;
         int a = 0;
         uint32_t aphase = 0;
         for (int u = first; u < tiles && ok; u += stride) {
             int n0, t0;
             pair_tile(p, u, &n0, &t0);
-            const int n = n0 + 128 * rank + 32 * warp + lane;
+            const int q = warp & 3, j0 = warp < 4 ? 0 : kPairTile / 2;  // a quarter of tensor memory, a half of the tokens
+            const int n = n0 + 128 * rank + 32 * q + lane;
             const bool mine = n < p.n;
             const float ws = mine ? p.w_scale[n] : 0.f, bias = mine && p.bias ? p.bias[n] : 0.f;
+            const int have = min(kPairTile, p.tokens - t0), j1 = min(have, j0 + kPairTile / 2);
             ok = mbar_wait(bar(bars.acc_full[a]), aphase, abort_flag, &g_status, 16);
             fence_after();
-            const int have = min(kPairTile, p.tokens - t0);
-            for (int j = 0; j < have; j += 32) {
+            T *y = static_cast<T *>(p.y) + (long long)(t0 + j0) * p.ld_y + n;
+            for (int j = j0; j < j1; j += 32) {
                 int acc[32];
-                tmem_ld32(tmem + 256 * a + ((uint32_t)(warp * 32) << 16) + j, acc);
+                tmem_ld32(tmem + 256 * a + ((uint32_t)(q * 32) << 16) + j, acc);
                 __syncwarp();
-                reinterpret_cast<float *>(s_scale[warp])[lane] = t0 + j + lane < p.tokens ? __ldg(p.x_scale + t0 + j + lane) : 0.f;
+                reinterpret_cast<float *>(s_scale[warp])[lane] = j + lane < have ? __ldg(p.x_scale + t0 + j + lane) : 0.f;
                 __syncwarp();
                 tmem_wait_ld();
-                if (mine) {
+                const int rows = mine ? j1 - j : 0;
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float4 xs = s_scale[warp][i / 4];
-                        const float sc[4] = {xs.x, xs.y, xs.z, xs.w};
+                for (int i = 0; i < 32; i += 4) {
+                    const float4 xs = s_scale[warp][i / 4];
+                    const float sc[4] = {xs.x, xs.y, xs.z, xs.w};
 #pragma unroll
-                        for (int l = 0; l < 4; ++l) {
-                            float v = fmaf((float)acc[i + l], sc[l] * ws, bias);
-                            if (p.relu && v < 0.f) v = 0.f;
-                            if (j + i + l < have) store_y(p, t0 + j + i + l, n, v);
-                        }
+                    for (int l = 0; l < 4; ++l) {
+                        if (i + l < rows) *y = from_float<T>(at_least(fmaf((float)acc[i + l], sc[l] * ws, bias), floor));
+                        y += p.ld_y;
                     }
                 }
             }
@@ -468,7 +490,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     fence_before();
     __syncthreads();
     cg::this_cluster().sync();  // no barrier of a CTA is signalled once it has gone
-    if (warp == 5)
+    if (warp == kPairOut + 1)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
@@ -489,8 +511,11 @@ accerl_status launch_pair(const CUtensorMap &mw, const CUtensorMap &mx, const Li
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = after_quant ? 2 : 1;
-    ACCERL_CUDA_TRY(allow_smem((const void *)linear_pair_kernel, smem));
-    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_pair_kernel, mw, mx, p));
+    const auto kernel = p.y_dtype == ACCERL_F32    ? linear_pair_kernel<float>
+                        : p.y_dtype == ACCERL_BF16 ? linear_pair_kernel<__nv_bfloat16>
+                                                   : linear_pair_kernel<__half>;
+    ACCERL_CUDA_TRY(allow_smem((const void *)kernel, smem));
+    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, mw, mx, p));
     return ACCERL_OK;
 }
 
@@ -530,7 +555,10 @@ extern "C" accerl_status accerl_quant_rows(const void *x, int64_t ld_x, int32_t 
         return ACCERL_ERR_INVALID_ARG;
     }
     const QuantArgs p{x, q, scale, ld_x, ld_q, rows, cols};
-    ACCERL_CUDA_TRY(with_dtype(dtype, [&](auto v) { return launch_quant<decltype(v)>(p, (cudaStream_t)cuda_stream); }));
+    int device = 0, sm_count = 0;
+    ACCERL_CUDA_TRY(cudaGetDevice(&device));
+    ACCERL_CUDA_TRY(cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device));
+    ACCERL_CUDA_TRY(launch_quant(p, dtype, sm_count, (cudaStream_t)cuda_stream));
     return ACCERL_OK;
 }
 
@@ -597,7 +625,7 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
     if (s != ACCERL_OK) return s;
     if (!given) {
         const QuantArgs q{a->x, static_cast<int8_t *>(a->workspace), const_cast<float *>(xs), a->ld_x, ld_xq, a->tokens, a->k};
-        ACCERL_CUDA_TRY(with_dtype(a->x_dtype, [&](auto v) { return launch_quant<decltype(v)>(q, st); }));
+        ACCERL_CUDA_TRY(launch_quant(q, a->x_dtype, sm_count, st));
     }
     LinearArgs p{xs, a->w_scale, a->bias, a->y, a->ld_y, a->tokens, a->n, a->k, a->y_dtype, a->relu != 0, (a->k + 127) / 128, 0};
     if (pair) return launch_pair(mw, mx, p, sm_count, !given, st);
