@@ -17,18 +17,17 @@ namespace accerl {
 
 namespace {
 
-constexpr int kThreads = 256, kAhead = 4, kUnit = kThreads * kAhead;  // pieces of a unit of work
+constexpr int kThreads = 256, kAhead = 4, kUnit = 32 * kAhead;  // pieces of a unit of work, a warp's
 
 struct CkptArgs {
     const void *in;  // x (save) or dy (backward)
     void *out;       // y, x^ or dx; null: none
     int8_t *q;
     uint8_t *e;
-    long long ld_in, ld_out, ld_q, ld_e, rows, units;
-    int cols, pieces;    // pieces of a row, the last block's padding among them
-    int rows_per_unit;   // short rows: so many a unit; long ones: 1, and `segments` units a row
-    int segments;
-    unsigned magic;      // l / pieces = l * magic >> 20 for l < kUnit
+    long long ld_in, ld_out, ld_q, ld_e, rows, cols;
+    long long pieces;  // of a row, the last block's padding among them
+    long long units;
+    unsigned segments;  // units of a row
 };
 
 enum { kSave, kLoad, kBackward };
@@ -94,92 +93,97 @@ __device__ __forceinline__ float byte_value(uint32_t flipped, int k)
     return __uint_as_float(__byte_perm(flipped, 0x4b000000u, 0x7440u | (unsigned)k)) - 8388736.f;  // 2^23 + 128
 }
 
-// ALIGNED: the rows of both arrays start at multiples of 16 bytes
+// A warp takes 128 neighbouring pieces of a row at a time, so that everything but a lane's offset is the warp's.
+// ALIGNED: the rows of both arrays start at multiples of 16 bytes.
 template <typename T, int MODE, int ACT, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads) ckpt_kernel(const __grid_constant__ CkptArgs p)
+__global__ void __launch_bounds__(kThreads, 5) ckpt_kernel(const __grid_constant__ CkptArgs p)
 {
     constexpr int V = Row<T>::kVec, kWords = V / 4, kLanes = 32 / V;  // lanes of a block
-    for (long long unit = blockIdx.x; unit < p.units; unit += gridDim.x) {
-        const long long row0 = p.segments == 1 ? unit * p.rows_per_unit : unit / p.segments;
-        const int piece0 = p.segments == 1 ? 0 : (int)(unit - row0 * p.segments) * kUnit;
-        long long row[kAhead];
-        int at[kAhead];
-        bool live[kAhead];
-        uint4 raw[kAhead];
-        uint32_t code[kAhead][kWords];
-        uint32_t scale[kAhead];
+    const int lane = threadIdx.x & 31;
+    const long long unit = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    if (unit >= p.units) return;
+    const long long row = p.rows == 1 ? 0 : (long long)((unsigned)unit / p.segments);  // (several rows: fewer than 2^32 units)
+    const long long begin = (unit - row * p.segments) * (kUnit * V);              // first element of the unit in its row
+    const T *in = static_cast<const T *>(p.in) + row * p.ld_in + begin;
+    T *out = static_cast<T *>(p.out) + row * p.ld_out + begin;
+    int8_t *q = p.q + row * p.ld_q + begin;
+    uint8_t *e = p.e + row * p.ld_e + begin / 32;
+    // elements of the unit that exist, and with the last block's padding
+    const int n = (int)min((long long)kUnit * V, p.cols - begin), n32 = (int)min((long long)kUnit * V, p.pieces * V - begin);
+    const bool full = n == kUnit * V;
+
+    uint4 raw[MODE != kLoad ? kAhead : 1];
+    uint32_t code[MODE != kSave ? kAhead : 1][kWords];
+    int kept = 0;
+    if constexpr (MODE != kSave) kept = lane < n32 / 32 ? e[lane] : 0;  // a unit has at most 32 blocks
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int l = i * kThreads + (int)threadIdx.x;
-            const int r = p.segments == 1 ? (int)((unsigned)l * p.magic >> 20) : 0;
-            const int piece = p.segments == 1 ? l - r * p.pieces : piece0 + l;
-            row[i] = row0 + r;
-            live[i] = r < p.rows_per_unit && row[i] < p.rows && piece < p.pieces;
-            at[i] = piece * V;
-            if constexpr (MODE != kLoad) {
-                const T *in = static_cast<const T *>(p.in) + row[i] * p.ld_in;
-                raw[i] = live[i] ? load_piece<T, ALIGNED>(in, at[i], p.cols, 0.f) : make_uint4(0, 0, 0, 0);
-            }
-            if constexpr (MODE != kSave) {
+    for (int i = 0; i < kAhead; ++i) {
+        const int at = (i * 32 + lane) * V;
+        if constexpr (MODE != kLoad) {
+            if (full) raw[i] = ALIGNED ? __ldcs(reinterpret_cast<const uint4 *>(in + at)) : load16(in + at);
+            else raw[i] = load_piece<T, ALIGNED>(in, at, n, 0.f);
+        }
+        if constexpr (MODE != kSave) {
 #pragma unroll
-                for (int j = 0; j < kWords; ++j) code[i][j] = 0;
-                scale[i] = 0;
-                if (live[i]) {
-                    const int8_t *q = p.q + row[i] * p.ld_q + at[i];
-                    if constexpr (kWords == 2) {
-                        const uint2 c = __ldcs(reinterpret_cast<const uint2 *>(q));
-                        code[i][0] = c.x;
-                        code[i][1] = c.y;
-                    } else {
-                        code[i][0] = __ldcs(reinterpret_cast<const unsigned *>(q));
-                    }
-                    scale[i] = p.e[row[i] * p.ld_e + at[i] / 32];
+            for (int j = 0; j < kWords; ++j) code[i][j] = 0;
+            if (at < n32) {
+                if constexpr (kWords == 2) {
+                    const uint2 c = __ldcs(reinterpret_cast<const uint2 *>(q + at));
+                    code[i][0] = c.x;
+                    code[i][1] = c.y;
+                } else {
+                    code[i][0] = __ldcs(reinterpret_cast<const unsigned *>(q + at));
                 }
             }
         }
+    }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            float v[V];
-            if constexpr (MODE == kSave) {
-                unpack<T>(raw[i], v);
-                uint32_t top = 0;
+    for (int i = 0; i < kAhead; ++i) {
+        const int at = (i * 32 + lane) * V;
+        float v[V];
+        if constexpr (MODE == kSave) {
+            unpack<T>(raw[i], v);
+            uint32_t top = 0;
 #pragma unroll
-                for (int k = 0; k < V; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
+            for (int k = 0; k < V; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
 #pragma unroll
-                for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const bool broken = top >= 0x7f800000u;  // an infinity or a NaN
-                const int e = broken ? 255 : max((int)((top + 0x10000u) >> 23) - 6, 1);
-                const float inv = __uint_as_float((uint32_t)(254 - min(e, 253)) << 23);  // (e <= 249 for finite values)
-                uint32_t w[kWords];
+            for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const bool broken = top >= 0x7f800000u;  // an infinity or a NaN
+            const int ev = broken ? 255 : max((int)((top + 0x10000u) >> 23) - 6, 1);
+            const float inv = __uint_as_float((uint32_t)(254 - min(ev, 253)) << 23);  // (ev <= 249 for finite values)
+            uint32_t w[kWords];
 #pragma unroll
-                for (int j = 0; j < kWords; ++j) {
-                    uint32_t b[4];
+            for (int j = 0; j < kWords; ++j) {
+                uint32_t b[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(fmaf(v[4 * j + k], inv, 12582912.f));
-                    w[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-                    if (broken) w[j] = 0;
-                }
-                if (live[i]) {
-                    int8_t *q = p.q + row[i] * p.ld_q + at[i];
-                    if constexpr (kWords == 2) *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
-                    else *reinterpret_cast<uint32_t *>(q) = w[0];
-                    if (at[i] % 32 == 0) p.e[row[i] * p.ld_e + at[i] / 32] = (uint8_t)e;
-                }
-#pragma unroll
-                for (int k = 0; k < V; ++k) v[k] = activation<ACT>(v[k]);
-            } else {
-                float dy[V];
-                if constexpr (MODE == kBackward) unpack<T>(raw[i], dy);
-                const float s = __uint_as_float(scale[i] << 23);  // (255: infinity times the block's zeros, NaN)
-#pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const float x = byte_value(code[i][k / 4] ^ 0x80808080u, k & 3) * s;
-                    v[k] = MODE == kBackward ? dy[k] * slope<ACT>(x) : x;
-                }
+                for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(fmaf(v[4 * j + k], inv, 12582912.f));
+                w[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+                if (broken) w[j] = 0;
             }
-            if (live[i] && p.out) {
-                T *out = static_cast<T *>(p.out) + row[i] * p.ld_out;
-                store_piece<T, ALIGNED>(out, at[i], p.cols, v);
+            if (at < n32) {
+                if constexpr (kWords == 2) *reinterpret_cast<uint2 *>(q + at) = make_uint2(w[0], w[1]);
+                else *reinterpret_cast<uint32_t *>(q + at) = w[0];
+                if (lane % kLanes == 0) e[i * V + lane / kLanes] = (uint8_t)ev;
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = activation<ACT>(v[k]);
+        } else {
+            float dy[V];
+            if constexpr (MODE == kBackward) unpack<T>(raw[i], dy);
+            // (255: infinity times the block's zeros, NaN)
+            const float s = __uint_as_float((uint32_t)__shfl_sync(0xffffffffu, kept, i * V + lane / kLanes) << 23);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float x = byte_value(code[i][k / 4] ^ 0x80808080u, k & 3) * s;
+                v[k] = MODE == kBackward ? dy[k] * slope<ACT>(x) : x;
+            }
+        }
+        if (MODE != kSave || p.out) {
+            if (full) {
+                if (ALIGNED) *reinterpret_cast<uint4 *>(out + at) = pack<T>(v);
+                else store16(out + at, pack<T>(v));
+            } else {
+                store_piece<T, ALIGNED>(out, at, n, v);
             }
         }
     }
@@ -199,20 +203,20 @@ auto kernel_of(int act)
 template <int MODE>
 accerl_status launch(CkptArgs &p, int dtype, int act, void *cuda_stream)
 {
-    const int cols32 = (p.cols + 31) / 32 * 32;
-    p.pieces = cols32 * dtype_size(dtype) / 16;
-    if (p.pieces <= kUnit) {
-        p.rows_per_unit = kUnit / p.pieces;
-        p.segments = 1;
-        p.magic = ((1u << 20) + p.pieces - 1) / p.pieces;
-        p.units = (p.rows + p.rows_per_unit - 1) / p.rows_per_unit;
-    } else {
-        p.rows_per_unit = 1;
-        p.segments = (p.pieces + kUnit - 1) / kUnit;
-        p.magic = 0;
-        p.units = p.rows * p.segments;
+    const bool dense = p.cols % 32 == 0 && (MODE == kLoad || p.ld_in == p.cols) && (!p.out || p.ld_out == p.cols) && p.ld_q == p.cols &&
+                       p.ld_e == p.cols / 32;
+    if (dense) {  // rows without gaps are one row
+        p.cols *= p.rows;
+        p.rows = 1;
     }
-    const unsigned blocks = (unsigned)(p.units < (1LL << 30) ? p.units : (1LL << 30));
+    p.pieces = (p.cols + 31) / 32 * 32 * dtype_size(dtype) / 16;
+    p.segments = (unsigned)((p.pieces + kUnit - 1) / kUnit);
+    p.units = p.rows * ((p.pieces + kUnit - 1) / kUnit);
+    if (p.units > (p.rows == 1 ? 1LL << 33 : (1LL << 32) - 1)) {
+        set_error("checkpoint: too many values");
+        return ACCERL_ERR_INVALID_ARG;
+    }
+    const unsigned blocks = (unsigned)((p.units + kThreads / 32 - 1) / (kThreads / 32));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const bool aligned = (MODE == kLoad || rows_aligned(p.in, p.ld_in, dtype)) && (!p.out || rows_aligned(p.out, p.ld_out, dtype));
     ACCERL_CUDA_TRY(with_dtype(dtype, [&](auto v) {
@@ -271,7 +275,7 @@ extern "C" accerl_status accerl_ckpt_save(const void *x, int64_t ld_x, int32_t d
     if (!good_sizes(who, rows, cols, dtype, act) || !good_rows(who, "x", x, ld_x, cols, dtype) ||
         (y && !good_rows(who, "y", y, ld_y, cols, dtype)) || !good_ckpt(who, q, ld_q, e, ld_e, cols))
         return ACCERL_ERR_INVALID_ARG;
-    CkptArgs p{x, y, q, e, ld_x, ld_y, ld_q, ld_e, rows, 0, cols, 0, 0, 0, 0};
+    CkptArgs p{x, y, q, e, ld_x, ld_y, ld_q, ld_e, rows, cols, 0, 0, 0};
     return launch<kSave>(p, dtype, act, cuda_stream);
 }
 
@@ -282,7 +286,7 @@ extern "C" accerl_status accerl_ckpt_load(const int8_t *q, int64_t ld_q, const u
     if (!good_sizes(who, rows, cols, dtype, ACCERL_ACT_NONE) || !good_rows(who, "x", x, ld_x, cols, dtype) ||
         !good_ckpt(who, q, ld_q, e, ld_e, cols))
         return ACCERL_ERR_INVALID_ARG;
-    CkptArgs p{nullptr, x, const_cast<int8_t *>(q), const_cast<uint8_t *>(e), 0, ld_x, ld_q, ld_e, rows, 0, cols, 0, 0, 0, 0};
+    CkptArgs p{nullptr, x, const_cast<int8_t *>(q), const_cast<uint8_t *>(e), 0, ld_x, ld_q, ld_e, rows, cols, 0, 0, 0};
     return launch<kLoad>(p, dtype, ACCERL_ACT_NONE, cuda_stream);
 }
 
@@ -294,6 +298,6 @@ extern "C" accerl_status accerl_ckpt_act_backward(const void *dy, int64_t ld_dy,
     if (!good_sizes(who, rows, cols, dtype, act) || !good_rows(who, "dy", dy, ld_dy, cols, dtype) ||
         !good_rows(who, "dx", dx, ld_dx, cols, dtype) || !good_ckpt(who, q, ld_q, e, ld_e, cols))
         return ACCERL_ERR_INVALID_ARG;
-    CkptArgs p{dy, dx, const_cast<int8_t *>(q), const_cast<uint8_t *>(e), ld_dy, ld_dx, ld_q, ld_e, rows, 0, cols, 0, 0, 0, 0};
+    CkptArgs p{dy, dx, const_cast<int8_t *>(q), const_cast<uint8_t *>(e), ld_dy, ld_dx, ld_q, ld_e, rows, cols, 0, 0, 0};
     return launch<kBackward>(p, dtype, act, cuda_stream);
 }
