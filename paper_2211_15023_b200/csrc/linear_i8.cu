@@ -174,7 +174,7 @@ __device__ __forceinline__ float at_least(float v, float floor)  // (a NaN stays
     return m;
 }
 
-constexpr int kFewThreads = 192, kMaxStages = 8;
+constexpr int kFewThreads = 192, kMaxStages = 8, kMaxShare = 8;
 
 // One tile of 128 channels x NT tokens; the CTAs of a cluster share its K.
 // Warps 0..3 drain the accumulator (and finish), warp 4 loads, warp 5 issues the tensor-core instructions.
@@ -291,13 +291,28 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     }
     if (share > 1) {
         cg::this_cluster().sync();
-        if (threadIdx.x < 128) {
-            const int have = min(NT, p.tokens - t0);
-            for (int t = rank; t < have; t += share) {
-                int acc = 0;
-                for (int r = 0; r < share; ++r) acc += *cg::this_cluster().map_shared_rank(&part[t * 128 + threadIdx.x], r);
-                finish(t0 + t, acc);
-            }
+        const int4 *four = reinterpret_cast<const int4 *>(part);
+        // four channels of a token a thread, the parts' loads all in flight (each answers in about a microsecond)
+        for (int i = rank * kFewThreads + (int)threadIdx.x; i < min(NT, p.tokens - t0) * 32; i += share * kFewThreads) {
+            int4 x[kMaxShare];
+#pragma unroll
+            for (int c = 0; c < kMaxShare; ++c)
+                if (c < share) x[c] = *cg::this_cluster().map_shared_rank(&four[i], c);
+            int acc[4] = {};
+#pragma unroll
+            for (int c = 0; c < kMaxShare; ++c)
+                if (c < share) {
+                    acc[0] += x[c].x;
+                    acc[1] += x[c].y;
+                    acc[2] += x[c].z;
+                    acc[3] += x[c].w;
+                }
+            const int t = t0 + i / 32, n4 = n0 + i % 32 * 4;
+            const float xs = p.x_scale[t], floor = p.relu ? 0.f : -INFINITY;
+#pragma unroll
+            for (int l = 0; l < 4; ++l)
+                if (n4 + l < p.n)
+                    store_y(p, t, n4 + l, at_least(fmaf((float)acc[l], xs * p.w_scale[n4 + l], p.bias ? p.bias[n4 + l] : 0.f), floor));
         }
         cg::this_cluster().sync();
     }
@@ -316,7 +331,7 @@ accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArg
     const size_t smem = 1024 + (size_t)p.stages * kStage;
     const int tiles = (p.n + 127) / 128, token_tiles = (p.tokens + NT - 1) / NT;
     int share = 1;
-    while (share < 8 && (long long)tiles * token_tiles * share < sm_count && p.chunks >= 4 * share) share *= 2;
+    while (share < kMaxShare && (long long)tiles * token_tiles * share < sm_count && p.chunks >= 4 * share) share *= 2;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;

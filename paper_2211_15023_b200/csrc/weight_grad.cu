@@ -27,6 +27,8 @@ __device__ int g_status;  // of this file's bounded waits
 constexpr int kTileK = 128, kTokens = 64;        // values of k a tile, tokens a stage
 constexpr int kRaw = 4, kDec = 3, kDy = 4;       // stages of the three rings
 constexpr int kRawBytes = kTokens * kTileK, kDecBytes = 2 * kRawBytes;
+constexpr int kAhead = 6;                        // stages whose exponents are on their way
+constexpr int kMaxShare = 8;                     // CTAs of a cluster
 constexpr int kConvWarps = 8, kThreads = 32 * (4 + kConvWarps + 4);
 
 struct GradArgs {
@@ -243,10 +245,14 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const uint8_t *e_col = p.e + col / 32;
             const bool in = kt < p.k_tiles && col < p.cols32;
             auto exponent = [&](int g) { return in && g < g1 && g * kTokens + t < p.tokens ? (int)__ldg(e_col + (long long)(g * kTokens + t) * p.ld_e) : 127; };
-            int e_next = exponent(g0);
+            int ahead[kAhead];  // a load takes as long as some stages
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) ahead[i] = exponent(g0 + i);
             for (int g = g0; g < g1 && ok; ++g) {
-                const int e = e_next;
-                e_next = exponent(g + 1);
+                const int e = ahead[0];
+#pragma unroll
+                for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+                ahead[kAhead - 1] = exponent(g + kAhead);
                 uint32_t q[8] = {};
                 if (kt < p.k_tiles) {
                     ok = mbar_wait(bar(bars.raw_full[r.slot]), r.phase, abort_flag, &g_status, 16);
@@ -318,23 +324,38 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             a.next();
         }
     }
-    if (share > 1) {  // one tile a cluster
+    if (share > 1) {  // one tile a cluster: every CTA adds up its share of the columns, four values a thread and a part's
+                      // loads all in flight (distributed shared memory answers in about a microsecond)
         cg::this_cluster().sync();
-        if (warp >= 4 + kConvWarps && first < p.tiles) {
+        if (first < p.tiles) {
             const int kt = first / p.n_tiles, n0 = (first - kt * p.n_tiles) * p.n_tile;
-            const int kl = (int)threadIdx.x - 32 * (4 + kConvWarps);
             const bool sums = kt == p.k_tiles;
-            const int k = kt * kTileK + kl, n_end = min(p.n_tile, p.n - n0);
-            float *part = reinterpret_cast<float *>(smem);
-            if (sums ? kl == 0 : k < p.k)
-                for (int j = rank; j < n_end; j += share) {
-                    float v = 0.f;
-                    for (int i = 0; i < share; ++i) v += *cg::this_cluster().map_shared_rank(&part[j * 128 + kl], i);
-                    void *base = sums ? p.db : p.dw;
-                    const long long at = sums ? n0 + j : (long long)(n0 + j) * p.ld_dw + k;
-                    if (p.accumulate) v += load_out(p, base, at);
-                    store_out(p, base, at, v);
-                }
+            const int n_end = min(p.n_tile, p.n - n0), k_end = sums ? 1 : min(kTileK, p.k - kt * kTileK);
+            void *base = sums ? p.db : p.dw;
+            float4 *part = reinterpret_cast<float4 *>(smem);
+            for (int i = rank * kThreads + (int)threadIdx.x; i < n_end * (kTileK / 4); i += share * kThreads) {
+                const int j = i / (kTileK / 4), kl = i % (kTileK / 4) * 4;
+                if (kl >= k_end) continue;
+                float4 x[kMaxShare];
+#pragma unroll
+                for (int c = 0; c < kMaxShare; ++c)
+                    if (c < share) x[c] = *cg::this_cluster().map_shared_rank(&part[i], c);
+                float v[4] = {};
+#pragma unroll
+                for (int c = 0; c < kMaxShare; ++c)
+                    if (c < share) {
+                        v[0] += x[c].x;
+                        v[1] += x[c].y;
+                        v[2] += x[c].z;
+                        v[3] += x[c].w;
+                    }
+#pragma unroll
+                for (int l = 0; l < 4; ++l)
+                    if (kl + l < k_end) {
+                        const long long at = sums ? n0 + j : (long long)(n0 + j) * p.ld_dw + kt * kTileK + kl + l;
+                        store_out(p, base, at, p.accumulate ? v[l] + load_out(p, base, at) : v[l]);
+                    }
+            }
         }
         cg::this_cluster().sync();
     }
@@ -442,6 +463,7 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     p.out_dtype = a->out_dtype;
     p.accumulate = a->accumulate != 0;
     p.n_tile = std::min(256, (a->n + 63) / 64 * 64);
+    if (p.n_tile == 256 && ((long long)a->n + 255) / 256 * ((a->k + kTileK - 1) / kTileK) * 4 <= sm_count) p.n_tile = 128;
     p.n_tiles = (a->n + p.n_tile - 1) / p.n_tile;
     p.k_tiles = (a->k + kTileK - 1) / kTileK;
     p.cols32 = cols32;
@@ -453,7 +475,7 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     p.tiles = (int)tiles;
     const int stages = (a->tokens + kTokens - 1) / kTokens;
     int share = 1;
-    while (share < 8 && 2LL * share * p.tiles <= sm_count && stages >= 4 * share) share *= 2;
+    share = std::max(1, std::min({kMaxShare, sm_count / p.tiles, stages / 2}));
     const unsigned grid = share > 1 ? (unsigned)(p.tiles * share) : (unsigned)std::min(p.tiles, sm_count);
     const size_t smem = 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens;
     const auto kernel = a->dy_dtype == ACCERL_F16 ? weight_grad_kernel<__half> : weight_grad_kernel<__nv_bfloat16>;
