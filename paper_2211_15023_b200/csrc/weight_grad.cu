@@ -98,6 +98,35 @@ struct Decode<__half> {
     static constexpr uint32_t kOnes = 0x3c003c00u;
 };
 
+// A thread's share of a stage: 32 values of one token (block b of the row, t the token of the stage) from the TMA's
+// swizzled codes to the operand's rows of 64 values, swizzled alike.  Lanes are tokens: no two of eight meet in a bank.
+template <typename T>
+__device__ __forceinline__ void load_codes(uint32_t raw, int b, int t, uint32_t (&q)[8])
+{
+    const uint32_t row = raw + t * 128;
+    const uint4 lo = lds16(row + (((2 * b) ^ (t & 7)) << 4)), hi = lds16(row + (((2 * b + 1) ^ (t & 7)) << 4));
+    q[0] = lo.x, q[1] = lo.y, q[2] = lo.z, q[3] = lo.w, q[4] = hi.x, q[5] = hi.y, q[6] = hi.z, q[7] = hi.w;
+}
+template <typename T>
+__device__ __forceinline__ void put_values(uint32_t dec, int b, int t, const uint32_t (&q)[8], int e, bool ones)
+{
+    const uint32_t out = dec + (b >> 1) * (kTokens * 128) + t * 128;
+    const Decode<T> d(e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint4 v;
+        if (!ones) {
+            v.x = d.pair(q[2 * i], 0x4140);
+            v.y = d.pair(q[2 * i], 0x4342);
+            v.z = d.pair(q[2 * i + 1], 0x4140);
+            v.w = d.pair(q[2 * i + 1], 0x4342);
+        } else {
+            v.x = v.y = v.z = v.w = Decode<T>::kOnes;
+        }
+        sts16(out + ((((b & 1) * 4 + i) ^ (t & 7)) << 4), v);
+    }
+}
+
 struct __align__(8) GradBars {
     uint64_t raw_full[kRaw], raw_empty[kRaw], dec_full[kDec], dec_empty[kDec], dy_full[kDy], dy_empty[kDy], acc_full[2], acc_empty[2];
     uint32_t tmem;
@@ -179,22 +208,28 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     bool ok = true;
 
     if (warp == 0) {
-        // ------------------------------------------------------------------------------------- loads
+        // ------------------------------------------------------------------------------ loads of codes
+        // (apart from those of dy, which would hold them up: a stage of dy is free only when the tensor cores are done with it)
         Ring<kRaw> r;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int kt = u / p.n_tiles;
+            for (int g = g0; g < g1 && ok && kt < p.k_tiles; ++g) {
+                ok = mbar_wait(bar(bars.raw_empty[r.slot]), r.phase ^ 1, abort_flag, &g_status, 1);
+                if (ok && elect_one()) {
+                    mbar_expect_tx(bar(bars.raw_full[r.slot]), kRawBytes);
+                    tma_load_2d(raw0 + r.slot * kRawBytes, &map_q, kt * kTileK, g * kTokens, bar(bars.raw_full[r.slot]));
+                }
+                __syncwarp();
+                r.next();
+            }
+        }
+    } else if (warp == 2) {
+        // --------------------------------------------------------------------------------- loads of dy
         Ring<kDy> d;
         for (int u = first; u < p.tiles && ok; u += stride) {
-            const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * p.n_tile;
+            const int n0 = u % p.n_tiles * p.n_tile;
             for (int g = g0; g < g1 && ok; ++g) {
-                if (kt < p.k_tiles) {
-                    ok = mbar_wait(bar(bars.raw_empty[r.slot]), r.phase ^ 1, abort_flag, &g_status, 1);
-                    if (ok && elect_one()) {
-                        mbar_expect_tx(bar(bars.raw_full[r.slot]), kRawBytes);
-                        tma_load_2d(raw0 + r.slot * kRawBytes, &map_q, kt * kTileK, g * kTokens, bar(bars.raw_full[r.slot]));
-                    }
-                    __syncwarp();
-                    r.next();
-                }
-                if (ok) ok = mbar_wait(bar(bars.dy_empty[d.slot]), d.phase ^ 1, abort_flag, &g_status, 2);
+                ok = mbar_wait(bar(bars.dy_empty[d.slot]), d.phase ^ 1, abort_flag, &g_status, 2);
                 if (ok && elect_one()) {
                     mbar_expect_tx(bar(bars.dy_full[d.slot]), (uint32_t)dy_bytes);
                     for (int b = 0; b < p.n_tile / 64; ++b)
@@ -248,42 +283,31 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             int ahead[kAhead];  // a load takes as long as some stages
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) ahead[i] = exponent(g0 + i);
-            for (int g = g0; g < g1 && ok; ++g) {
-                const int e = ahead[0];
+            for (int g = g0; g < g1 && ok;) {
 #pragma unroll
-                for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
-                ahead[kAhead - 1] = exponent(g + kAhead);
-                uint32_t q[8] = {};
-                if (kt < p.k_tiles) {
-                    ok = mbar_wait(bar(bars.raw_full[r.slot]), r.phase, abort_flag, &g_status, 16);
-                    const uint32_t row = raw0 + r.slot * kRawBytes + t * 128;
-                    const uint4 lo = lds16(row + (((2 * b) ^ (t & 7)) << 4)), hi = lds16(row + (((2 * b + 1) ^ (t & 7)) << 4));
-                    q[0] = lo.x, q[1] = lo.y, q[2] = lo.z, q[3] = lo.w, q[4] = hi.x, q[5] = hi.y, q[6] = hi.z, q[7] = hi.w;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(bars.raw_empty[r.slot]));
-                    r.next();
-                }
-                if (ok) ok = mbar_wait(bar(bars.dec_empty[c.slot]), c.phase ^ 1, abort_flag, &g_status, 32);
-                ok = __all_sync(0xffffffffu, ok);
-                const uint32_t out = dec0 + c.slot * kDecBytes + (b >> 1) * (kTokens * 128) + t * 128;
-                const Decode<T> dec(e);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint4 v;
+                for (int i = 0; i < kAhead; ++i) {  // (unrolled: a value on its way is not to be moved)
+                    if (g >= g1 || !ok) break;
+                    const int e = ahead[i];
+                    ahead[i] = exponent(g + kAhead);
+                    uint32_t q[8] = {};
                     if (kt < p.k_tiles) {
-                        v.x = dec.pair(q[2 * i], 0x4140);
-                        v.y = dec.pair(q[2 * i], 0x4342);
-                        v.z = dec.pair(q[2 * i + 1], 0x4140);
-                        v.w = dec.pair(q[2 * i + 1], 0x4342);
-                    } else {
-                        v.x = v.y = v.z = v.w = Decode<T>::kOnes;
+                        ok = mbar_wait(bar(bars.raw_full[r.slot]), r.phase, abort_flag, &g_status, 16);
+                        load_codes<T>(raw0 + r.slot * kRawBytes, b, t, q);
                     }
-                    sts16(out + ((((b & 1) * 4 + i) ^ (t & 7)) << 4), v);
+                    if (ok) ok = mbar_wait(bar(bars.dec_empty[c.slot]), c.phase ^ 1, abort_flag, &g_status, 32);
+                    ok = __all_sync(0xffffffffu, ok);
+                    put_values<T>(dec0 + c.slot * kDecBytes, b, t, q, e, kt == p.k_tiles);
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar(bars.dec_full[c.slot]));
+                        // (only now: the codes have arrived in registers, not merely been asked for)
+                        if (kt < p.k_tiles) mbar_arrive(bar(bars.raw_empty[r.slot]));
+                    }
+                    if (kt < p.k_tiles) r.next();
+                    c.next();
+                    ++g;
                 }
-                fence_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(bars.dec_full[c.slot]));
-                c.next();
             }
         }
     } else if (warp >= 4 + kConvWarps) {
@@ -365,6 +389,264 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     __syncthreads();
     if (warp == 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// Many tiles: pairs of CTAs on tiles of 256 values of k x 256 channels.  A CTA decodes its 128 values of k and loads 128
+// channels of dy; an instruction of the pair takes both CTAs' halves of dy, so that a CTA moves 40 KB a stage through its
+// shared memory instead of 56, and 24 KB instead of 40 from L2.  Decoding is a chain of some 700 cycles a stage (wait,
+// load, about 100 instructions, store, fence): two groups of eight warps take stages in turn.
+//
+// fp32 results: the tensor cores cut a sum off at every addition, which over 8192 tokens costs 4.5e-6 of the result's
+// norm (4e-7 with an fp32 product's rounding).  So the accumulator covers at most kChunk stages, and the parts
+// are added in fp32 to the result in memory, without waiting for it (one thread adds to a value, part by part: the order
+// is fixed): 5e-7.
+constexpr int kPairTile = 256, kChunk = 24;
+constexpr int kPairRaw = 4, kPairDec = 5, kPairDy = 5, kPairDyBytes = 2 * 128 * kTokens, kGroups = 2;
+constexpr int kPairThreads = 32 * (4 + kGroups * kConvWarps + 4);
+constexpr size_t kPairSmem = 1024 + kPairRaw * kRawBytes + kPairDec * kDecBytes + kPairDy * kPairDyBytes;
+
+struct __align__(8) PairBars {
+    uint64_t raw_full[kPairRaw], raw_empty[kPairRaw], dec_full[kPairDec], dec_empty[kPairDec], dy_full[kPairDy], dy_empty[kPairDy],
+        acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int abort_flag;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kPairThreads, 1)
+weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_dy,
+                        const __grid_constant__ GradArgs p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ PairBars bars;
+    namespace cg = cooperative_groups;
+    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t raw0 = smem_u32(smem), dec0 = raw0 + kPairRaw * kRawBytes, dy0 = dec0 + kPairDec * kDecBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cg::this_cluster().block_rank();
+    const int stages = (p.tokens + kTokens - 1) / kTokens;
+    const int chunks = p.out_dtype == ACCERL_F32 ? (stages + kChunk - 1) / kChunk : 1;
+    const int first = (int)blockIdx.x >> 1, stride = (int)gridDim.x >> 1;
+    volatile int *abort_flag = &bars.abort_flag;
+    auto bar = [](uint64_t &b) { return smem_u32(&b); };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPairRaw; ++i) {
+            mbar_init(bar(bars.raw_full[i]), 1);
+            mbar_init(bar(bars.raw_empty[i]), kConvWarps);
+        }
+        for (int i = 0; i < kPairDec; ++i) {
+            mbar_init(bar(bars.dec_full[i]), kConvWarps + (rank == 0 ? 1 : 0));  // the first CTA's: its warps, and the other's relay
+            mbar_init(bar(bars.dec_empty[i]), 1);
+        }
+        for (int i = 0; i < kPairDy; ++i) {
+            mbar_init(bar(bars.dy_full[i]), 1);  // the first CTA's: the loads of both
+            mbar_init(bar(bars.dy_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(bars.acc_full[i]), 1);
+            mbar_init(bar(bars.acc_empty[i]), 4 + (rank == 0 ? 1 : 0));  // the same
+        }
+        bars.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    cg::this_cluster().sync();
+    fence_after();
+    const uint32_t tmem = bars.tmem;
+    bool ok = true;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------------------ loads of codes
+        Ring<kPairRaw> r;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int kt = u / p.n_tiles;
+            for (int g = 0; g < stages && ok && kt < p.k_tiles; ++g) {
+                ok = mbar_wait(bar(bars.raw_empty[r.slot]), r.phase ^ 1, abort_flag, &g_status, 1);
+                if (ok && elect_one()) {
+                    mbar_expect_tx(bar(bars.raw_full[r.slot]), kRawBytes);
+                    tma_load_2d(raw0 + r.slot * kRawBytes, &map_q, kt * kPairTile + 128 * rank, g * kTokens, bar(bars.raw_full[r.slot]));
+                }
+                __syncwarp();
+                r.next();
+            }
+        }
+    } else if (warp == 2) {
+        // --------------------------------------------------------------------------------- loads of dy
+        Ring<kPairDy> d;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int n0 = u % p.n_tiles * kPairTile + 128 * rank;
+            for (int g = 0; g < stages && ok; ++g) {
+                ok = mbar_wait(bar(bars.dy_empty[d.slot]), d.phase ^ 1, abort_flag, &g_status, 2);
+                if (ok && elect_one()) {
+                    const uint32_t full = peer_addr(bar(bars.dy_full[d.slot]), 0);
+                    if (rank == 0) mbar_expect_tx(bar(bars.dy_full[d.slot]), 2 * kPairDyBytes);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        tma_load_2d_pair(dy0 + d.slot * kPairDyBytes + b * kTokens * 128, &map_dy, (n0 + 64 * b) * 2, g * kTokens, full);
+                }
+                __syncwarp();
+                d.next();
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ------------------------------------------------------------------------------ tensor core
+        constexpr uint32_t kType = std::is_same<T, __half>::value ? 0u : 1u;
+        constexpr uint32_t idesc = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 15) | (1u << 16) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+        Ring<kPairDec> c;
+        Ring<kPairDy> d;
+        Ring<2> a;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            for (int ch = 0; ch < chunks && ok; ++ch) {
+                const int g0 = (int)((long long)stages * ch / chunks), g1 = (int)((long long)stages * (ch + 1) / chunks);
+                ok = mbar_wait_cluster(bar(bars.acc_empty[a.slot]), a.phase ^ 1, abort_flag, &g_status, 4);
+                fence_after();
+                for (int g = g0; g < g1 && ok; ++g) {
+                    ok = mbar_wait_cluster(bar(bars.dec_full[c.slot]), c.phase, abort_flag, &g_status, 8);
+                    if (ok) ok = mbar_wait(bar(bars.dy_full[d.slot]), d.phase, abort_flag, &g_status, 8);
+                    fence_after();
+                    if (ok && elect_one()) {
+                        const uint64_t ad = mn_desc(dec0 + c.slot * kDecBytes), bd = mn_desc(dy0 + d.slot * kPairDyBytes);
+#pragma unroll
+                        for (int ks = 0; ks < kTokens / 16; ++ks)
+                            mma_f16_pair(tmem + 256 * a.slot, ad + ks * (2048 >> 4), bd + ks * (2048 >> 4), idesc, (uint32_t)((g - g0) | ks));
+                        mma_commit_pair(bar(bars.dec_empty[c.slot]));
+                        mma_commit_pair(bar(bars.dy_empty[d.slot]));
+                        if (g == g1 - 1) mma_commit_pair(bar(bars.acc_full[a.slot]));
+                    }
+                    __syncwarp();
+                    c.next();
+                    d.next();
+                }
+                a.next();
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------- the second CTA's operands, told to the first
+        Ring<kPairDec> c;
+        for (int u = first; u < p.tiles && ok; u += stride)
+            for (int g = 0; g < stages && ok; ++g) {
+                ok = mbar_wait(bar(bars.dec_full[c.slot]), c.phase, abort_flag, &g_status, 128);
+                if (lane == 0) mbar_arrive_cluster(peer_addr(bar(bars.dec_full[c.slot]), 0));
+                __syncwarp();
+                c.next();
+            }
+    } else if (warp == 3 && rank == 1) {
+        // ---------------------------------------------- the second CTA's accumulators, told to the first
+        Ring<2> a;
+        for (int u = first; u < p.tiles && ok; u += stride)
+            for (int ch = 0; ch < chunks && ok; ++ch) {
+                ok = mbar_wait(bar(bars.acc_empty[a.slot]), a.phase, abort_flag, &g_status, 256);
+                if (lane == 0) mbar_arrive_cluster(peer_addr(bar(bars.acc_empty[a.slot]), 0));
+                __syncwarp();
+                a.next();
+            }
+    } else if (warp >= 4 && warp < 4 + kGroups * kConvWarps) {
+        // ------------------------------------------------------------------------------------ decoding
+        const int group = (warp - 4) / kConvWarps, w = (warp - 4) % kConvWarps;
+        const int b = w & 3, t = (w >> 2) * 32 + lane;  // block of 32 values, token of the stage
+        int seq = 0, raws = 0;                          // stages so far, of the CTA; those with codes
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int kt = u / p.n_tiles;
+            const bool codes = kt < p.k_tiles;
+            const int col = kt * kPairTile + 128 * rank + 32 * b;
+            const bool in = codes && col < p.cols32;
+            const uint8_t *e_at = p.e + col / 32 + (long long)t * p.ld_e;
+            const long long e_step = (long long)kTokens * p.ld_e;
+            // this group's stages of the tile
+            const int g_first = (group - seq % kGroups + kGroups) % kGroups;
+            auto exponent = [&](int g) { return in && g < stages && g * kTokens + t < p.tokens ? (int)__ldg(e_at + g * e_step) : 127; };
+            int ahead[kAhead / kGroups];  // a load takes as long as some stages
+#pragma unroll
+            for (int i = 0; i < kAhead / kGroups; ++i) ahead[i] = exponent(g_first + kGroups * i);
+            for (int g = g_first; g < stages && ok;) {
+#pragma unroll
+                for (int i = 0; i < kAhead / kGroups; ++i) {  // (unrolled: a value on its way is not to be moved)
+                    if (g >= stages || !ok) break;
+                    const int e = ahead[i];
+                    ahead[i] = exponent(g + kAhead);
+                    const int n = seq + g, rs = (raws + g) % kPairRaw, ds = n % kPairDec;
+                    uint32_t q[8] = {};
+                    if (codes) {
+                        ok = mbar_wait(bar(bars.raw_full[rs]), (uint32_t)((raws + g) / kPairRaw & 1), abort_flag, &g_status, 16);
+                        load_codes<T>(raw0 + rs * kRawBytes, b, t, q);
+                    }
+                    if (ok) ok = mbar_wait(bar(bars.dec_empty[ds]), (uint32_t)(n / kPairDec & 1) ^ 1, abort_flag, &g_status, 32);
+                    ok = __all_sync(0xffffffffu, ok);
+                    put_values<T>(dec0 + ds * kDecBytes, b, t, q, e, !codes);
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar(bars.dec_full[ds]));
+                        // (only now: the codes have arrived in registers, not merely been asked for)
+                        if (codes) mbar_arrive(bar(bars.raw_empty[rs]));
+                    }
+                    g += kGroups;
+                }
+            }
+            seq += stages;
+            if (codes) raws += stages;
+        }
+    } else if (warp >= 4 + kGroups * kConvWarps) {
+        // ---------------------------------------------------------------------------------------- out
+        const int q = warp & 3;
+        Ring<2> a;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * kPairTile;
+            const bool sums = kt == p.k_tiles;  // db: every row of the accumulator is the same
+            const int k = kt * kPairTile + 128 * rank + 32 * q + lane;
+            const bool mine = sums ? rank == 0 && q == 0 && lane == 0 : k < p.k;
+            const int n_end = min(kPairTile, p.n - n0);
+            void *base = sums ? p.db : p.dw;
+            const long long at0 = sums ? n0 : (long long)n0 * p.ld_dw + k, step = sums ? 1 : p.ld_dw;
+            for (int ch = 0; ch < chunks && ok; ++ch) {
+                ok = mbar_wait(bar(bars.acc_full[a.slot]), a.phase, abort_flag, &g_status, 64);
+                fence_after();
+                const bool add = p.accumulate || ch > 0;
+                for (int j = 0; j < kPairTile; j += 32) {
+                    int raw[32];
+                    tmem_ld32(tmem + 256 * a.slot + ((uint32_t)(q * 32) << 16) + j, raw);
+                    tmem_wait_ld();
+                    const int rows = mine ? n_end - j : 0;
+                    if (p.out_dtype == ACCERL_F32) {
+                        float *at = static_cast<float *>(base) + at0 + j * step;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            if (i < rows) {
+                                if (add) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(at), "f"(__int_as_float(raw[i])) : "memory");
+                                else *at = __int_as_float(raw[i]);
+                            }
+                            at += step;
+                        }
+                    } else {
+                        T *at = static_cast<T *>(base) + at0 + j * step;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            if (i < rows) *at = from_float<T>(__int_as_float(raw[i]));
+                            at += step;
+                        }
+                    }
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(bars.acc_empty[a.slot]));
+                a.next();
+            }
+        }
+    }
+    if (*abort_flag)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    cg::this_cluster().sync();  // no barrier of a CTA is signalled once it has gone
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
 // dy at rows of a multiple of 16 bytes, for the TMA
@@ -462,10 +744,14 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     p.k = a->k;
     p.out_dtype = a->out_dtype;
     p.accumulate = a->accumulate != 0;
-    p.n_tile = std::min(256, (a->n + 63) / 64 * 64);
-    if (p.n_tile == 256 && ((long long)a->n + 255) / 256 * ((a->k + kTileK - 1) / kTileK) * 4 <= sm_count) p.n_tile = 128;
+    // Pairs where their tiles are at least three for every two pairs of SMs.
+    const long long pair_tiles = ((a->n + kPairTile - 1LL) / kPairTile) * ((a->k + kPairTile - 1LL) / kPairTile + (a->db ? 1 : 0));
+    const bool pair = 4 * pair_tiles >= 3 * sm_count;
+    p.n_tile = pair ? kPairTile : std::min(256, (a->n + 63) / 64 * 64);
+    if (!pair && p.n_tile == 256 && ((long long)a->n + 255) / 256 * ((a->k + kTileK - 1) / kTileK) * 4 <= sm_count) p.n_tile = 128;
     p.n_tiles = (a->n + p.n_tile - 1) / p.n_tile;
-    p.k_tiles = (a->k + kTileK - 1) / kTileK;
+    const int k_tile = pair ? kPairTile : kTileK;
+    p.k_tiles = (a->k + k_tile - 1) / k_tile;
     p.cols32 = cols32;
     const long long tiles = (long long)p.n_tiles * (p.k_tiles + (a->db ? 1 : 0));
     if (tiles > (1 << 30)) {
@@ -474,18 +760,20 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     }
     p.tiles = (int)tiles;
     const int stages = (a->tokens + kTokens - 1) / kTokens;
-    int share = 1;
-    share = std::max(1, std::min({kMaxShare, sm_count / p.tiles, stages / 2}));
-    const unsigned grid = share > 1 ? (unsigned)(p.tiles * share) : (unsigned)std::min(p.tiles, sm_count);
-    const size_t smem = 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens;
-    const auto kernel = a->dy_dtype == ACCERL_F16 ? weight_grad_kernel<__half> : weight_grad_kernel<__nv_bfloat16>;
+    const int share = pair ? 2 : std::max(1, std::min({kMaxShare, sm_count / p.tiles, stages / 2}));
+    const unsigned grid = pair        ? 2u * (unsigned)std::min(p.tiles, sm_count / 2)
+                          : share > 1 ? (unsigned)(p.tiles * share) : (unsigned)std::min(p.tiles, sm_count);
+    const size_t smem = pair ? kPairSmem : 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens;
+    const bool half = a->dy_dtype == ACCERL_F16;
+    const auto kernel = pair ? (half ? weight_grad_pair_kernel<__half> : weight_grad_pair_kernel<__nv_bfloat16>)
+                             : (half ? weight_grad_kernel<__half> : weight_grad_kernel<__nv_bfloat16>);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)share;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(pair ? kPairThreads : kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
