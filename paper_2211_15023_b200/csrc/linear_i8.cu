@@ -355,7 +355,7 @@ accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArg
 // SM in 128 cycles, half of what a single CTA's 128 x 256 tile would.  Two accumulators fill tensor memory, so that eight
 // warps (each 32 channels by 128 tokens, neighbouring lanes neighbours in a row of y) write a tile out while the next
 // one is computed; that takes some 8 instructions a value, and with four warps bounded the kernel.
-constexpr int kPairTile = 256, kPairStages = 6, kPairStage = 2 * 128 * 128, kPairOut = 8, kPairThreads = 32 * (kPairOut + 3);
+constexpr int kPairTile = 256, kPairStages = 6, kPairStage = 2 * 128 * 128, kPairOut = 8, kPairThreads = 32 * (kPairOut + 2);
 constexpr int kGroup = 8;  // token tiles whose channel tiles are walked together: their operands stay in L2
 
 __device__ __forceinline__ void pair_tile(const LinearArgs &p, int tile, int *channel, int *token)
@@ -394,7 +394,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(bar(bars.acc_full[a]), 1);
-            mbar_init(bar(bars.acc_empty[a]), kPairOut + (rank == 0 ? 1 : 0));  // the first CTA's: its warps, and the other's relay
+            mbar_init(bar(bars.acc_empty[a]), 2 * kPairOut);  // the first CTA's: the writing warps of both
         }
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -438,7 +438,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         int s = 0, a = 0;
         uint32_t phase = 0, aphase = 0;
         for (int u = first; u < tiles && ok; u += stride) {
-            ok = mbar_wait_cluster(bar(bars.acc_empty[a]), aphase ^ 1, abort_flag, &g_status, 4);
+            ok = mbar_wait(bar(bars.acc_empty[a]), aphase ^ 1, abort_flag, &g_status, 4);
             fence_after();
             for (int c = 0; c < p.chunks && ok; ++c) {
                 ok = mbar_wait(bar(bars.full[s]), phase, abort_flag, &g_status, 8);
@@ -456,16 +456,6 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                     phase ^= 1;
                 }
             }
-            if ((a ^= 1) == 0) aphase ^= 1;
-        }
-    } else if (warp == kPairOut + 2 && rank == 1) {
-        // the second CTA's accumulators, told to the first
-        int a = 0;
-        uint32_t aphase = 0;
-        for (int u = first; u < tiles && ok; u += stride) {
-            ok = mbar_wait(bar(bars.acc_empty[a]), aphase, abort_flag, &g_status, 128);
-            if (lane == 0) mbar_arrive_cluster(peer_addr(bar(bars.acc_empty[a]), 0));
-            __syncwarp();
             if ((a ^= 1) == 0) aphase ^= 1;
         }
     } else if (warp < kPairOut) {
@@ -505,7 +495,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
             }
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(bars.acc_empty[a]));
+            if (lane == 0) mbar_arrive_pair(peer_addr(bar(bars.acc_empty[a]), 0));
             if ((a ^= 1) == 0) aphase ^= 1;
         }
     }

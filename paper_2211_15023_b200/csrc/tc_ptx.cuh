@@ -170,38 +170,12 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar)
                  : "memory");
 }
 
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
+// Arrives on a barrier of either CTA of the pair.  What the arrival stands for is shared memory that fence.proxy.async has
+// handed to the tensor cores, or tensor memory that has been read (tcgen05.wait): nothing that a release at cluster scope
+// would have to make visible, and that waits for all the thread's memory traffic (1300 cycles an arrival were measured).
+__device__ __forceinline__ void mbar_arrive_pair(uint32_t cluster_bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-
-// A wait that also sees what the other CTA of the pair did before it arrived.  An arrival there at cluster scope waits
-// for everything its thread has under way (loads from global memory too), so one thread with nothing else to do passes
-// the arrivals of its CTA on.
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status, int code)
-{
-    auto arrived = [&] {
-        uint32_t ok;
-        asm volatile(
-            "{\n.reg .pred p;\n"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-            "selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        return ok != 0;
-    };
-    if (arrived()) return true;
-    unsigned ns = 32;
-    for (int i = 0; i < kWaitLimitPolls; ++i) {
-        __nanosleep(ns);
-        if (arrived()) return true;
-        if (*abort_flag) return false;
-        if (ns < 256) ns <<= 1;
-    }
-    *abort_flag = 1;
-    atomicOr(status, code);
-    return false;
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
 __device__ __forceinline__ void mma_f16_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)

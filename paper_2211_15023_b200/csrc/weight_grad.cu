@@ -435,7 +435,7 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             mbar_init(bar(bars.raw_empty[i]), kConvWarps);
         }
         for (int i = 0; i < kPairDec; ++i) {
-            mbar_init(bar(bars.dec_full[i]), kConvWarps + (rank == 0 ? 1 : 0));  // the first CTA's: its warps, and the other's relay
+            mbar_init(bar(bars.dec_full[i]), 2 * kConvWarps);  // the first CTA's: the warps of both
             mbar_init(bar(bars.dec_empty[i]), 1);
         }
         for (int i = 0; i < kPairDy; ++i) {
@@ -444,7 +444,7 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(bars.acc_full[i]), 1);
-            mbar_init(bar(bars.acc_empty[i]), 4 + (rank == 0 ? 1 : 0));  // the same
+            mbar_init(bar(bars.acc_empty[i]), 8);  // the first CTA's: the writing warps of both
         }
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -504,10 +504,10 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         for (int u = first; u < p.tiles && ok; u += stride) {
             for (int ch = 0; ch < chunks && ok; ++ch) {
                 const int g0 = (int)((long long)stages * ch / chunks), g1 = (int)((long long)stages * (ch + 1) / chunks);
-                ok = mbar_wait_cluster(bar(bars.acc_empty[a.slot]), a.phase ^ 1, abort_flag, &g_status, 4);
+                ok = mbar_wait(bar(bars.acc_empty[a.slot]), a.phase ^ 1, abort_flag, &g_status, 4);
                 fence_after();
                 for (int g = g0; g < g1 && ok; ++g) {
-                    ok = mbar_wait_cluster(bar(bars.dec_full[c.slot]), c.phase, abort_flag, &g_status, 8);
+                    ok = mbar_wait(bar(bars.dec_full[c.slot]), c.phase, abort_flag, &g_status, 8);
                     if (ok) ok = mbar_wait(bar(bars.dy_full[d.slot]), d.phase, abort_flag, &g_status, 8);
                     fence_after();
                     if (ok && elect_one()) {
@@ -526,26 +526,6 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 a.next();
             }
         }
-    } else if (warp == 1) {
-        // ------------------------------------------------- the second CTA's operands, told to the first
-        Ring<kPairDec> c;
-        for (int u = first; u < p.tiles && ok; u += stride)
-            for (int g = 0; g < stages && ok; ++g) {
-                ok = mbar_wait(bar(bars.dec_full[c.slot]), c.phase, abort_flag, &g_status, 128);
-                if (lane == 0) mbar_arrive_cluster(peer_addr(bar(bars.dec_full[c.slot]), 0));
-                __syncwarp();
-                c.next();
-            }
-    } else if (warp == 3 && rank == 1) {
-        // ---------------------------------------------- the second CTA's accumulators, told to the first
-        Ring<2> a;
-        for (int u = first; u < p.tiles && ok; u += stride)
-            for (int ch = 0; ch < chunks && ok; ++ch) {
-                ok = mbar_wait(bar(bars.acc_empty[a.slot]), a.phase, abort_flag, &g_status, 256);
-                if (lane == 0) mbar_arrive_cluster(peer_addr(bar(bars.acc_empty[a.slot]), 0));
-                __syncwarp();
-                a.next();
-            }
     } else if (warp >= 4 && warp < 4 + kGroups * kConvWarps) {
         // ------------------------------------------------------------------------------------ decoding
         const int group = (warp - 4) / kConvWarps, w = (warp - 4) % kConvWarps;
@@ -582,7 +562,7 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     fence_async();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(bar(bars.dec_full[ds]));
+                        mbar_arrive_pair(peer_addr(bar(bars.dec_full[ds]), 0));
                         // (only now: the codes have arrived in registers, not merely been asked for)
                         if (codes) mbar_arrive(bar(bars.raw_empty[rs]));
                     }
@@ -634,7 +614,7 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 }
                 fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(bars.acc_empty[a.slot]));
+                if (lane == 0) mbar_arrive_pair(peer_addr(bar(bars.acc_empty[a.slot]), 0));
                 a.next();
             }
         }
