@@ -397,13 +397,29 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // load, about 100 instructions, store, fence): two groups of eight warps take stages in turn.
 //
 // fp32 results: the tensor cores cut a sum off at every addition, which over 8192 tokens costs 4.5e-6 of the result's
-// norm (4e-7 with an fp32 product's rounding).  So the accumulator covers at most kChunk stages, and the parts
-// are added in fp32 to the result in memory, without waiting for it (one thread adds to a value, part by part: the order
-// is fixed): 5e-7.
+// norm (4e-7 with an fp32 product's rounding).  So an accumulator covers at most kChunk stages, and its parts are
+// added in fp32 by the warps that write: 5e-7.  The sum lies in the other half of tensor memory (adding in memory instead
+// cost 634 us with loads and 379 with reductions, for 8192 x 4096 x 4096), and the tensor cores wait while a part is
+// added, some 5 % of a part's time.  Results of one part, and 16-bit ones, have two accumulators in turn instead.
 constexpr int kPairTile = 256, kChunk = 24;
 constexpr int kPairRaw = 4, kPairDec = 5, kPairDy = 5, kPairDyBytes = 2 * 128 * kTokens, kGroups = 2;
-constexpr int kPairThreads = 32 * (4 + kGroups * kConvWarps + 4);
+constexpr int kPairOut = 8, kPairThreads = 32 * (4 + kGroups * kConvWarps + kPairOut);
 constexpr size_t kPairSmem = 1024 + kPairRaw * kRawBytes + kPairDec * kDecBytes + kPairDy * kPairDyBytes;
+
+// the accumulators in turn: two, or always the first
+struct Acc {
+    int slot = 0;
+    uint32_t phase = 0;
+    bool one;
+    __device__ __forceinline__ explicit Acc(bool single) : one(single) {}
+    __device__ __forceinline__ void next()
+    {
+        if (one || ++slot == 2) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
 
 struct __align__(8) PairBars {
     uint64_t raw_full[kPairRaw], raw_empty[kPairRaw], dec_full[kPairDec], dec_empty[kPairDec], dy_full[kPairDy], dy_empty[kPairDy],
@@ -444,7 +460,7 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(bars.acc_full[i]), 1);
-            mbar_init(bar(bars.acc_empty[i]), 8);  // the first CTA's: the writing warps of both
+            mbar_init(bar(bars.acc_empty[i]), 2 * kPairOut);  // the first CTA's: the writing warps of both
         }
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -500,7 +516,7 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         constexpr uint32_t idesc = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 15) | (1u << 16) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
         Ring<kPairDec> c;
         Ring<kPairDy> d;
-        Ring<2> a;
+        Acc a(chunks > 1);
         for (int u = first; u < p.tiles && ok; u += stride) {
             for (int ch = 0; ch < chunks && ok; ++ch) {
                 const int g0 = (int)((long long)stages * ch / chunks), g1 = (int)((long long)stages * (ch + 1) / chunks);
@@ -574,8 +590,9 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
     } else if (warp >= 4 + kGroups * kConvWarps) {
         // ---------------------------------------------------------------------------------------- out
-        const int q = warp & 3;
-        Ring<2> a;
+        const int q = warp & 3, j0 = (warp - (4 + kGroups * kConvWarps)) / 4 * (kPairTile / 2), j1 = j0 + kPairTile / 2;
+        const uint32_t quarter = tmem + ((uint32_t)(q * 32) << 16), total = quarter + 256;
+        Acc a(chunks > 1);
         for (int u = first; u < p.tiles && ok; u += stride) {
             const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * kPairTile;
             const bool sums = kt == p.k_tiles;  // db: every row of the accumulator is the same
@@ -584,39 +601,58 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             const int n_end = min(kPairTile, p.n - n0);
             void *base = sums ? p.db : p.dw;
             const long long at0 = sums ? n0 : (long long)n0 * p.ld_dw + k, step = sums ? 1 : p.ld_dw;
-            for (int ch = 0; ch < chunks && ok; ++ch) {
-                ok = mbar_wait(bar(bars.acc_full[a.slot]), a.phase, abort_flag, &g_status, 64);
-                fence_after();
-                const bool add = p.accumulate || ch > 0;
-                for (int j = 0; j < kPairTile; j += 32) {
-                    int raw[32];
-                    tmem_ld32(tmem + 256 * a.slot + ((uint32_t)(q * 32) << 16) + j, raw);
-                    tmem_wait_ld();
-                    const int rows = mine ? n_end - j : 0;
-                    if (p.out_dtype == ACCERL_F32) {
-                        float *at = static_cast<float *>(base) + at0 + j * step;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (i < rows) {
-                                if (add) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(at), "f"(__int_as_float(raw[i])) : "memory");
-                                else *at = __int_as_float(raw[i]);
-                            }
-                            at += step;
-                        }
-                    } else {
-                        T *at = static_cast<T *>(base) + at0 + j * step;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (i < rows) *at = from_float<T>(__int_as_float(raw[i]));
-                            at += step;
-                        }
-                    }
-                }
+            auto release = [&] {
                 fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_pair(peer_addr(bar(bars.acc_empty[a.slot]), 0));
                 a.next();
+            };
+            for (int ch = 0; ch < chunks && ok; ++ch) {
+                ok = mbar_wait(bar(bars.acc_full[a.slot]), a.phase, abort_flag, &g_status, 64);
+                fence_after();
+                if (chunks == 1) break;
+                for (int j = j0; j < j1; j += 16) {  // add the part to the sum
+                    int part[16], sum[16];
+                    tmem_ld16(quarter + j, part);
+                    if (ch > 0) tmem_ld16(total + j, sum);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[i] = ch > 0 ? __float_as_int(__int_as_float(sum[i]) + __int_as_float(part[i])) : part[i];
+                    tmem_st16(total + j, sum);
+                }
+                tmem_wait_st();
+                release();
             }
+            const uint32_t from = chunks > 1 ? total : quarter + 256 * a.slot;
+            for (int j = j0; j < j1; j += 16) {
+                int raw[16];
+                tmem_ld16(from + j, raw);
+                tmem_wait_ld();
+                const int rows = mine ? n_end - j : 0;
+                if (p.out_dtype == ACCERL_F32) {
+                    float *at = static_cast<float *>(base) + at0 + j * step;
+                    if (p.accumulate) {
+                        float old[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) old[i] = i < rows ? at[i * step] : 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) raw[i] = __float_as_int(__int_as_float(raw[i]) + old[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (i < rows) *at = __int_as_float(raw[i]);
+                        at += step;
+                    }
+                } else {
+                    T *at = static_cast<T *>(base) + at0 + j * step;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (i < rows) *at = from_float<T>(__int_as_float(raw[i]));
+                        at += step;
+                    }
+                }
+            }
+            if (chunks == 1) release();
         }
     }
     if (*abort_flag)
