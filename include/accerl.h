@@ -515,11 +515,14 @@ typedef struct {
     int32_t dy_dtype, out_dtype, accumulate;
 } accerl_weight_grad_args;
 
-/* bytes of the workspace: 0 where dy is aligned to 16 bytes with ld_dy a multiple of 8, else a copy of dy that is */
+/*
+ * Bytes of the workspace: a copy of dy where it is not aligned to 16 bytes with ld_dy a multiple of 8; the checkpoint's
+ * values in 16 bits (2 bytes a value, for the time of the call) where n and k are large (from 1025 channels on).
+ */
 int64_t accerl_ckpt_weight_grad_workspace(const accerl_weight_grad_args *args);
 
 /*
- * Asynchronous on `cuda_stream`, one launch (two with a workspace).  Errors: INVALID_ARG, UNSUPPORTED (fp32 dy), CUDA; a
+ * Asynchronous on `cuda_stream`, one to three launches.  Errors: INVALID_ARG, UNSUPPORTED (fp32 dy), CUDA; a
  * bounded wait on the device that gave up is reported by accerl_device_check.
  */
 accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *args, void *cuda_stream);

@@ -127,6 +127,44 @@ __device__ __forceinline__ void put_values(uint32_t dec, int b, int t, const uin
     }
 }
 
+// fp32 results: the tensor cores cut a sum off at every addition, which over 8192 tokens costs 4.5e-6 of the result's
+// norm (4e-7 with an fp32 product's rounding).  So an accumulator covers at most kChunk stages, and its parts are
+// added in fp32 by the warps that write: 5e-7.  The sum lies in the other half of tensor memory (adding in memory instead
+// cost 634 us with loads and 379 with reductions, for 8192 x 4096 x 4096), and the tensor cores wait while a part is
+// added, some 5 % of a part's time.  Results of one part, and 16-bit ones, have two accumulators in turn instead.
+constexpr int kChunk = 24;
+__host__ __device__ __forceinline__ int chunks_of(int out_dtype, int stages) { return out_dtype == ACCERL_F32 ? (stages + kChunk - 1) / kChunk : 1; }
+
+// the accumulators in turn: two, or always the first
+struct Acc {
+    int slot = 0;
+    uint32_t phase = 0;
+    bool one;
+    __device__ __forceinline__ explicit Acc(bool single) : one(single) {}
+    __device__ __forceinline__ void next()
+    {
+        if (one || ++slot == 2) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+// Adds a part to the sum in a warp's quarter of tensor memory (columns 256 behind it), or begins it.
+__device__ __forceinline__ void add_part(uint32_t quarter, int j0, int j1, bool begin)
+{
+    for (int j = j0; j < j1; j += 16) {
+        int part[16], sum[16];
+        tmem_ld16(quarter + j, part);
+        if (!begin) tmem_ld16(quarter + 256 + j, sum);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[i] = begin ? part[i] : __float_as_int(__int_as_float(sum[i]) + __int_as_float(part[i]));
+        tmem_st16(quarter + 256 + j, sum);
+    }
+    tmem_wait_st();
+}
+
 struct __align__(8) GradBars {
     uint64_t raw_full[kRaw], raw_empty[kRaw], dec_full[kDec], dec_empty[kDec], dy_full[kDy], dy_empty[kDy], acc_full[2], acc_empty[2];
     uint32_t tmem;
@@ -174,6 +212,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const int stages_all = (p.tokens + kTokens - 1) / kTokens;
     const int g0 = (int)((long long)stages_all * rank / share), g1 = (int)((long long)stages_all * (rank + 1) / share);
     const int first = (int)(blockIdx.x / (unsigned)share), stride = (int)(gridDim.x / (unsigned)share);
+    const int chunks = chunks_of(p.out_dtype, g1 - g0);
     volatile int *abort_flag = &bars.abort_flag;
     auto bar = [](uint64_t &b) { return smem_u32(&b); };
     if (threadIdx.x == 0) {
@@ -246,29 +285,31 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                ((uint32_t)(kTileK >> 4) << 24);
         Ring<kDec> c;
         Ring<kDy> d;
-        Ring<2> a;
-        for (int u = first; u < p.tiles && ok; u += stride) {
-            ok = mbar_wait(bar(bars.acc_empty[a.slot]), a.phase ^ 1, abort_flag, &g_status, 4);
-            fence_after();
-            for (int g = g0; g < g1 && ok; ++g) {
-                ok = mbar_wait(bar(bars.dec_full[c.slot]), c.phase, abort_flag, &g_status, 8);
-                if (ok) ok = mbar_wait(bar(bars.dy_full[d.slot]), d.phase, abort_flag, &g_status, 8);
+        Acc a(chunks > 1);
+        for (int u = first; u < p.tiles && ok; u += stride)
+            for (int ch = 0; ch < chunks && ok; ++ch) {
+                const int h0 = g0 + (int)((long long)(g1 - g0) * ch / chunks), h1 = g0 + (int)((long long)(g1 - g0) * (ch + 1) / chunks);
+                ok = mbar_wait(bar(bars.acc_empty[a.slot]), a.phase ^ 1, abort_flag, &g_status, 4);
                 fence_after();
-                if (ok && elect_one()) {
-                    const uint64_t ad = mn_desc(dec0 + c.slot * kDecBytes), bd = mn_desc(dy0 + d.slot * dy_bytes);
+                for (int g = h0; g < h1 && ok; ++g) {
+                    ok = mbar_wait(bar(bars.dec_full[c.slot]), c.phase, abort_flag, &g_status, 8);
+                    if (ok) ok = mbar_wait(bar(bars.dy_full[d.slot]), d.phase, abort_flag, &g_status, 8);
+                    fence_after();
+                    if (ok && elect_one()) {
+                        const uint64_t ad = mn_desc(dec0 + c.slot * kDecBytes), bd = mn_desc(dy0 + d.slot * dy_bytes);
 #pragma unroll
-                    for (int ks = 0; ks < kTokens / 16; ++ks)
-                        mma_f16(tmem + 256 * a.slot, ad + ks * (2048 >> 4), bd + ks * (2048 >> 4), idesc, (uint32_t)((g - g0) | ks));
-                    mma_commit(bar(bars.dec_empty[c.slot]));
-                    mma_commit(bar(bars.dy_empty[d.slot]));
-                    if (g == g1 - 1) mma_commit(bar(bars.acc_full[a.slot]));
+                        for (int ks = 0; ks < kTokens / 16; ++ks)
+                            mma_f16(tmem + 256 * a.slot, ad + ks * (2048 >> 4), bd + ks * (2048 >> 4), idesc, (uint32_t)((g - h0) | ks));
+                        mma_commit(bar(bars.dec_empty[c.slot]));
+                        mma_commit(bar(bars.dy_empty[d.slot]));
+                        if (g == h1 - 1) mma_commit(bar(bars.acc_full[a.slot]));
+                    }
+                    __syncwarp();
+                    c.next();
+                    d.next();
                 }
-                __syncwarp();
-                c.next();
-                d.next();
+                a.next();
             }
-            a.next();
-        }
     } else if (warp >= 4 && warp < 4 + kConvWarps) {
         // ------------------------------------------------------------------------------------ decoding
         const int w = warp - 4, b = w & 3, t = (w >> 2) * 32 + lane;  // block of 32 values, token of the stage
@@ -314,18 +355,31 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---------------------------------------------------------------------------------------- out
         const int q = warp & 3;
         const int kl = 32 * q + lane;
-        Ring<2> a;
+        const uint32_t quarter = tmem + ((uint32_t)(q * 32) << 16);
+        Acc a(chunks > 1);
+        auto release = [&] {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(bars.acc_empty[a.slot]));
+            a.next();
+        };
         for (int u = first; u < p.tiles && ok; u += stride) {
             const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * p.n_tile;
-            ok = mbar_wait(bar(bars.acc_full[a.slot]), a.phase, abort_flag, &g_status, 64);
-            fence_after();
+            for (int ch = 0; ch < chunks && ok; ++ch) {
+                ok = mbar_wait(bar(bars.acc_full[a.slot]), a.phase, abort_flag, &g_status, 64);
+                fence_after();
+                if (chunks == 1) break;
+                add_part(quarter, 0, p.n_tile, ch == 0);
+                release();
+            }
+            const uint32_t from = chunks > 1 ? quarter + 256 : quarter + 256 * a.slot;
             const bool sums = kt == p.k_tiles;  // db: every row of the accumulator is the same
             const int k = kt * kTileK + kl;
             const int n_end = min(p.n_tile, p.n - n0);
             float *part = reinterpret_cast<float *>(smem);  // [n_tile][128] of this CTA (share > 1: the rings are done with)
             for (int j = 0; j < p.n_tile; j += 32) {
                 int raw[32];
-                tmem_ld32(tmem + 256 * a.slot + ((uint32_t)(q * 32) << 16) + j, raw);
+                tmem_ld32(from + j, raw);
                 tmem_wait_ld();
                 if (share > 1) {
 #pragma unroll
@@ -342,10 +396,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                 }
             }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(bars.acc_empty[a.slot]));
-            a.next();
+            if (chunks == 1) release();
         }
     }
     if (share > 1) {  // one tile a cluster: every CTA adds up its share of the columns, four values a thread and a part's
@@ -395,31 +446,74 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // channels of dy; an instruction of the pair takes both CTAs' halves of dy, so that a CTA moves 40 KB a stage through its
 // shared memory instead of 56, and 24 KB instead of 40 from L2.  Decoding is a chain of some 700 cycles a stage (wait,
 // load, about 100 instructions, store, fence): two groups of eight warps take stages in turn.
-//
-// fp32 results: the tensor cores cut a sum off at every addition, which over 8192 tokens costs 4.5e-6 of the result's
-// norm (4e-7 with an fp32 product's rounding).  So an accumulator covers at most kChunk stages, and its parts are
-// added in fp32 by the warps that write: 5e-7.  The sum lies in the other half of tensor memory (adding in memory instead
-// cost 634 us with loads and 379 with reductions, for 8192 x 4096 x 4096), and the tensor cores wait while a part is
-// added, some 5 % of a part's time.  Results of one part, and 16-bit ones, have two accumulators in turn instead.
-constexpr int kPairTile = 256, kChunk = 24;
+constexpr int kPairTile = 256;
 constexpr int kPairRaw = 4, kPairDec = 5, kPairDy = 5, kPairDyBytes = 2 * 128 * kTokens, kGroups = 2;
 constexpr int kPairOut = 8, kPairThreads = 32 * (4 + kGroups * kConvWarps + kPairOut);
 constexpr size_t kPairSmem = 1024 + kPairRaw * kRawBytes + kPairDec * kDecBytes + kPairDy * kPairDyBytes;
 
-// the accumulators in turn: two, or always the first
-struct Acc {
-    int slot = 0;
-    uint32_t phase = 0;
-    bool one;
-    __device__ __forceinline__ explicit Acc(bool single) : one(single) {}
-    __device__ __forceinline__ void next()
-    {
-        if (one || ++slot == 2) {
-            slot = 0;
-            phase ^= 1;
+// The writing role of a pair's CTA (kPairOut warps, `warp` among them): parts are added up, tiles written.
+template <typename T>
+__device__ __forceinline__ void write_pair_tiles(const GradArgs &p, uint64_t *acc_full, uint64_t *acc_empty, uint32_t tmem, int warp, int lane,
+                                                 int rank, int first, int stride, int chunks, volatile int *abort_flag)
+{
+    bool ok = true;
+    auto bar = [](uint64_t &b) { return smem_u32(&b); };
+    const int q = warp & 3, j0 = warp / 4 * (kPairTile / 2), j1 = j0 + kPairTile / 2;  // a quarter of tensor memory, a half of the columns
+    const uint32_t quarter = tmem + ((uint32_t)(q * 32) << 16), total = quarter + 256;
+    Acc a(chunks > 1);
+    for (int u = first; u < p.tiles && ok; u += stride) {
+        const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * kPairTile;
+        const bool sums = kt == p.k_tiles;  // db: every row of the accumulator is the same
+        const int k = kt * kPairTile + 128 * rank + 32 * q + lane;
+        const bool mine = sums ? rank == 0 && q == 0 && lane == 0 : k < p.k;
+        const int n_end = min(kPairTile, p.n - n0);
+        void *base = sums ? p.db : p.dw;
+        const long long at0 = sums ? n0 : (long long)n0 * p.ld_dw + k, step = sums ? 1 : p.ld_dw;
+        auto release = [&] {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_pair(peer_addr(bar(acc_empty[a.slot]), 0));
+            a.next();
+        };
+        for (int ch = 0; ch < chunks && ok; ++ch) {
+            ok = mbar_wait(bar(acc_full[a.slot]), a.phase, abort_flag, &g_status, 64);
+            fence_after();
+            if (chunks == 1) break;
+            add_part(quarter, j0, j1, ch == 0);
+            release();
         }
+        const uint32_t from = chunks > 1 ? total : quarter + 256 * a.slot;
+        for (int j = j0; j < j1; j += 16) {
+            int raw[16];
+            tmem_ld16(from + j, raw);
+            tmem_wait_ld();
+            const int rows = mine ? n_end - j : 0;
+            if (p.out_dtype == ACCERL_F32) {
+                float *at = static_cast<float *>(base) + at0 + j * step;
+                if (p.accumulate) {
+                    float old[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) old[i] = i < rows ? at[i * step] : 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) raw[i] = __float_as_int(__int_as_float(raw[i]) + old[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (i < rows) *at = __int_as_float(raw[i]);
+                    at += step;
+                }
+            } else {
+                T *at = static_cast<T *>(base) + at0 + j * step;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (i < rows) *at = from_float<T>(__int_as_float(raw[i]));
+                    at += step;
+                }
+            }
+        }
+        if (chunks == 1) release();
     }
-};
+}
 
 struct __align__(8) PairBars {
     uint64_t raw_full[kPairRaw], raw_empty[kPairRaw], dec_full[kPairDec], dec_empty[kPairDec], dy_full[kPairDy], dy_empty[kPairDy],
@@ -441,7 +535,7 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cg::this_cluster().block_rank();
     const int stages = (p.tokens + kTokens - 1) / kTokens;
-    const int chunks = p.out_dtype == ACCERL_F32 ? (stages + kChunk - 1) / kChunk : 1;
+    const int chunks = chunks_of(p.out_dtype, stages);
     const int first = (int)blockIdx.x >> 1, stride = (int)gridDim.x >> 1;
     volatile int *abort_flag = &bars.abort_flag;
     auto bar = [](uint64_t &b) { return smem_u32(&b); };
@@ -590,70 +684,122 @@ weight_grad_pair_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
     } else if (warp >= 4 + kGroups * kConvWarps) {
         // ---------------------------------------------------------------------------------------- out
-        const int q = warp & 3, j0 = (warp - (4 + kGroups * kConvWarps)) / 4 * (kPairTile / 2), j1 = j0 + kPairTile / 2;
-        const uint32_t quarter = tmem + ((uint32_t)(q * 32) << 16), total = quarter + 256;
+        write_pair_tiles<T>(p, bars.acc_full, bars.acc_empty, tmem, warp - (4 + kGroups * kConvWarps), lane, rank, first, stride, chunks, abort_flag);
+    }
+    if (*abort_flag)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    cg::this_cluster().sync();  // no barrier of a CTA is signalled once it has gone
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// The same from a checkpoint that has been read back (ckpt_load) into 16-bit rows: both operands come by TMA.  Every tile
+// column of channels decodes a checkpoint anew, and decoding, not the tensor cores, bounds the kernel above (303 us for
+// 8192 x 4096 x 4096, of which the tensor cores need 190); reading it back once costs 3 bytes a value, about what a
+// 256-wide tile column takes on the tensor cores.  So from five tile columns on it is read back first.
+constexpr int kPlainStages = 6, kPlainStage = kDecBytes + kPairDyBytes, kPlainThreads = 32 * (kPairOut + 4);
+constexpr size_t kPlainSmem = 1024 + kDecBytes + kPlainStages * kPlainStage;
+
+template <typename T>
+__global__ void __launch_bounds__(kPlainThreads, 1)
+weight_grad_plain_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_dy,
+                         const __grid_constant__ GradArgs p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ struct {
+        uint64_t full[kPlainStages], empty[kPlainStages], acc_full[2], acc_empty[2];
+        uint32_t tmem;
+        int abort_flag;
+    } bars;
+    namespace cg = cooperative_groups;
+    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t ones = smem_u32(smem), ring = ones + kDecBytes;  // the operand of db; the stages
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cg::this_cluster().block_rank();
+    const int stages = (p.tokens + kTokens - 1) / kTokens;
+    const int chunks = chunks_of(p.out_dtype, stages);
+    const int first = (int)blockIdx.x >> 1, stride = (int)gridDim.x >> 1;
+    volatile int *abort_flag = &bars.abort_flag;
+    auto bar = [](uint64_t &b) { return smem_u32(&b); };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPlainStages; ++i) {
+            mbar_init(bar(bars.full[i]), 1);  // the first CTA's: the loads of both
+            mbar_init(bar(bars.empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(bars.acc_full[i]), 1);
+            mbar_init(bar(bars.acc_empty[i]), 2 * kPairOut);  // the first CTA's: the writing warps of both
+        }
+        bars.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    for (int i = threadIdx.x; i < kDecBytes / 16; i += kPlainThreads)
+        sts16(ones + 16 * i, make_uint4(Decode<T>::kOnes, Decode<T>::kOnes, Decode<T>::kOnes, Decode<T>::kOnes));
+    fence_async();
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    cg::this_cluster().sync();
+    fence_after();
+    const uint32_t tmem = bars.tmem;
+    bool ok = true;
+    if (warp == 0) {
+        Ring<kPlainStages> r;
+        for (int u = first; u < p.tiles && ok; u += stride) {
+            const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * kPairTile + 128 * rank;
+            const bool codes = kt < p.k_tiles;
+            for (int g = 0; g < stages && ok; ++g) {
+                ok = mbar_wait(bar(bars.empty[r.slot]), r.phase ^ 1, abort_flag, &g_status, 1);
+                if (ok && elect_one()) {
+                    const uint32_t full = peer_addr(bar(bars.full[r.slot]), 0), at = ring + r.slot * kPlainStage;
+                    if (rank == 0) mbar_expect_tx(bar(bars.full[r.slot]), codes ? 2 * kPlainStage : 2 * kPairDyBytes);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        if (codes) tma_load_2d_pair(at + b * kTokens * 128, &map_x, (kt * kPairTile + 128 * rank + 64 * b) * 2, g * kTokens, full);
+                        tma_load_2d_pair(at + kDecBytes + b * kTokens * 128, &map_dy, (n0 + 64 * b) * 2, g * kTokens, full);
+                    }
+                }
+                __syncwarp();
+                r.next();
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        constexpr uint32_t kType = std::is_same<T, __half>::value ? 0u : 1u;
+        constexpr uint32_t idesc = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 15) | (1u << 16) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+        Ring<kPlainStages> r;
         Acc a(chunks > 1);
         for (int u = first; u < p.tiles && ok; u += stride) {
-            const int kt = u / p.n_tiles, n0 = (u - kt * p.n_tiles) * kPairTile;
-            const bool sums = kt == p.k_tiles;  // db: every row of the accumulator is the same
-            const int k = kt * kPairTile + 128 * rank + 32 * q + lane;
-            const bool mine = sums ? rank == 0 && q == 0 && lane == 0 : k < p.k;
-            const int n_end = min(kPairTile, p.n - n0);
-            void *base = sums ? p.db : p.dw;
-            const long long at0 = sums ? n0 : (long long)n0 * p.ld_dw + k, step = sums ? 1 : p.ld_dw;
-            auto release = [&] {
-                fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_pair(peer_addr(bar(bars.acc_empty[a.slot]), 0));
-                a.next();
-            };
+            const bool codes = u / p.n_tiles < p.k_tiles;
             for (int ch = 0; ch < chunks && ok; ++ch) {
-                ok = mbar_wait(bar(bars.acc_full[a.slot]), a.phase, abort_flag, &g_status, 64);
+                const int g0 = (int)((long long)stages * ch / chunks), g1 = (int)((long long)stages * (ch + 1) / chunks);
+                ok = mbar_wait(bar(bars.acc_empty[a.slot]), a.phase ^ 1, abort_flag, &g_status, 4);
                 fence_after();
-                if (chunks == 1) break;
-                for (int j = j0; j < j1; j += 16) {  // add the part to the sum
-                    int part[16], sum[16];
-                    tmem_ld16(quarter + j, part);
-                    if (ch > 0) tmem_ld16(total + j, sum);
-                    tmem_wait_ld();
+                for (int g = g0; g < g1 && ok; ++g) {
+                    ok = mbar_wait(bar(bars.full[r.slot]), r.phase, abort_flag, &g_status, 8);
+                    fence_after();
+                    if (ok && elect_one()) {
+                        const uint32_t at = ring + r.slot * kPlainStage;
+                        const uint64_t ad = mn_desc(codes ? at : ones), bd = mn_desc(at + kDecBytes);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sum[i] = ch > 0 ? __float_as_int(__int_as_float(sum[i]) + __int_as_float(part[i])) : part[i];
-                    tmem_st16(total + j, sum);
+                        for (int ks = 0; ks < kTokens / 16; ++ks)
+                            mma_f16_pair(tmem + 256 * a.slot, ad + ks * (2048 >> 4), bd + ks * (2048 >> 4), idesc, (uint32_t)((g - g0) | ks));
+                        mma_commit_pair(bar(bars.empty[r.slot]));
+                        if (g == g1 - 1) mma_commit_pair(bar(bars.acc_full[a.slot]));
+                    }
+                    __syncwarp();
+                    r.next();
                 }
-                tmem_wait_st();
-                release();
+                a.next();
             }
-            const uint32_t from = chunks > 1 ? total : quarter + 256 * a.slot;
-            for (int j = j0; j < j1; j += 16) {
-                int raw[16];
-                tmem_ld16(from + j, raw);
-                tmem_wait_ld();
-                const int rows = mine ? n_end - j : 0;
-                if (p.out_dtype == ACCERL_F32) {
-                    float *at = static_cast<float *>(base) + at0 + j * step;
-                    if (p.accumulate) {
-                        float old[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) old[i] = i < rows ? at[i * step] : 0.f;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) raw[i] = __float_as_int(__int_as_float(raw[i]) + old[i]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (i < rows) *at = __int_as_float(raw[i]);
-                        at += step;
-                    }
-                } else {
-                    T *at = static_cast<T *>(base) + at0 + j * step;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (i < rows) *at = from_float<T>(__int_as_float(raw[i]));
-                        at += step;
-                    }
-                }
-            }
-            if (chunks == 1) release();
         }
+    } else if (warp >= 4) {
+        write_pair_tiles<T>(p, bars.acc_full, bars.acc_empty, tmem, warp - 4, lane, rank, first, stride, chunks, abort_flag);
     }
     if (*abort_flag)
         for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
@@ -692,12 +838,31 @@ cudaError_t weight_grad_status(int *out)  // (clears it)
 
 using namespace accerl;
 
-static bool dy_aligned(const accerl_weight_grad_args *a) { return !((uintptr_t)a->dy & 15) && a->ld_dy % 8 == 0; }
+namespace {
+
+// Which kernel, and what it needs beside its operands: sizes and dy's alignment decide.
+struct Plan {
+    bool pair = false, plain = false;
+    int64_t dy_bytes = 0, x_bytes = 0;
+};
+Plan plan_of(const accerl_weight_grad_args *a)
+{
+    Plan r;
+    const long long n_tiles = (a->n + kPairTile - 1LL) / kPairTile, k_tiles = (a->k + kPairTile - 1LL) / kPairTile;  // (whether db is wanted changes no bit of dw)
+    r.pair = n_tiles * k_tiles >= 111;  // three tiles for every two pairs of a B200's 148 SMs
+    r.plain = r.pair && n_tiles >= 5;
+    if (((uintptr_t)a->dy & 15) || a->ld_dy % 8) r.dy_bytes = (2LL * a->tokens * padded_n(a->n) + 255) / 256 * 256;
+    if (r.plain) r.x_bytes = (2LL * a->tokens * padded_n(a->k) + 255) / 256 * 256;
+    return r;
+}
+
+}  // namespace
 
 extern "C" int64_t accerl_ckpt_weight_grad_workspace(const accerl_weight_grad_args *a)
 {
-    if (!a || a->tokens < 1 || a->n < 1 || dy_aligned(a)) return 0;
-    return (2LL * a->tokens * padded_n(a->n) + 255) / 256 * 256;
+    if (!a || a->tokens < 1 || a->n < 1 || a->k < 1) return 0;
+    const Plan plan = plan_of(a);
+    return plan.dy_bytes + plan.x_bytes;
 }
 
 extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *a, void *cuda_stream)
@@ -737,17 +902,25 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     ACCERL_CUDA_TRY(cudaGetDevice(&device));
     ACCERL_CUDA_TRY(cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device));
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const void *dy = need ? a->workspace : a->dy;
-    const long long ld_dy = need ? padded_n(a->n) : a->ld_dy;
+    const Plan plan = plan_of(a);
+    const bool pair = plan.pair, copy = plan.dy_bytes > 0;
+    const void *dy = copy ? a->workspace : a->dy;
+    const long long ld_dy = copy ? padded_n(a->n) : a->ld_dy;
+    void *x = static_cast<char *>(a->workspace) + plan.dy_bytes;
     CUtensorMap mq, md;
-    accerl_status s = tc_make_map(&mq, a->q, a->tokens, cols32, a->ld_q, kTokens, 128);
+    accerl_status s = plan.plain ? tc_make_map(&mq, x, a->tokens, 2 * a->k, 2 * padded_n(a->k), kTokens, 128)
+                                 : tc_make_map(&mq, a->q, a->tokens, cols32, a->ld_q, kTokens, 128);
     if (s == ACCERL_OK) s = tc_make_map(&md, dy, a->tokens, 2 * a->n, 2 * ld_dy, kTokens, 128);
     if (s != ACCERL_OK) return s;
-    if (need) {
+    if (copy) {
         const dim3 grid((unsigned)std::min((a->n + 2047) / 2048, 1024), (unsigned)std::min(a->tokens, 65535));
         realign_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(a->dy), a->ld_dy, static_cast<uint16_t *>(a->workspace),
                                              padded_n(a->n), a->tokens, a->n);
         ACCERL_CUDA_TRY(cudaGetLastError());
+    }
+    if (plan.plain) {
+        s = accerl_ckpt_load(a->q, a->ld_q, a->e, a->ld_e, a->tokens, a->k, x, padded_n(a->k), a->dy_dtype, cuda_stream);
+        if (s != ACCERL_OK) return s;
     }
     GradArgs p;
     p.e = a->e;
@@ -760,9 +933,6 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     p.k = a->k;
     p.out_dtype = a->out_dtype;
     p.accumulate = a->accumulate != 0;
-    // Pairs where their tiles are at least three for every two pairs of SMs.
-    const long long pair_tiles = ((a->n + kPairTile - 1LL) / kPairTile) * ((a->k + kPairTile - 1LL) / kPairTile + (a->db ? 1 : 0));
-    const bool pair = 4 * pair_tiles >= 3 * sm_count;
     p.n_tile = pair ? kPairTile : std::min(256, (a->n + 63) / 64 * 64);
     if (!pair && p.n_tile == 256 && ((long long)a->n + 255) / 256 * ((a->k + kTileK - 1) / kTileK) * 4 <= sm_count) p.n_tile = 128;
     p.n_tiles = (a->n + p.n_tile - 1) / p.n_tile;
@@ -779,9 +949,10 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     const int share = pair ? 2 : std::max(1, std::min({kMaxShare, sm_count / p.tiles, stages / 2}));
     const unsigned grid = pair        ? 2u * (unsigned)std::min(p.tiles, sm_count / 2)
                           : share > 1 ? (unsigned)(p.tiles * share) : (unsigned)std::min(p.tiles, sm_count);
-    const size_t smem = pair ? kPairSmem : 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens;
+    const size_t smem = plan.plain ? kPlainSmem : pair ? kPairSmem : 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens;
     const bool half = a->dy_dtype == ACCERL_F16;
-    const auto kernel = pair ? (half ? weight_grad_pair_kernel<__half> : weight_grad_pair_kernel<__nv_bfloat16>)
+    const auto kernel = plan.plain ? (half ? weight_grad_plain_kernel<__half> : weight_grad_plain_kernel<__nv_bfloat16>)
+                        : pair ? (half ? weight_grad_pair_kernel<__half> : weight_grad_pair_kernel<__nv_bfloat16>)
                              : (half ? weight_grad_kernel<__half> : weight_grad_kernel<__nv_bfloat16>);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
@@ -789,7 +960,7 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     attr[0].val.clusterDim.x = (unsigned)share;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(pair ? kPairThreads : kThreads);
+    cfg.blockDim = dim3(plan.plain ? kPlainThreads : pair ? kPairThreads : kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;

@@ -55,7 +55,7 @@ def check(got, want, slack, out):
 # tokens: parts of a stage, split over a cluster or not; n: every tile width and parts of it; k: parts of a tile and a block
 SIZES = [(1, 1, 1), (3, 16, 32), (64, 64, 128), (65, 70, 129), (63, 130, 40), (200, 256, 100), (512, 257, 300), (1000, 18, 512),
          (2047, 256, 2592), (300, 1000, 1000), (129, 515, 2100), (5000, 40, 200), (1030, 4100, 1300),
-         (70, 3000, 2900), (3333, 2050, 2570), (1, 5000, 2500)]
+         (70, 3000, 2900), (3333, 2050, 2570), (1, 5000, 2500), (200, 600, 9000), (2500, 300, 14001)]
 
 
 @pytest.mark.parametrize("t,n,k", SIZES)

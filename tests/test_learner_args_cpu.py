@@ -173,3 +173,6 @@ def test_ckpt_weight_grad_workspace_and_types(lib):
     assert lib.accerl_ckpt_weight_grad_workspace(C.byref(grad_args())) == 0
     assert lib.accerl_ckpt_weight_grad_workspace(C.byref(grad_args(n=15, ld_dy=15))) == 256  # 4 rows of 16 16-bit values
     assert lib.accerl_ckpt_weight_grad_workspace(C.byref(grad_args(dy=AT + 2, tokens=1 << 20, n=1 << 14, ld_dy=1 << 14))) == 1 << 35
+    # many tiles, five or more columns of channels: the checkpoint's values in 16 bits
+    big = dict(n=2048, ld_dy=2048, k=4001, ld_q=4032, ld_e=126, ld_dw=4001, tokens=100)
+    assert lib.accerl_ckpt_weight_grad_workspace(C.byref(grad_args(**big))) == (100 * 4008 * 2 + 255) // 256 * 256
