@@ -12,6 +12,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "learn.cuh"
 #include "tc_image.cuh"
@@ -53,6 +54,20 @@ __device__ __forceinline__ uint32_t quantised4(const float *v, float s, float in
     for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(b4[k]);
     return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }
+
+// what a row's largest magnitude makes of it
+struct Scale {
+    float s, inv;
+    bool zero, exact;
+    __device__ __forceinline__ explicit Scale(uint32_t top)
+    {
+        const bool broken = top >= 0x7f800000u;  // an infinity or a NaN
+        s = broken ? NAN : __fdiv_rn(__uint_as_float(top), 127.f);
+        zero = broken || s == 0.f;
+        exact = s < 1e-30f;  // (tiny scales: 1 / s may overflow, s itself be coarse)
+        inv = zero || exact ? 0.f : __fdiv_rn(1.f, s);
+    }
+};
 
 template <typename T>
 __device__ __forceinline__ void quantise_piece(const QuantArgs &p, int8_t *q_row, int first, const uint4 &raw, float s, float inv,
@@ -109,16 +124,13 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) quant_rows_kernel(const __g
         __syncthreads();
         top = __reduce_max_sync(0xffffffffu, lane < lanes / 32 ? s_top[lane] : 0u);
     }
-    const bool broken = top >= 0x7f800000u;
-    const float s = broken ? NAN : __fdiv_rn(__uint_as_float(top), 127.f);
-    const bool zero = broken || s == 0.f, exact = s < 1e-30f;  // (tiny scales: 1 / s may overflow, s itself be coarse)
-    const float inv = zero || exact ? 0.f : __fdiv_rn(1.f, s);
-    if (first == 0) p.scale[row] = s;
+    const Scale sc(top);
+    if (first == 0) p.scale[row] = sc.s;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) quantise_piece<T>(p, q, first + i * step, raw[i], s, inv, exact, zero);
+    for (int i = 0; i < NV; ++i) quantise_piece<T>(p, q, first + i * step, raw[i], sc.s, sc.inv, sc.exact, sc.zero);
     if constexpr (LOOP)
         for (int at = first + NV * step; at < p.cols; at += step)
-            quantise_piece<T>(p, q, at, load_piece<T, ALIGNED>(x, at, p.cols, 0.f), s, inv, exact, zero);
+            quantise_piece<T>(p, q, at, load_piece<T, ALIGNED>(x, at, p.cols, 0.f), sc.s, sc.inv, sc.exact, sc.zero);
 }
 
 template <typename T, bool ALIGNED>
@@ -157,6 +169,8 @@ struct LinearArgs {
     int tokens, n, k, y_dtype, relu;
     int chunks;  // of 128 bytes along K
     int stages;
+    const void *x;  // tokens that the product quantises itself
+    long long ld_x;
 };
 
 __device__ __forceinline__ void store_y(const LinearArgs &p, int t, int n, float v)
@@ -174,11 +188,16 @@ __device__ __forceinline__ float at_least(float v, float floor)  // (a NaN stays
     return m;
 }
 
+constexpr int kFused = 4;  // up to so many tokens are quantised by the product itself
 constexpr int kFewThreads = 192, kMaxStages = 8, kMaxShare = 8;
 
 // One tile of 128 channels x NT tokens; the CTAs of a cluster share its K.
 // Warps 0..3 drain the accumulator (and finish), warp 4 loads, warp 5 issues the tensor-core instructions.
-template <int NT>
+//
+// XT: the type of up to kFused tokens that the kernel quantises itself (void: they come quantised): warps 0..3 find the
+// tokens' maxima and write this CTA's part of K as the operand, while the weights are on their way.  Every CTA reads the
+// tokens whole (from L2), which a launch less repays for a few of them only.
+template <int NT, typename XT>
 __global__ void __launch_bounds__(kFewThreads)
 linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                   const __grid_constant__ LinearArgs p)
@@ -189,10 +208,15 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         uint32_t tmem;
         int abort_flag;
     } bars;
+    __shared__ uint32_t s_top[kFused][4];
+    __shared__ float s_scale[kFused];
+    __shared__ uint64_t s_ready;
     namespace cg = cooperative_groups;
-    constexpr int kStage = 128 * 128 + NT * 128, kCols = NT < 32 ? 32 : NT;
+    constexpr bool FUSED = !std::is_void<XT>::value;
+    constexpr int kStage = 128 * 128 + (FUSED ? 0 : NT * 128), kCols = NT < 32 ? 32 : NT;
     uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t base = smem_u32(smem), full0 = smem_u32(&bars.full[0]), empty0 = smem_u32(&bars.empty[0]);
+    const uint32_t tokens0 = base + p.stages * kStage;  // FUSED: [chunk][NT][128], swizzled
     const int warp = threadIdx.x >> 5;
     const int share = (int)cg::this_cluster().num_blocks(), rank = (int)cg::this_cluster().block_rank();
     const int n0 = (int)(blockIdx.x / (unsigned)share) * 128, t0 = (int)blockIdx.y * NT;
@@ -204,6 +228,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
             mbar_init(empty0 + 8 * s, 1);
         }
         mbar_init(smem_u32(&bars.acc), 1);
+        mbar_init(smem_u32(&s_ready), 4);
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
@@ -239,18 +264,20 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                     mbar_expect_tx(full0 + 8 * s, kStage);
                     tma_load_2d(at, &map_w, (c0 + i) * 128, n0, full0 + 8 * s);
                 }
-                tma_load_2d(at + 128 * 128, &map_x, (c0 + i) * 128, t0, full0 + 8 * s);
+                if (!FUSED) tma_load_2d(at + 128 * 128, &map_x, (c0 + i) * 128, t0, full0 + 8 * s);
             }
             __syncwarp();
         }
     } else if (warp == 5) {
         bool ok = true;
+        if (FUSED) ok = mbar_wait(smem_u32(&s_ready), 0, abort_flag, &g_status, 32);
         for (int i = 0; i < c1 - c0 && ok; ++i) {
             const int s = i % p.stages;
             ok = mbar_wait(full0 + 8 * s, (uint32_t)((i / p.stages) & 1), abort_flag, &g_status, 8);
             fence_after();
             if (ok && elect_one()) {
-                const uint64_t a = make_desc(base + s * kStage, 128), b = make_desc(base + s * kStage + 128 * 128, 128);
+                const uint64_t a = make_desc(base + s * kStage, 128),
+                               b = make_desc(FUSED ? tokens0 + i * (NT * 128) : base + s * kStage + 128 * 128, 128);
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks) mma_i8(tmem, a + 2 * ks, b + 2 * ks, idesc_for(NT), (uint32_t)(i | ks));
                 mma_commit(empty0 + 8 * s);
@@ -259,6 +286,43 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
             __syncwarp();
         }
     } else {
+        if constexpr (FUSED) {
+            constexpr int V = Row<XT>::kVec;
+            const int lane = threadIdx.x & 31;
+            for (int t = 0; t < p.tokens; ++t) {
+                const XT *x = static_cast<const XT *>(p.x) + t * p.ld_x;
+                uint32_t top = 0;
+#pragma unroll 4
+                for (int k = (int)threadIdx.x * V; k < p.k; k += 128 * V) {
+                    float v[V];
+                    unpack<XT>(load_piece<XT>(x, k, p.k, 0.f), v);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) top = max(top, magnitude(v[j]));
+                }
+                top = __reduce_max_sync(0xffffffffu, top);
+                if (lane == 0) s_top[t][warp] = top;
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            for (int i = threadIdx.x; i < p.tokens * (c1 - c0) * 8; i += 128) {  // sixteen values
+                const int piece = i % 8, c = i / 8 % (c1 - c0), t = i / 8 / (c1 - c0);
+                const Scale sc(max(max(s_top[t][0], s_top[t][1]), max(s_top[t][2], s_top[t][3])));
+                if (piece == 0 && c == 0) s_scale[t] = sc.s;
+                const XT *x = static_cast<const XT *>(p.x) + t * p.ld_x;
+                uint32_t w[4];
+#pragma unroll
+                for (int h = 0; h < 16 / V; ++h) {
+                    float v[V];
+                    unpack<XT>(load_piece<XT>(x, (c0 + c) * 128 + piece * 16 + h * V, p.k, 0.f), v);
+#pragma unroll
+                    for (int j = 0; j < V / 4; ++j) w[h * (V / 4) + j] = sc.zero ? 0u : quantised4(v + 4 * j, sc.s, sc.inv, sc.exact);
+                }
+                sts16(tokens0 + c * (NT * 128) + t * 128 + ((piece ^ (t & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_ready));
+            asm volatile("bar.sync 1, 128;" ::: "memory");  // (the scales)
+        }
         mbar_wait(smem_u32(&bars.acc), 0, abort_flag, &g_status, 16);
         fence_after();
     }
@@ -272,7 +336,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the tokens' scales are the quantiser's
     auto finish = [&](int t, int acc) {
         if (!mine || t >= p.tokens) return;
-        store_y(p, t, n, at_least(fmaf((float)acc, p.x_scale[t] * ws, bias), p.relu ? 0.f : -INFINITY));
+        store_y(p, t, n, at_least(fmaf((float)acc, (FUSED ? s_scale[t % kFused] : p.x_scale[t]) * ws, bias), p.relu ? 0.f : -INFINITY));
     };
     int *part = reinterpret_cast<int *>(smem);  // [NT][128]: every operand has been read
     if (warp < 4) {
@@ -308,7 +372,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                     acc[3] += x[c].w;
                 }
             const int t = t0 + i / 32, n4 = n0 + i % 32 * 4;
-            const float xs = p.x_scale[t], floor = p.relu ? 0.f : -INFINITY;
+            const float xs = FUSED ? s_scale[t % kFused] : p.x_scale[t], floor = p.relu ? 0.f : -INFINITY;
 #pragma unroll
             for (int l = 0; l < 4; ++l)
                 if (n4 + l < p.n)
@@ -323,15 +387,22 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kCols) : "memory");
 }
 
-template <int NT>
+int few_share(const LinearArgs &p, int tiles, int sm_count)
+{
+    int share = 1;
+    while (share < kMaxShare && (long long)tiles * share < sm_count && p.chunks >= 4 * share) share *= 2;
+    return share;
+}
+
+template <int NT, typename XT>
 accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArgs &p, int sm_count, bool after_quant, cudaStream_t st)
 {
-    constexpr int kStage = 128 * 128 + NT * 128;
-    p.stages = std::min(kMaxStages, 110 * 1024 / kStage);
-    const size_t smem = 1024 + (size_t)p.stages * kStage;
-    const int tiles = (p.n + 127) / 128, token_tiles = (p.tokens + NT - 1) / NT;
-    int share = 1;
-    while (share < kMaxShare && (long long)tiles * token_tiles * share < sm_count && p.chunks >= 4 * share) share *= 2;
+    constexpr bool FUSED = !std::is_void<XT>::value;
+    constexpr int kStage = 128 * 128 + (FUSED ? 0 : NT * 128);
+    const int tiles = (p.n + 127) / 128, token_tiles = (p.tokens + NT - 1) / NT, share = few_share(p, tiles * token_tiles, sm_count);
+    const size_t own = FUSED ? (size_t)((p.chunks + share - 1) / share) * NT * 128 : 0;  // the tokens' part
+    p.stages = std::min<int>(kMaxStages, (int)((110 * 1024 - own) / kStage));
+    const size_t smem = 1024 + (size_t)p.stages * kStage + own;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -345,8 +416,8 @@ accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArg
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = after_quant ? 2 : 1;
-    ACCERL_CUDA_TRY(allow_smem((const void *)linear_few_kernel<NT>, smem));
-    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_few_kernel<NT>, mw, mx, p));
+    ACCERL_CUDA_TRY(allow_smem((const void *)linear_few_kernel<NT, XT>, smem));
+    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_few_kernel<NT, XT>, mw, mx, p));
     return ACCERL_OK;
 }
 
@@ -638,16 +709,19 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
     accerl_status s = tc_make_map(&mw, a->w, a->n, a->k, a->ld_w, 128, 128);
     if (s == ACCERL_OK) s = tc_make_map(&mx, xq, a->tokens, a->k, ld_xq, nt, 128);
     if (s != ACCERL_OK) return s;
+    LinearArgs p{xs, a->w_scale, a->bias, a->y, a->ld_y, a->tokens, a->n, a->k, a->y_dtype, a->relu != 0, (a->k + 127) / 128, 0, a->x, a->ld_x};
+    // (the tokens' part of K in shared memory: 32 KB at most)
+    if (!given && a->tokens <= kFused && p.chunks <= 16 * few_share(p, (a->n + 127) / 128, sm_count))
+        return with_dtype(a->x_dtype, [&](auto v) { return launch_few<16, decltype(v)>(mw, mx, p, sm_count, false, st); });
     if (!given) {
         const QuantArgs q{a->x, static_cast<int8_t *>(a->workspace), const_cast<float *>(xs), a->ld_x, ld_xq, a->tokens, a->k};
         ACCERL_CUDA_TRY(launch_quant(q, a->x_dtype, sm_count, st));
     }
-    LinearArgs p{xs, a->w_scale, a->bias, a->y, a->ld_y, a->tokens, a->n, a->k, a->y_dtype, a->relu != 0, (a->k + 127) / 128, 0};
     if (pair) return launch_pair(mw, mx, p, sm_count, !given, st);
-    return nt == 16   ? launch_few<16>(mw, mx, p, sm_count, !given, st)
-           : nt == 32 ? launch_few<32>(mw, mx, p, sm_count, !given, st)
-           : nt == 64 ? launch_few<64>(mw, mx, p, sm_count, !given, st)
-                      : launch_few<128>(mw, mx, p, sm_count, !given, st);
+    return nt == 16   ? launch_few<16, void>(mw, mx, p, sm_count, !given, st)
+           : nt == 32 ? launch_few<32, void>(mw, mx, p, sm_count, !given, st)
+           : nt == 64 ? launch_few<64, void>(mw, mx, p, sm_count, !given, st)
+                      : launch_few<128, void>(mw, mx, p, sm_count, !given, st);
 }
 
 extern "C" accerl_status accerl_device_check(void)

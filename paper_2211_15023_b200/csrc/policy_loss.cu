@@ -70,6 +70,7 @@ __device__ __forceinline__ float expm1_of(float x) { return expm1f(x); }
 template <typename R>
 struct RowResult {
     R base, slope;
+    float pg, r, kl, H;  // what the sums over rows take (r negative where the clamp decided)
 };
 template <typename R>
 __device__ __forceinline__ RowResult<R> finish_row(const LossArgs &p, long long row, double logp, R kl_full, R H, bool empty, bool writer)
@@ -93,13 +94,17 @@ __device__ __forceinline__ RowResult<R> finish_row(const LossArgs &p, long long 
             slope -= (R)p.kl_coef * e;
         }
     }
-    if (writer) {
-        *reinterpret_cast<float2 *>(p.terms + 2 * row) = make_float2((float)pg, inside ? (float)r : -(float)r);
-        p.logp[row] = (float)logp;
-        p.kl[row] = (float)kl;
-        p.entropy[row] = (float)H;
-    }
     RowResult<R> o;
+    o.pg = (float)pg;
+    o.r = inside ? (float)r : -(float)r;
+    o.kl = (float)kl;
+    o.H = (float)H;
+    if (writer) {
+        *reinterpret_cast<float2 *>(p.terms + 2 * row) = make_float2(o.pg, o.r);
+        p.logp[row] = (float)logp;
+        p.kl[row] = o.kl;
+        p.entropy[row] = o.H;
+    }
     o.slope = slope;
     o.base = -slope + (R)p.entropy_coef * H - (p.ref && p.kl_coef != 0.f ? (R)p.kl_coef * kl : (R)0);
     return o;
@@ -111,14 +116,119 @@ __device__ __forceinline__ void skip_row(const LossArgs &p, long long row)
     *reinterpret_cast<float2 *>(p.terms + 2 * row) = make_float2(0.f, 0.f);
 }
 
+// -------------------------------------------------------------------------------------- sums over rows
+constexpr int kStatsThreads = 1024, kStatsCluster = 8, kSums = 7;
+
+// A row's share of the sums: weight, pg, kl, H, and r, negative where the clamp decided.
+struct RowSums {
+    double sum[kSums] = {};
+    float most = -INFINITY;
+    __device__ __forceinline__ void add(const LossArgs &p, float weight, float pg, float kl, float H, float r)
+    {
+        const double w = (double)weight;
+        sum[0] += w * ((double)pg + (p.kl_coef != 0.f ? (double)p.kl_coef * kl : 0.0) - (double)p.entropy_coef * H);
+        sum[1] += w * (double)pg;
+        sum[2] += w * (double)kl;
+        sum[3] += w * (double)H;
+        sum[4] += signbit(r) ? w : 0.0;
+        sum[5] += w;
+        sum[6] += w * fabs((double)r);
+        most = fmaxf(most, kl);
+    }
+};
+
+// Adds up the rows' shares of the threads of a cluster (of one CTA or eight) in a fixed order.  The cluster's first barrier
+// phase has been arrived at.
+__device__ __forceinline__ void write_stats(RowSums s, float *__restrict__ stats)
+{
+    namespace cg = cooperative_groups;
+    __shared__ double s_sum[kStatsThreads / 32][kSums];
+    __shared__ float s_max[kStatsThreads / 32];
+    __shared__ double c_sum[kStatsCluster][kSums];  // used in the first CTA
+    __shared__ float c_max[kStatsCluster];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+        for (int j = 0; j < kSums; ++j) s.sum[j] += __shfl_xor_sync(0xffffffffu, s.sum[j], o);
+        s.most = fmaxf(s.most, __shfl_xor_sync(0xffffffffu, s.most, o));
+    }
+    if (lane == 0) {
+#pragma unroll
+        for (int j = 0; j < kSums; ++j) s_sum[warp][j] = s.sum[j];
+        s_max[warp] = s.most;
+    }
+    __syncthreads();
+    asm volatile("barrier.cluster.wait;" ::: "memory");  // the first CTA has started
+    if (warp == 0) {
+#pragma unroll
+        for (int j = 0; j < kSums; ++j) s.sum[j] = lane < warps ? s_sum[lane][j] : 0.0;
+        s.most = lane < warps ? s_max[lane] : -INFINITY;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+            for (int j = 0; j < kSums; ++j) s.sum[j] += __shfl_xor_sync(0xffffffffu, s.sum[j], o);
+            s.most = fmaxf(s.most, __shfl_xor_sync(0xffffffffu, s.most, o));
+        }
+        if (lane == 0) {
+            const unsigned rank = cg::this_cluster().block_rank();
+#pragma unroll
+            for (int j = 0; j < kSums; ++j) *cg::this_cluster().map_shared_rank(&c_sum[rank][j], 0) = s.sum[j];
+            *cg::this_cluster().map_shared_rank(&c_max[rank], 0) = s.most;
+        }
+    }
+    cg::this_cluster().sync();
+    if (blockIdx.x == 0 && threadIdx.x < kSums) {
+        double v = 0.0;
+        for (unsigned i = 0; i < gridDim.x; ++i) v += c_sum[i][threadIdx.x];
+        const int j = (int)threadIdx.x;
+        stats[j < 6 ? j : 7] = (float)v;
+        if (j == 0) {
+            float most = -INFINITY;
+            for (unsigned i = 0; i < gridDim.x; ++i) most = fmaxf(most, c_max[i]);
+            stats[6] = most == -INFINITY ? 0.f : most;
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kStatsThreads)
+loss_stats_kernel(const __grid_constant__ LossArgs p, float *__restrict__ stats)
+{
+    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    RowSums s;
+    const long long stride = (long long)gridDim.x * blockDim.x;
+    constexpr int kAhead = 4;  // rows whose loads are in flight: the kernel is a chain of memory latencies
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < p.rows; i += kAhead * stride) {
+        float w[kAhead], kl[kAhead], H[kAhead];
+        float2 t[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const long long row = min(i + j * stride, (long long)p.rows - 1);
+            w[j] = i + j * stride < p.rows ? weight_of(p, row) : 0.f;
+            t[j] = __ldcg(reinterpret_cast<const float2 *>(p.terms + 2 * row));
+            kl[j] = __ldcg(p.kl + row);
+            H[j] = __ldcg(p.entropy + row);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (w[j] != 0.f) s.add(p, w[j], t[j].x, kl[j], H[j], t[j].y);
+    }
+    write_stats(s, stats);
+}
+
 // ------------------------------------------------------------------------------------------ narrow rows
 // Up to 64 actions: a group of G lanes per row, at most 8 elements a lane, in double (two exponentials an element are
 // free beside the latencies here, and whether a ratio is clipped is decided where the definition decides it).
 constexpr int kNarrow = 64, kNarrowPer = 8;
 
-template <typename T, bool REF, int G>
-__global__ void __launch_bounds__(128) loss_narrow_kernel(const __grid_constant__ LossArgs p)
+//
+// STATS (few rows, one CTA): the sums over rows come out of the same launch.
+template <typename T, bool REF, int G, bool STATS>
+__global__ void __launch_bounds__(STATS ? 1024 : 128) loss_narrow_kernel(const __grid_constant__ LossArgs p, float *__restrict__ stats)
 {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (STATS) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     __shared__ double table[64];
     fill_exp_table(table);
     __syncthreads();
@@ -180,33 +290,37 @@ __global__ void __launch_bounds__(128) loss_narrow_kernel(const __grid_constant_
     for (int k = 0; k < kNarrowPer; ++k)
         if (known && k == (int)a / G) za = z[k];
     za = __shfl_sync(0xffffffffu, za, known ? (int)a % G : 0, G);
-    if (!live) return;
-    T *g_row = static_cast<T *>(p.grad) + row * p.ld_grad;
-    if (!work) {
+    RowSums sums;
+    T *g_row = p.grad ? static_cast<T *>(p.grad) + (live ? row : 0) * p.ld_grad : nullptr;
+    if (live && !work) {
         if (lane == 0) skip_row(p, row);
-        if (p.grad)
+        if (g_row)
             for (int v = lane; v < p.A; v += G) g_row[v] = from_float<T>(0.f);
-        return;
     }
-    const double lso = log(so), lsr = REF ? log(ss) : 0.0;
-    const double logp = known ? ((double)za - mo) - lso : (double)NAN;
-    const double kl = REF ? sd / so - (lso - lsr) : 0.0, H = lso - st / so;
-    // (a row without a finite logit: log 0 everywhere, and no distribution to have a gradient)
-    const RowResult<double> f = finish_row<double>(p, row, empty && known ? -INFINITY : logp, kl, H, empty && known, lane == 0);
-    if (!p.grad) return;
+    if (work) {
+        const double lso = log(so), lsr = REF ? log(ss) : 0.0;
+        const double logp = known ? ((double)za - mo) - lso : (double)NAN;
+        const double kl = REF ? sd / so - (lso - lsr) : 0.0, H = lso - st / so;
+        // (a row without a finite logit: log 0 everywhere, and no distribution to have a gradient)
+        const RowResult<double> f = finish_row<double>(p, row, empty && known ? -INFINITY : logp, kl, H, empty && known, lane == 0);
+        if (STATS && lane == 0) sums.add(p, w, f.pg, f.kl, f.H, f.r);
+        if (g_row) {
 #pragma unroll
-    for (int k = 0; k < kNarrowPer; ++k) {
-        const int v = k * G + lane;
-        if (v >= p.A) break;
-        const double pv = e[k] / so, lp = ((double)z[k] - mo) - lso;
-        double b = f.base + (double)p.entropy_coef * lp;
-        if constexpr (REF) {
-            if (p.kl_coef != 0.f) b += (double)p.kl_coef * (lp - (((double)zr[k] - mr) - lsr));
+            for (int k = 0; k < kNarrowPer; ++k) {
+                const int v = k * G + lane;
+                if (v >= p.A) break;
+                const double pv = e[k] / so, lp = ((double)z[k] - mo) - lso;
+                double b = f.base + (double)p.entropy_coef * lp;
+                if constexpr (REF) {
+                    if (p.kl_coef != 0.f) b += (double)p.kl_coef * (lp - (((double)zr[k] - mr) - lsr));
+                }
+                double g = e[k] == 0.0 ? 0.0 : pv * b;
+                if (v == a) g += f.slope;
+                g_row[v] = from_float<T>(empty && known ? 0.f : (float)((double)w * g));
+            }
         }
-        double g = e[k] == 0.0 ? 0.0 : pv * b;
-        if (v == a) g += f.slope;
-        g_row[v] = from_float<T>(empty && known ? 0.f : (float)((double)w * g));
     }
+    if (STATS) write_stats(sums, stats);
 }
 
 // -------------------------------------------------------------------------------------------- long rows
@@ -368,6 +482,7 @@ template <typename T, bool REF>
 __global__ void __launch_bounds__(128, 4) loss_warp_kernel(const __grid_constant__ LossArgs p)
 {
     constexpr int V = Row<T>::kVec, NV = kWarpPieces;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (row >= p.rows) return;
@@ -491,6 +606,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
     const int share = (int)cg::this_cluster().num_blocks(), rank = (int)cg::this_cluster().block_rank();
     asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const long long row = (long long)(blockIdx.x / (unsigned)share);
     const float w = weight_of(p, row);
     const T *z_row = static_cast<const T *>(p.logits) + row * p.ld;
@@ -666,96 +782,24 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
         for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
 }
 
-// -------------------------------------------------------------------------------------- sums over rows
-constexpr int kStatsThreads = 1024, kStatsCluster = 8, kSums = 7;
-
-// One cluster (of one CTA or eight), double sums in a fixed order.
-__global__ void __launch_bounds__(kStatsThreads)
-loss_stats_kernel(const __grid_constant__ LossArgs p, float *__restrict__ stats)
+// ---------------------------------------------------------------------------------------------- launch
+template <typename T, bool REF, bool STATS>
+auto narrow_kernel(int g)
 {
-    namespace cg = cooperative_groups;
-    __shared__ double s_sum[kStatsThreads / 32][kSums];
-    __shared__ float s_max[kStatsThreads / 32];
-    __shared__ double c_sum[kStatsCluster][kSums];  // used in the first CTA
-    __shared__ float c_max[kStatsCluster];
-    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    double sum[kSums] = {};
-    float mx = -INFINITY;
-    const long long stride = (long long)gridDim.x * blockDim.x;
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < p.rows; i += stride) {
-        const double w = (double)weight_of(p, i);
-        const float2 t = __ldcg(reinterpret_cast<const float2 *>(p.terms + 2 * i));
-        const float kl = __ldcg(p.kl + i), H = __ldcg(p.entropy + i);
-        if (w == 0.0) continue;
-        const double pg = (double)t.x, r = fabs((double)t.y);
-        sum[0] += w * (pg + (p.kl_coef != 0.f ? (double)p.kl_coef * kl : 0.0) - (double)p.entropy_coef * H);
-        sum[1] += w * pg;
-        sum[2] += w * (double)kl;
-        sum[3] += w * (double)H;
-        sum[4] += signbit(t.y) ? w : 0.0;
-        sum[5] += w;
-        sum[6] += w * r;
-        mx = fmaxf(mx, kl);
-    }
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-#pragma unroll
-        for (int j = 0; j < kSums; ++j) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    }
-    if (lane == 0) {
-#pragma unroll
-        for (int j = 0; j < kSums; ++j) s_sum[warp][j] = sum[j];
-        s_max[warp] = mx;
-    }
-    __syncthreads();
-    asm volatile("barrier.cluster.wait;" ::: "memory");  // the first CTA has started
-    if (warp == 0) {
-#pragma unroll
-        for (int j = 0; j < kSums; ++j) sum[j] = lane < warps ? s_sum[lane][j] : 0.0;
-        mx = lane < warps ? s_max[lane] : -INFINITY;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-#pragma unroll
-            for (int j = 0; j < kSums; ++j) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        }
-        if (lane == 0) {
-            const unsigned rank = cg::this_cluster().block_rank();
-#pragma unroll
-            for (int j = 0; j < kSums; ++j) *cg::this_cluster().map_shared_rank(&c_sum[rank][j], 0) = sum[j];
-            *cg::this_cluster().map_shared_rank(&c_max[rank], 0) = mx;
-        }
-    }
-    cg::this_cluster().sync();
-    if (blockIdx.x == 0 && threadIdx.x < kSums) {
-        double v = 0.0;
-        for (unsigned i = 0; i < gridDim.x; ++i) v += c_sum[i][threadIdx.x];
-        const int j = (int)threadIdx.x;
-        stats[j < 6 ? j : 7] = (float)v;
-        if (j == 0) {
-            float most = -INFINITY;
-            for (unsigned i = 0; i < gridDim.x; ++i) most = fmaxf(most, c_max[i]);
-            stats[6] = most == -INFINITY ? 0.f : most;
-        }
-    }
+    return g == 1 ? loss_narrow_kernel<T, REF, 1, STATS> : g == 2 ? loss_narrow_kernel<T, REF, 2, STATS>
+         : g == 4 ? loss_narrow_kernel<T, REF, 4, STATS> : loss_narrow_kernel<T, REF, 8, STATS>;
 }
 
-// ---------------------------------------------------------------------------------------------- launch
+// `done`: the sums over rows have been taken too (rows that fit one CTA: a second launch costs some 3 us)
 template <typename T, bool REF>
-cudaError_t launch_narrow(const LossArgs &p, cudaStream_t st)
+cudaError_t launch_narrow(const LossArgs &p, float *stats, bool *done, cudaStream_t st)
 {
     int g = 1;
     while (g * kNarrowPer < p.A) g *= 2;
     const long long threads = (long long)p.rows * g;
-    const unsigned blocks = (unsigned)((threads + 127) / 128);
-    const auto kernel = g == 1   ? loss_narrow_kernel<T, REF, 1>
-                        : g == 2 ? loss_narrow_kernel<T, REF, 2>
-                        : g == 4 ? loss_narrow_kernel<T, REF, 4>
-                                 : loss_narrow_kernel<T, REF, 8>;
-    kernel<<<blocks, 128, 0, st>>>(p);
+    *done = threads <= 1024;
+    if (*done) narrow_kernel<T, REF, true>(g)<<<1, (unsigned)std::max<long long>(64, (threads + 31) / 32 * 32), 0, st>>>(p, stats);
+    else narrow_kernel<T, REF, false>(g)<<<(unsigned)((threads + 127) / 128), 128, 0, st>>>(p, nullptr);
     return cudaGetLastError();
 }
 
@@ -876,12 +920,14 @@ extern "C" accerl_status accerl_policy_loss(const accerl_policy_loss_args *a, vo
     ACCERL_CUDA_TRY(cudaGetDevice(&device));
     ACCERL_CUDA_TRY(cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device));
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    bool done = false;
     ACCERL_CUDA_TRY(with_dtype(a->dtype, [&](auto v) {
         using T = decltype(v);
-        if (p.A <= kNarrow) return p.ref ? launch_narrow<T, true>(p, st) : launch_narrow<T, false>(p, st);
+        if (p.A <= kNarrow) return p.ref ? launch_narrow<T, true>(p, a->stats, &done, st) : launch_narrow<T, false>(p, a->stats, &done, st);
         return p.ref ? launch_rows<T, true>(p, sm_count, st) : launch_rows<T, false>(p, sm_count, st);
     }));
-    const unsigned ctas = p.rows <= 8192 ? 1 : kStatsCluster;
+    if (done) return ACCERL_OK;
+    const unsigned ctas = p.rows <= 2048 ? 1 : kStatsCluster;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -891,7 +937,9 @@ extern "C" accerl_status accerl_policy_loss(const accerl_policy_loss_args *a, vo
     cfg.blockDim = dim3(p.rows < kStatsThreads ? (unsigned)(p.rows + 31) / 32 * 32 : kStatsThreads);
     cfg.stream = st;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 2;
     ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, loss_stats_kernel, p, a->stats));
     return ACCERL_OK;
 }
