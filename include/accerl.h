@@ -552,7 +552,7 @@ typedef struct {
     const float *w_scale;  /* [n] */
     const float *bias;     /* [n] or NULL */
     void *y;               /* [tokens][n] */
-    void *workspace;       /* accerl_linear_i8_workspace bytes, 256-byte aligned; ACCERL_I8: not used */
+    void *workspace;       /* accerl_linear_i8_workspace bytes, 256-byte aligned; NULL where that is 0 */
     int64_t ld_x, ld_w, ld_y, workspace_bytes;
     int32_t tokens, n, k;  /* k at most 131072 */
     int32_t x_dtype, y_dtype, relu;
@@ -562,7 +562,7 @@ typedef struct {
 int64_t accerl_linear_i8_workspace(int32_t tokens, int32_t k, int32_t x_dtype);
 
 /*
- * Asynchronous on `cuda_stream`, one launch for ACCERL_I8, else two.  The workspace is the call's until the stream has
+ * Asynchronous on `cuda_stream`, one launch for ACCERL_I8 or one token, else two.  The workspace is the call's until the stream has
  * passed it: calls that may run at the same time (two streams, two captured graphs) need one each.
  * Errors: INVALID_ARG, UNSUPPORTED (no tensor-memory device), CUDA; a bounded wait on the device that gave up is
  * reported by accerl_device_check.

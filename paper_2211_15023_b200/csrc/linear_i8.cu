@@ -5,14 +5,13 @@
 // to fp32; it is computed as x * (1 / s) and the division is done only where that product lies so near to a tie that
 // its error (below 127 * 2^-22) could matter.
 //
-// linear_few_kernel: the product.  Channels are the M of the tensor-core instructions and tokens their N, so that one
-// token needs no more than 16 columns and the weights, which bound the few-token case, stream through shared memory
+// linear_token_kernel: the product for one token.  linear_few_kernel: for some.  Channels are the M of the tensor-core instructions and tokens their N, so that
+// few tokens need few columns and the weights, which bound the few-token case, stream through shared memory
 // once.  K is split over the CTAs of a cluster until the chip is covered; their int32 partial sums are added
-// through distributed shared memory (integers: any order gives the same bits).
+// through distributed shared memory (integers: any order gives the same bits).  linear_pair_kernel: for many.
 #include <cooperative_groups.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "learn.cuh"
 #include "tc_image.cuh"
@@ -169,8 +168,6 @@ struct LinearArgs {
     int tokens, n, k, y_dtype, relu;
     int chunks;  // of 128 bytes along K
     int stages;
-    const void *x;  // tokens that the product quantises itself
-    long long ld_x;
 };
 
 __device__ __forceinline__ void store_y(const LinearArgs &p, int t, int n, float v)
@@ -188,16 +185,121 @@ __device__ __forceinline__ float at_least(float v, float floor)  // (a NaN stays
     return m;
 }
 
-constexpr int kFused = 4;  // up to so many tokens are quantised by the product itself
+// One token, of at most 64 KB once quantised: a warp takes a channel at a time, whose weights it has asked for before the CTA
+// quantises the token (every CTA all of it, from L2) into shared memory; four products an instruction.  There is one
+// product a byte of weights, and what counts is latency: no second launch, no tensor memory to set up, no cluster to wait
+// for.  4096 x 4096 in a captured graph 5.6 us, with the kernels below 8.6, and 14 us against 8.7 with four tokens done
+// this way: from two tokens on the tensor cores take them.
+constexpr int kTokenThreads = 256, kTokenAhead = 8;  // pieces of 16 bytes of a channel in flight, a lane
+
+struct TokenArgs {
+    const void *x;
+    const float *x_scale;
+    const int8_t *w;
+    long long ld_w;
+    int room;  // of the token in shared memory: k rounded up to 512
+};
+
+template <typename XT>
+__global__ void __launch_bounds__(kTokenThreads, 4)
+linear_token_kernel(const __grid_constant__ LinearArgs p, const __grid_constant__ TokenArgs a)
+{
+    extern __shared__ __align__(16) uint8_t s_x[];
+    __shared__ uint32_t s_top[kTokenThreads / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kTokenThreads / 32;
+    const int channels = (int)gridDim.x * warps;
+    int n = (int)blockIdx.x * warps + warp;
+    uint4 w[kTokenAhead];
+    auto ask = [&](int channel, int k0) {  // the pieces from k0 on
+        const int8_t *row = a.w + (long long)channel * a.ld_w;
+#pragma unroll
+        for (int i = 0; i < kTokenAhead; ++i) {
+            const int k = k0 + 512 * i + 16 * lane;
+            w[i] = channel < p.n && k < p.k ? __ldcs(reinterpret_cast<const uint4 *>(row + k)) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    ask(n, 0);
+    uint32_t *out = reinterpret_cast<uint32_t *>(s_x);
+    float scale;
+    if constexpr (sizeof(XT) == 1) {
+        const int8_t *x = static_cast<const int8_t *>(a.x);
+        for (int i = threadIdx.x; i < a.room / 4; i += kTokenThreads) {
+            uint32_t v = 0;
+            if (4 * i + 3 < p.k) v = reinterpret_cast<const uint32_t *>(x)[i];
+            else
+                for (int j = 0; j < 4; ++j)
+                    if (4 * i + j < p.k) v |= (uint32_t)(uint8_t)x[4 * i + j] << 8 * j;
+            out[i] = v;
+        }
+        scale = a.x_scale[0];
+    } else {
+        constexpr int V = Row<XT>::kVec;
+        const XT *x = static_cast<const XT *>(a.x);
+        uint32_t top = 0;
+#pragma unroll 4
+        for (int k = (int)threadIdx.x * V; k < p.k; k += kTokenThreads * V) {
+            float v[V];
+            unpack<XT>(load_piece<XT>(x, k, p.k, 0.f), v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) top = max(top, magnitude(v[j]));
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) s_top[warp] = top;
+        __syncthreads();
+        top = __reduce_max_sync(0xffffffffu, s_top[lane % warps]);
+        const Scale sc(top);
+        scale = sc.s;
+#pragma unroll 2
+        for (int k = (int)threadIdx.x * V; k < a.room; k += kTokenThreads * V) {
+            float v[V];
+            unpack<XT>(load_piece<XT>(x, k, p.k, 0.f), v);
+#pragma unroll
+            for (int j = 0; j < V / 4; ++j) out[k / 4 + j] = sc.zero ? 0u : quantised4(v + 4 * j, sc.s, sc.inv, sc.exact);
+        }
+    }
+    __syncthreads();
+    for (; n < p.n; n += channels) {
+        const float ws = p.w_scale[n], bias = p.bias ? p.bias[n] : 0.f;
+        int acc = 0;
+        for (int k0 = 0; k0 < p.k; k0 += 512 * kTokenAhead) {
+            if (k0) ask(n, k0);
+#pragma unroll
+            for (int i = 0; i < kTokenAhead; ++i) {
+                const int k = k0 + 512 * i;
+                if (k >= p.k) break;
+                const uint4 v = *reinterpret_cast<const uint4 *>(s_x + k + 16 * lane);
+                acc = __dp4a((int)w[i].x, (int)v.x, acc);
+                acc = __dp4a((int)w[i].y, (int)v.y, acc);
+                acc = __dp4a((int)w[i].z, (int)v.z, acc);
+                acc = __dp4a((int)w[i].w, (int)v.w, acc);
+            }
+        }
+        ask(n + channels, 0);
+        const int sum = __reduce_add_sync(0xffffffffu, acc);
+        if (lane == 0) store_y(p, 0, n, at_least(fmaf((float)sum, scale * ws, bias), p.relu ? 0.f : -INFINITY));
+    }
+}
+
+// as many CTAs as the chip holds at most: 4 an SM, 3 beside long tokens
+accerl_status launch_token(const accerl_linear_i8_args *a, const LinearArgs &p, int sm_count, cudaStream_t st)
+{
+    const TokenArgs t{a->x, a->x_scale, a->w, a->ld_w, (a->k + 511) / 512 * 512};
+    const int warps = kTokenThreads / 32, resident = sm_count * std::min(4, 220 * 1024 / (t.room + 1024));
+    const auto kernel = a->x_dtype == ACCERL_I8     ? linear_token_kernel<int8_t>
+                        : a->x_dtype == ACCERL_F32  ? linear_token_kernel<float>
+                        : a->x_dtype == ACCERL_BF16 ? linear_token_kernel<__nv_bfloat16>
+                                                    : linear_token_kernel<__half>;
+    ACCERL_CUDA_TRY(allow_smem((const void *)kernel, t.room));
+    kernel<<<(unsigned)std::min((a->n + warps - 1) / warps, resident), kTokenThreads, (size_t)t.room, st>>>(p, t);
+    ACCERL_CUDA_TRY(cudaGetLastError());
+    return ACCERL_OK;
+}
+
 constexpr int kFewThreads = 192, kMaxStages = 8, kMaxShare = 8;
 
 // One tile of 128 channels x NT tokens; the CTAs of a cluster share its K.
 // Warps 0..3 drain the accumulator (and finish), warp 4 loads, warp 5 issues the tensor-core instructions.
-//
-// XT: the type of up to kFused tokens that the kernel quantises itself (void: they come quantised): warps 0..3 find the
-// tokens' maxima and write this CTA's part of K as the operand, while the weights are on their way.  Every CTA reads the
-// tokens whole (from L2), which a launch less repays for a few of them only.
-template <int NT, typename XT>
+template <int NT>
 __global__ void __launch_bounds__(kFewThreads)
 linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                   const __grid_constant__ LinearArgs p)
@@ -208,15 +310,10 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         uint32_t tmem;
         int abort_flag;
     } bars;
-    __shared__ uint32_t s_top[kFused][4];
-    __shared__ float s_scale[kFused];
-    __shared__ uint64_t s_ready;
     namespace cg = cooperative_groups;
-    constexpr bool FUSED = !std::is_void<XT>::value;
-    constexpr int kStage = 128 * 128 + (FUSED ? 0 : NT * 128), kCols = NT < 32 ? 32 : NT;
+    constexpr int kStage = 128 * 128 + NT * 128, kCols = NT < 32 ? 32 : NT;
     uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t base = smem_u32(smem), full0 = smem_u32(&bars.full[0]), empty0 = smem_u32(&bars.empty[0]);
-    const uint32_t tokens0 = base + p.stages * kStage;  // FUSED: [chunk][NT][128], swizzled
     const int warp = threadIdx.x >> 5;
     const int share = (int)cg::this_cluster().num_blocks(), rank = (int)cg::this_cluster().block_rank();
     const int n0 = (int)(blockIdx.x / (unsigned)share) * 128, t0 = (int)blockIdx.y * NT;
@@ -228,7 +325,6 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
             mbar_init(empty0 + 8 * s, 1);
         }
         mbar_init(smem_u32(&bars.acc), 1);
-        mbar_init(smem_u32(&s_ready), 4);
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
@@ -264,20 +360,18 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                     mbar_expect_tx(full0 + 8 * s, kStage);
                     tma_load_2d(at, &map_w, (c0 + i) * 128, n0, full0 + 8 * s);
                 }
-                if (!FUSED) tma_load_2d(at + 128 * 128, &map_x, (c0 + i) * 128, t0, full0 + 8 * s);
+                tma_load_2d(at + 128 * 128, &map_x, (c0 + i) * 128, t0, full0 + 8 * s);
             }
             __syncwarp();
         }
     } else if (warp == 5) {
         bool ok = true;
-        if (FUSED) ok = mbar_wait(smem_u32(&s_ready), 0, abort_flag, &g_status, 32);
         for (int i = 0; i < c1 - c0 && ok; ++i) {
             const int s = i % p.stages;
             ok = mbar_wait(full0 + 8 * s, (uint32_t)((i / p.stages) & 1), abort_flag, &g_status, 8);
             fence_after();
             if (ok && elect_one()) {
-                const uint64_t a = make_desc(base + s * kStage, 128),
-                               b = make_desc(FUSED ? tokens0 + i * (NT * 128) : base + s * kStage + 128 * 128, 128);
+                const uint64_t a = make_desc(base + s * kStage, 128), b = make_desc(base + s * kStage + 128 * 128, 128);
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks) mma_i8(tmem, a + 2 * ks, b + 2 * ks, idesc_for(NT), (uint32_t)(i | ks));
                 mma_commit(empty0 + 8 * s);
@@ -286,43 +380,6 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
             __syncwarp();
         }
     } else {
-        if constexpr (FUSED) {
-            constexpr int V = Row<XT>::kVec;
-            const int lane = threadIdx.x & 31;
-            for (int t = 0; t < p.tokens; ++t) {
-                const XT *x = static_cast<const XT *>(p.x) + t * p.ld_x;
-                uint32_t top = 0;
-#pragma unroll 4
-                for (int k = (int)threadIdx.x * V; k < p.k; k += 128 * V) {
-                    float v[V];
-                    unpack<XT>(load_piece<XT>(x, k, p.k, 0.f), v);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) top = max(top, magnitude(v[j]));
-                }
-                top = __reduce_max_sync(0xffffffffu, top);
-                if (lane == 0) s_top[t][warp] = top;
-            }
-            asm volatile("bar.sync 1, 128;" ::: "memory");
-            for (int i = threadIdx.x; i < p.tokens * (c1 - c0) * 8; i += 128) {  // sixteen values
-                const int piece = i % 8, c = i / 8 % (c1 - c0), t = i / 8 / (c1 - c0);
-                const Scale sc(max(max(s_top[t][0], s_top[t][1]), max(s_top[t][2], s_top[t][3])));
-                if (piece == 0 && c == 0) s_scale[t] = sc.s;
-                const XT *x = static_cast<const XT *>(p.x) + t * p.ld_x;
-                uint32_t w[4];
-#pragma unroll
-                for (int h = 0; h < 16 / V; ++h) {
-                    float v[V];
-                    unpack<XT>(load_piece<XT>(x, (c0 + c) * 128 + piece * 16 + h * V, p.k, 0.f), v);
-#pragma unroll
-                    for (int j = 0; j < V / 4; ++j) w[h * (V / 4) + j] = sc.zero ? 0u : quantised4(v + 4 * j, sc.s, sc.inv, sc.exact);
-                }
-                sts16(tokens0 + c * (NT * 128) + t * 128 + ((piece ^ (t & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
-            }
-            fence_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_ready));
-            asm volatile("bar.sync 1, 128;" ::: "memory");  // (the scales)
-        }
         mbar_wait(smem_u32(&bars.acc), 0, abort_flag, &g_status, 16);
         fence_after();
     }
@@ -336,7 +393,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the tokens' scales are the quantiser's
     auto finish = [&](int t, int acc) {
         if (!mine || t >= p.tokens) return;
-        store_y(p, t, n, at_least(fmaf((float)acc, (FUSED ? s_scale[t % kFused] : p.x_scale[t]) * ws, bias), p.relu ? 0.f : -INFINITY));
+        store_y(p, t, n, at_least(fmaf((float)acc, p.x_scale[t] * ws, bias), p.relu ? 0.f : -INFINITY));
     };
     int *part = reinterpret_cast<int *>(smem);  // [NT][128]: every operand has been read
     if (warp < 4) {
@@ -372,7 +429,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                     acc[3] += x[c].w;
                 }
             const int t = t0 + i / 32, n4 = n0 + i % 32 * 4;
-            const float xs = FUSED ? s_scale[t % kFused] : p.x_scale[t], floor = p.relu ? 0.f : -INFINITY;
+            const float xs = p.x_scale[t], floor = p.relu ? 0.f : -INFINITY;
 #pragma unroll
             for (int l = 0; l < 4; ++l)
                 if (n4 + l < p.n)
@@ -387,22 +444,15 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kCols) : "memory");
 }
 
-int few_share(const LinearArgs &p, int tiles, int sm_count)
-{
-    int share = 1;
-    while (share < kMaxShare && (long long)tiles * share < sm_count && p.chunks >= 4 * share) share *= 2;
-    return share;
-}
-
-template <int NT, typename XT>
+template <int NT>
 accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArgs &p, int sm_count, bool after_quant, cudaStream_t st)
 {
-    constexpr bool FUSED = !std::is_void<XT>::value;
-    constexpr int kStage = 128 * 128 + (FUSED ? 0 : NT * 128);
-    const int tiles = (p.n + 127) / 128, token_tiles = (p.tokens + NT - 1) / NT, share = few_share(p, tiles * token_tiles, sm_count);
-    const size_t own = FUSED ? (size_t)((p.chunks + share - 1) / share) * NT * 128 : 0;  // the tokens' part
-    p.stages = std::min<int>(kMaxStages, (int)((110 * 1024 - own) / kStage));
-    const size_t smem = 1024 + (size_t)p.stages * kStage + own;
+    constexpr int kStage = 128 * 128 + NT * 128;
+    p.stages = std::min(kMaxStages, 110 * 1024 / kStage);
+    const size_t smem = 1024 + (size_t)p.stages * kStage;
+    const int tiles = (p.n + 127) / 128, token_tiles = (p.tokens + NT - 1) / NT;
+    int share = 1;
+    while (share < kMaxShare && (long long)tiles * token_tiles * share < sm_count && p.chunks >= 4 * share) share *= 2;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -416,8 +466,8 @@ accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArg
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = after_quant ? 2 : 1;
-    ACCERL_CUDA_TRY(allow_smem((const void *)linear_few_kernel<NT, XT>, smem));
-    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_few_kernel<NT, XT>, mw, mx, p));
+    ACCERL_CUDA_TRY(allow_smem((const void *)linear_few_kernel<NT>, smem));
+    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_few_kernel<NT>, mw, mx, p));
     return ACCERL_OK;
 }
 
@@ -648,11 +698,14 @@ extern "C" accerl_status accerl_quant_rows(const void *x, int64_t ld_x, int32_t 
     return ACCERL_OK;
 }
 
+// one token that linear_token_kernel's shared memory holds
+static bool one_token(int32_t tokens, int32_t k) { return tokens == 1 && k <= 64 * 1024; }
+
 static int64_t quantised_bytes(int64_t tokens, int64_t k) { return (tokens * ((k + 15) / 16 * 16) + 255) / 256 * 256; }
 
 extern "C" int64_t accerl_linear_i8_workspace(int32_t tokens, int32_t k, int32_t x_dtype)
 {
-    if (x_dtype == ACCERL_I8 || tokens < 1 || k < 1) return 0;
+    if (x_dtype == ACCERL_I8 || tokens < 1 || k < 1 || one_token(tokens, k)) return 0;
     return quantised_bytes(tokens, k) + (4LL * tokens + 255) / 256 * 256;
 }
 
@@ -694,6 +747,8 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
     ACCERL_CUDA_TRY(cudaGetDevice(&device));
     ACCERL_CUDA_TRY(cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device));
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    LinearArgs p{a->x_scale, a->w_scale, a->bias, a->y, a->ld_y, a->tokens, a->n, a->k, a->y_dtype, a->relu != 0, (a->k + 127) / 128, 0};
+    if (one_token(a->tokens, a->k)) return launch_token(a, p, sm_count, st);
     const void *xq = a->x;
     const float *xs = a->x_scale;
     int64_t ld_xq = a->ld_x;
@@ -709,19 +764,16 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
     accerl_status s = tc_make_map(&mw, a->w, a->n, a->k, a->ld_w, 128, 128);
     if (s == ACCERL_OK) s = tc_make_map(&mx, xq, a->tokens, a->k, ld_xq, nt, 128);
     if (s != ACCERL_OK) return s;
-    LinearArgs p{xs, a->w_scale, a->bias, a->y, a->ld_y, a->tokens, a->n, a->k, a->y_dtype, a->relu != 0, (a->k + 127) / 128, 0, a->x, a->ld_x};
-    // (the tokens' part of K in shared memory: 32 KB at most)
-    if (!given && a->tokens <= kFused && p.chunks <= 16 * few_share(p, (a->n + 127) / 128, sm_count))
-        return with_dtype(a->x_dtype, [&](auto v) { return launch_few<16, decltype(v)>(mw, mx, p, sm_count, false, st); });
     if (!given) {
         const QuantArgs q{a->x, static_cast<int8_t *>(a->workspace), const_cast<float *>(xs), a->ld_x, ld_xq, a->tokens, a->k};
         ACCERL_CUDA_TRY(launch_quant(q, a->x_dtype, sm_count, st));
     }
+    p.x_scale = xs;
     if (pair) return launch_pair(mw, mx, p, sm_count, !given, st);
-    return nt == 16   ? launch_few<16, void>(mw, mx, p, sm_count, !given, st)
-           : nt == 32 ? launch_few<32, void>(mw, mx, p, sm_count, !given, st)
-           : nt == 64 ? launch_few<64, void>(mw, mx, p, sm_count, !given, st)
-                      : launch_few<128, void>(mw, mx, p, sm_count, !given, st);
+    return nt == 16   ? launch_few<16>(mw, mx, p, sm_count, !given, st)
+           : nt == 32 ? launch_few<32>(mw, mx, p, sm_count, !given, st)
+           : nt == 64 ? launch_few<64>(mw, mx, p, sm_count, !given, st)
+                      : launch_few<128>(mw, mx, p, sm_count, !given, st);
 }
 
 extern "C" accerl_status accerl_device_check(void)

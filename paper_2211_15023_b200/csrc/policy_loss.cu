@@ -11,6 +11,7 @@
 // single one of 128 001 logits takes no longer than a short one).  Logits are read from memory once and the gradient
 // is written once; the kernel is bound by HBM.
 #include <cooperative_groups.h>
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -359,10 +360,11 @@ __device__ __forceinline__ uint32_t min_words(uint32_t a, uint32_t b)
 // What -inf is taken for (finite, so that its probability of 0 times its logarithm is 0), as a word of one or two
 // elements; a row or part of a row with nothing above it is looked at again, see `low_part`.
 template <typename T>
+__device__ __forceinline__ constexpr float low_value() { return std::is_same<T, __half>::value ? -65504.f : -1e30f; }
+template <typename T>
 __device__ __forceinline__ uint32_t low_word()
 {
-    const float v[2] = {sizeof(T) == 2 && std::is_same<T, __half>::value ? -65504.f : -1e30f,
-                        sizeof(T) == 2 && std::is_same<T, __half>::value ? -65504.f : -1e30f};
+    const float v[2] = {low_value<T>(), low_value<T>()};
     return pack_word(v, (const T *)nullptr);
 }
 template <typename T>
@@ -502,7 +504,7 @@ __global__ void __launch_bounds__(128, 4) loss_warp_kernel(const __grid_constant
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         raw[i] = load_piece<T, true>(z_row, first + i * step, p.A, -INFINITY);
-        if constexpr (REF) raw_r[i] = load_piece<T>(r_row, first + i * step, p.A, -INFINITY);
+        if constexpr (REF) raw_r[i] = load_piece<T>(r_row, first + i * step, p.A, low_value<T>());
         else raw_r[i] = raw[i];
     }
     const long long wanted = action_of(p, row);
@@ -644,11 +646,11 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
         const int j = threadIdx.x == 0 ? 0 : n - 1;
         if (n > 0 && (j < whole0 || j >= whole1)) {
             z_s[j] = load_piece<T>(z_row, first + j * V, p.A, -INFINITY);
-            if (REF && alike) r_s[j] = load_piece<T>(r_row, first + j * V, p.A, -INFINITY);
+            if (REF && alike) r_s[j] = load_piece<T>(r_row, first + j * V, p.A, low_value<T>());
         }
     }
     if (REF && !alike)
-        for (int j = threadIdx.x; j < n; j += blockDim.x) r_s[j] = load_piece<T>(r_row, first + j * V, p.A, -INFINITY);
+        for (int j = threadIdx.x; j < n; j += blockDim.x) r_s[j] = load_piece<T>(r_row, first + j * V, p.A, low_value<T>());
     const long long wanted = action_of(p, row);
     const int a = wanted >= 0 && wanted < p.A ? (int)wanted : -1;
     const float za = a >= 0 ? to_float(z_row[a]) : NAN;  // (`grad` may be `logits`: read before the barriers below)
@@ -782,6 +784,270 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
         for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
 }
 
+// ------------------------------------------------------------------------------------- many very long rows
+// A CTA per row, persistent, the row streaming through a ring in shared memory twice: for the sums, and, backwards, for the
+// gradient.  The second time it comes from L2, which holds the rows of all CTAs (the launch sees to that).  Against
+// the kernel above a row's end (barriers, one warp's arithmetic: some 2 us in which an SM does little else) comes once for
+// a whole row instead of once for an eighth of one, and the loads of what follows go on meanwhile: 606 -> 332 us for
+// 2048 rows of 128001 with a reference.  Every thread keeps a maximum of its own and rebases its sums when it rises.
+constexpr int kStreamThreads = 512, kStreamBytes = 16 * kStreamThreads;  // of an array, a stage
+constexpr int kStreamSmem = 12 * 2 * kStreamBytes;
+
+template <typename T, bool REF>
+__global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(const __grid_constant__ LossArgs p)
+{
+    constexpr int V = Row<T>::kVec, kStages = REF ? 12 : 24;
+    extern __shared__ __align__(128) uint4 s_piece[];  // [kStages][REF ? 2 : 1][kStreamThreads]
+    __shared__ uint64_t s_full[kStages], s_empty[kStages];
+    __shared__ Partial s_part[kStreamThreads / 32];
+    __shared__ RowCoef s_row;
+    __shared__ int s_holes, s_abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_empty[i]), kStreamThreads / 32);
+        }
+        s_abort = s_holes = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    // a row's whole pieces [w0, w1) and the chunks of them that fill a stage
+    auto whole = [&](const T *z_row, int *phase, int *w0, int *w1) {
+        *phase = phase_of(z_row);
+        const int pieces = (*phase + p.A + V - 1) / V;
+        *w0 = *phase > 0;
+        *w1 = pieces * V - *phase > p.A ? pieces - 1 : pieces;
+        return (*w1 - *w0 + kStreamThreads - 1) / kStreamThreads;
+    };
+    int slot = 0, phase, w0, w1;
+    uint32_t turn = 0;
+    auto next = [&] {
+        if (++slot == kStages) {
+            slot = 0;
+            turn ^= 1;
+        }
+    };
+    if (warp == kStreamThreads / 32) {
+        // ------------------------------------------------------------------------------------- loads
+        for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+            if (weight_of(p, row) == 0.f) continue;
+            const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = REF ? static_cast<const T *>(p.ref) + row * p.ld_ref : z_row;
+            const int chunks = whole(z_row, &phase, &w0, &w1);
+            for (int i = 0; i < (p.grad ? 2 : 1) * chunks; ++i) {
+                const int c = i < chunks ? i : 2 * chunks - 1 - i, j = w0 + c * kStreamThreads;
+                if (!mbar_wait(smem_u32(&s_empty[slot]), turn ^ 1, &s_abort, &g_status, 2)) break;
+                if (elect_one()) {
+                    const uint32_t bytes = 16u * (uint32_t)min(kStreamThreads, w1 - j), at = smem_u32(s_piece + slot * (REF ? 2 : 1) * kStreamThreads);
+                    mbar_expect_tx(smem_u32(&s_full[slot]), (REF ? 2 : 1) * bytes);
+                    bulk_load(at, z_row + j * V - phase, bytes, smem_u32(&s_full[slot]));
+                    if (REF) bulk_load(at + kStreamBytes, r_row + j * V - phase, bytes, smem_u32(&s_full[slot]));
+                }
+                __syncwarp();
+                next();
+            }
+        }
+    } else {
+        auto all = [] { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+        const uint32_t low_w = low_word<T>();
+        float low[2];
+        unpack_word(low_w, low, (const T *)nullptr);
+        for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+            const float w = weight_of(p, row);
+            const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = REF ? static_cast<const T *>(p.ref) + row * p.ld_ref : z_row;
+            T *g_row = p.grad ? static_cast<T *>(p.grad) + row * p.ld_grad : nullptr;
+            const int chunks = whole(z_row, &phase, &w0, &w1);
+            if (w == 0.f) {
+                if (threadIdx.x == 0) skip_row(p, row);
+                const float zero[V] = {};
+                if (g_row)
+                    for (int v = (int)threadIdx.x * V - phase; v < p.A; v += kStreamThreads * V) store_piece<T>(g_row, v, p.A, zero);
+                continue;
+            }
+            // the pieces at the row's ends that are not whole: the first thread's and the second's
+            const int ragged = threadIdx.x == 0 && w0 > 0 ? -phase : threadIdx.x == 1 && w1 * V - phase < p.A ? w1 * V - phase : INT_MIN;
+            const long long wanted = action_of(p, row);
+            const int a = wanted >= 0 && wanted < p.A ? (int)wanted : -1;
+            const float za = a >= 0 ? to_float(z_row[a]) : NAN;
+            Partial s;
+            float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f, c = low[0], cr = low[0];
+            bool holes = false;  // -inf among the reference's logits
+            // what a thread's sums are relative to: its maximum, or 0 as long as it has met nothing above the low value
+            auto from_base = [&](float most) { return most <= low[0] ? 0.f : most; };
+            auto take = [&](uint4 raw, uint4 raw_r) {
+                uint32_t m = low_w, mr = low_w, least = low_w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    words(raw)[i] = max_words<T>(words(raw)[i], low_w);
+                    m = max_words<T>(m, words(raw)[i]);
+                    if constexpr (REF) {
+                        least = min_words<T>(least, words(raw_r)[i]);
+                        words(raw_r)[i] = max_words<T>(words(raw_r)[i], low_w);
+                        mr = max_words<T>(mr, words(raw_r)[i]);
+                    }
+                }
+                const float top = word_max<T>(m);
+                if (top > c) {
+                    const float d = so != 0.f ? (c - top) * kLog2e : 0.f, f = exp2_fast(d);
+                    st = f * (st + d * so);
+                    sd = f * (sd + d * so);
+                    so *= f;
+                    c = top;
+                }
+                if constexpr (REF) {
+                    holes |= word_min<T>(least) == -INFINITY;
+                    const float top_r = word_max<T>(mr);
+                    if (top_r > cr) {
+                        sd -= (from_base(cr) - top_r) * kLog2e * so;
+                        ss *= exp2_fast(ss != 0.f ? (cr - top_r) * kLog2e : 0.f);
+                        cr = top_r;
+                    }
+                }
+                add_sums<T, REF>(raw, raw_r, -from_base(c) * kLog2e, -from_base(cr) * kLog2e, so, st, ss, sd);
+            };
+            if (ragged != INT_MIN)
+                take(load_piece<T>(z_row, ragged, p.A, -INFINITY), REF ? load_piece<T>(r_row, ragged, p.A, low[0]) : make_uint4(0, 0, 0, 0));
+            for (int i = 0; i < chunks; ++i) {
+                const int j = w0 + i * kStreamThreads + (int)threadIdx.x;
+                mbar_wait(smem_u32(&s_full[slot]), turn, &s_abort, &g_status, 1);
+                const uint4 *at = s_piece + slot * (REF ? 2 : 1) * kStreamThreads + threadIdx.x;
+                if (j < w1) take(at[0], REF ? at[kStreamThreads] : at[0]);
+                // (always so; it waits for the values to be in every lane's registers, not merely asked for)
+                if (__all_sync(0xffffffffu, c >= low[0] && cr >= low[0]) && lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
+                next();
+            }
+            // a warp's sums, relative to its maxima
+            s.c = c;
+            s.cr = cr;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                s.c = max_nan(s.c, __shfl_xor_sync(0xffffffffu, s.c, o));
+                s.cr = max_nan(s.cr, __shfl_xor_sync(0xffffffffu, s.cr, o));
+            }
+            {
+                const float d = so != 0.f ? (c - s.c) * kLog2e : 0.f, dr = (from_base(cr) - from_base(s.cr)) * kLog2e, f = exp2f(d);
+                st = f != 0.f ? f * (st + d * so) : 0.f;
+                sd = f != 0.f ? f * (sd + (d - dr) * so) : 0.f;
+                so *= f;
+                ss *= exp2f(ss != 0.f ? dr : 0.f);
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                so += __shfl_xor_sync(0xffffffffu, so, o);
+                st += __shfl_xor_sync(0xffffffffu, st, o);
+                if (REF) {
+                    ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                    sd += __shfl_xor_sync(0xffffffffu, sd, o);
+                }
+            }
+            s.so = so, s.st = st, s.ss = ss, s.sd = sd;
+            if (lane == 0) s_part[warp] = s;
+            if (holes) s_holes = 1;
+            all();
+            float C = s_part[lane & 15].c, CR = s_part[lane & 15].cr;
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) {
+                C = max_nan(C, __shfl_xor_sync(0xffffffffu, C, o));
+                CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
+            }
+            // Nothing above the low value in one of the rows, or no probability where the policy may have one: the row is
+            // done from memory, value by value (masks of the type's lowest value only, or none left at all).
+            const bool odd = C <= low[0] || (REF && (CR <= low[0] || s_holes));
+            if (odd) {
+                C = CR = -INFINITY;
+                for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
+                    C = max_nan(C, to_float(z_row[v]));
+                    if (REF) CR = max_nan(CR, to_float(r_row[v]));
+                }
+                all();  // (the parts have been read)
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    C = max_nan(C, __shfl_xor_sync(0xffffffffu, C, o));
+                    CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
+                }
+                if (lane == 0) s_part[warp].c = C, s_part[warp].cr = CR;
+                all();
+                for (int i = 0; i < kStreamThreads / 32; ++i) {
+                    C = max_nan(C, s_part[i].c);
+                    CR = max_nan(CR, s_part[i].cr);
+                }
+                all();
+                double v4[4] = {};
+                for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
+                    const float z = to_float(z_row[v]), t = z == -INFINITY ? -1e30f : (z - C) * kLog2e, e = exp2_fast(t);
+                    v4[0] += e;
+                    if (e != 0.f) v4[1] += (double)e * t;
+                    if (REF) {
+                        const float zr = to_float(r_row[v]), tr = zr == -INFINITY ? -INFINITY : (zr - CR) * kLog2e;
+                        v4[2] += exp2_fast(tr);
+                        if (e != 0.f) v4[3] += (double)e * ((double)t - (double)tr);
+                    }
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v4[i] += __shfl_xor_sync(0xffffffffu, v4[i], o);
+                s.c = C, s.cr = CR, s.so = v4[0], s.st = v4[1], s.ss = v4[2], s.sd = v4[3];
+                if (C == -INFINITY) s.so = s.st = s.sd = 0.0;
+                if (lane == 0) s_part[warp] = s;
+                all();
+            }
+            if (warp == 0) {
+                Partial b = s_part[lane & 15];
+                const float d = b.so != 0.0 ? (b.c - C) * kLog2e : 0.f, dr = b.ss != 0.0 ? (b.cr - CR) * kLog2e : 0.f;
+                const double f = lane < 16 ? (double)exp2f(d) : 0.0, df = (double)d, dd = (double)(d - dr);
+                double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, lane < 16 ? (double)exp2f(dr) * b.ss : 0.0,
+                               f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+                const RowCoef f0 = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], lane == 0);
+                if (lane == 0) {
+                    s_row = f0;
+                    if (s_holes) s_holes = 0;  // (then every warp has come past two barriers since it looked)
+                }
+            }
+            all();
+            if (!g_row) continue;
+            const RowCoef f = s_row;
+            const float sh = shift_of(0.f, f.c), shr = shift_of(0.f, f.cr);
+            if (!odd && ragged != INT_MIN) {
+                uint4 raw = load_piece<T>(z_row, ragged, p.A, low[0]), raw_r = REF ? load_piece<T>(r_row, ragged, p.A, low[0]) : raw;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) words(raw)[i] = max_words<T>(words(raw)[i], low_w);
+                put_gradient<T, REF>(p, g_row, ragged, a, raw, raw_r, f, sh, shr);
+            }
+            for (int i = chunks - 1; i >= 0; --i) {
+                const int j = w0 + i * kStreamThreads + (int)threadIdx.x;
+                mbar_wait(smem_u32(&s_full[slot]), turn, &s_abort, &g_status, 1);
+                const uint4 *at = s_piece + slot * (REF ? 2 : 1) * kStreamThreads + threadIdx.x;
+                if (!odd && j < w1) {
+                    uint4 raw = at[0], raw_r = REF ? at[kStreamThreads] : at[0];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) words(raw)[k] = max_words<T>(words(raw)[k], low_w);
+                    put_gradient<T, REF>(p, g_row, j * V - phase, a, raw, raw_r, f, sh, shr);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
+                next();
+            }
+            if (odd) {
+                for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
+                    const float z = to_float(z_row[v]), t = z == -INFINITY || f.c == -INFINITY ? -1e30f : (z - f.c) * kLog2e, e = exp2_fast(t);
+                    float b = fmaf(f.kt, t, f.k0);
+                    if (REF) b = fmaf(-f.kr, (to_float(r_row[v]) - f.cr) * kLog2e, b);
+                    g_row[v] = from_float<T>((e != 0.f ? e * b : 0.f) + (v == a ? f.at_a : 0.f));
+                }
+            }
+        }
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (s_abort)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
+}
+
 // ---------------------------------------------------------------------------------------------- launch
 template <typename T, bool REF, bool STATS>
 auto narrow_kernel(int g)
@@ -810,6 +1076,16 @@ cudaError_t launch_rows(LossArgs &p, int sm_count, cudaStream_t st)
     const int pieces = (p.A + V - 1 + V - 1) / V;  // a row may start up to V - 1 elements behind a multiple of 16 bytes
     if (pieces <= 32 * kWarpPieces) {
         loss_warp_kernel<T, REF><<<(unsigned)(((long long)p.rows + 3) / 4), 128, 0, st>>>(p);
+        return cudaGetLastError();
+    }
+    // Rows from 256 KB on (the reference's counted), one for every SM or more, and all SMs' rows in two thirds of L2: streamed.
+    const long long row_bytes = 16LL * pieces * (REF ? 2 : 1);
+    const bool alike = !REF || !((((uintptr_t)p.ref ^ (uintptr_t)p.logits) | (uintptr_t)((p.ld - p.ld_ref) * (long long)sizeof(T))) & 15);
+    if (p.rows >= sm_count && row_bytes >= 256 * 1024 && row_bytes * sm_count <= 84LL << 20 && alike) {
+        const auto kernel = loss_stream_kernel<T, REF>;
+        const cudaError_t e = allow_smem((const void *)kernel, kStreamSmem);
+        if (e != cudaSuccess) return e;
+        kernel<<<(unsigned)sm_count, kStreamThreads + 32, kStreamSmem, st>>>(p);
         return cudaGetLastError();
     }
     // As few CTAs a row as keep three of them on an SM (72 KB each); more where the rows alone do not cover the chip.

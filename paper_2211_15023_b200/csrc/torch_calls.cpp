@@ -352,11 +352,13 @@ PyObject *py_linear_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (dtype_code(type) < 0) Py_RETURN_NONE;
     at::Tensor y = empty({x.rows, w.rows}, type, *x.t), space;
     g.workspace_bytes = accerl_linear_i8_workspace((int32_t)x.rows, (int32_t)x.cols, x.code);
-    space = empty({g.workspace_bytes}, at::kByte, *x.t);
+    if (g.workspace_bytes) {
+        space = empty({g.workspace_bytes}, at::kByte, *x.t);
+        g.workspace = space.data_ptr();
+    }
     g.x = x.p;
     g.w = (const int8_t *)w.p;
     g.y = y.data_ptr();
-    g.workspace = space.data_ptr();
     g.ld_x = x.ld;
     g.ld_w = w.ld;
     g.ld_y = w.rows;

@@ -97,7 +97,7 @@ def close(got, want, dtype):
 
 
 # tokens: every width of the instruction and its edges; k: parts of a 128-byte chunk, one chunk, many; n: parts of a tile
-@pytest.mark.parametrize("t,k,n", [(1, 1, 1), (1, 64, 16), (1, 4096, 512), (2, 127, 130), (16, 129, 128), (17, 512, 129),
+@pytest.mark.parametrize("t,k,n", [(1, 1, 1), (4, 4097, 1000), (3, 9000, 5001), (2, 33000, 40), (4, 30000, 33), (5, 700, 90), (1, 64, 16), (1, 4096, 512), (2, 127, 130), (16, 129, 128), (17, 512, 129),
                                    (32, 1000, 257), (33, 640, 100), (64, 2592, 256), (65, 3136, 512), (128, 4100, 640),
                                    (129, 256, 300), (300, 1537, 1000), (1000, 384, 2000), (257, 16, 4097), (2047, 2592, 256),
                                    (4000, 300, 700), (9700, 130, 250), (513, 1000, 5000), (300, 64, 20001)])

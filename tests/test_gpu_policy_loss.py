@@ -264,3 +264,61 @@ def test_captured_and_replayed_beside_another_stream():
         torch.cuda.synchronize()
         for o, w in zip(outs, (want, want_other)):
             assert torch.equal(o["grad"], w["grad"]) and torch.equal(o["stats"], w["stats"])
+
+
+@pytest.mark.parametrize("dtype,v,ref", [("bf16", 70001, "logits"), ("fp32", 70003, "none"), ("fp16", 66000, "logits"),
+                                         ("bf16", 140007, "logp")])
+def test_many_very_long_rows_that_are_streamed(dtype, v, ref):
+    """A row for every SM and more: rows of weight 0 and NaN, masks, rows with nothing left, a reference without a
+    probability that the policy has; the gradient apart, in place and not wanted; against the definition row by row."""
+    import paper_2211_15023_b200 as P
+    dt, t = TYPES[dtype], 301
+    s = inputs(t, v, dt, v)
+    s["w"][:] = 0.5
+    low = torch.finfo(dt).min
+    s["z"][3, 1:v // 2] = -math.inf
+    s["zr"][3, 1:v // 2] = -math.inf
+    s["z"][4, v // 2:] = low
+    s["z"][5, :] = -math.inf
+    s["z"][6, :] = low
+    s["z"][150, :] = float("nan")
+    s["zr"][150, :] = float("nan")
+    s["w"][150] = 0.0
+    s["z"][299, 1:] = -math.inf
+    s["z"][300, :] = -math.inf
+    for i in (3, 4, 299):
+        s["a"][i] = 0
+    lp = torch.log_softmax(s["z"].double(), 1).gather(1, s["a"][:, None])[:, 0]
+    s["logp_old"] = torch.nan_to_num(lp + 0.1, nan=0.0, neginf=0.0).float()
+    s["logp_ref"] = torch.nan_to_num(lp - 0.2, nan=0.0, neginf=0.0).float()
+    kw = dict(logits_ref=s["zr"]) if ref == "logits" else dict(logp_ref=s["logp_ref"]) if ref == "logp" else {}
+    call = lambda grad, **k: P.policy_loss(s["z"], s["a"], s["logp_old"], s["adv"], weights=s["w"], kl_coef=0.05,  # noqa: E731
+                                           entropy_coef=0.02, grad=grad, **k)
+    out = call(True, **kw)
+    P.device_check()
+    some = torch.tensor([0, 1, 2, 3, 4, 5, 6, 147, 148, 149, 150, 151, 296, 299, 300], device="cuda")
+    part = {k: x[some] for k, x in s.items()}
+    _, want = run(part, dt, ref)
+    got = {k: out[k][some] for k in ("logp", "kl", "entropy", "grad")}
+    got["stats"] = torch.zeros(8)
+    want["stats"] = torch.zeros(8, dtype=torch.float64)
+    check(got, want, dt, scale_of(s))
+    # the same rows through the kernels for few rows: the sums of all
+    few = [P.policy_loss(s["z"][i:i + 43], s["a"][i:i + 43], s["logp_old"][i:i + 43], s["adv"][i:i + 43],
+                         weights=s["w"][i:i + 43], kl_coef=0.05, entropy_coef=0.02,
+                         **{k: x[i:i + 43] for k, x in kw.items()}) for i in range(0, t, 43)]
+    total = sum(f["stats"][[0, 1, 2, 3, 4, 5, 7]].double() for f in few)
+    torch.testing.assert_close(out["stats"][[0, 1, 2, 3, 4, 5, 7]].double(), total, rtol=1e-5, atol=1e-3)
+    none = call(False, **kw)
+    assert torch.equal(none["stats"], out["stats"]) and torch.equal(none["logp"], out["logp"])
+    again = call(True, **kw)
+    assert torch.equal(again["grad"], out["grad"]) and torch.equal(again["stats"], out["stats"])
+    if ref == "logits":
+        hole = s["zr"].clone()
+        hole[7, 11] = -math.inf
+        with_hole = call(True, logits_ref=hole)
+        assert with_hole["kl"][7] == math.inf and torch.equal(with_hole["kl"][8:], out["kl"][8:])
+        assert not torch.isfinite(with_hole["grad"][7]).all() and torch.equal(with_hole["grad"][8:], out["grad"][8:])
+    inplace = call(s["z"], **kw)
+    assert torch.equal(s["z"], out["grad"]) and torch.equal(inplace["stats"], out["stats"])
+    P.device_check()
