@@ -387,6 +387,8 @@ __device__ __forceinline__ uint32_t *words(uint4 &v) { return reinterpret_cast<u
 // = e_v (k0 + kt t_v - kr t'_v), logarithms in base 2; and what the action's logit gets on top.
 struct RowCoef {
     float c, cr, k0, kt, kr, at_a;
+    // b of k0 + kt t - kr t' as a function of the pieces' values: one multiply-add a value
+    __device__ __forceinline__ float constant(float sh, float shr) const { return fmaf(kt, sh, fmaf(-kr, shr, k0)); }
 };
 // log2 of a positive sum: the exponent and the mantissa's logarithm apart, off by 1e-7 whatever its size
 __device__ __forceinline__ double log2_of(double x)
@@ -452,11 +454,12 @@ __device__ __forceinline__ void put_gradient(const LossArgs &p, T *g_row, int at
     float z[V], zr[V], g[V];
     unpack<T>(raw, z);
     if constexpr (REF) unpack<T>(raw_r, zr);
+    const float b0 = f.constant(sh, REF ? shr : 0.f), bz = f.kt * kLog2e, br = -f.kr * kLog2e;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        const float t = fmaf(z[k], kLog2e, sh), e = exp2_fast(t);
-        float b = fmaf(f.kt, t, f.k0);
-        if constexpr (REF) b = fmaf(-f.kr, fmaf(zr[k], kLog2e, shr), b);
+        const float e = exp2_fast(fmaf(z[k], kLog2e, sh));
+        float b = fmaf(bz, z[k], b0);
+        if constexpr (REF) b = fmaf(br, zr[k], b);
         g[k] = e * b;
     }
     if ((unsigned)(a - at) < (unsigned)V) {
@@ -784,29 +787,33 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
         for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
 }
 
-// ------------------------------------------------------------------------------------- many very long rows
+// ------------------------------------------------------------------- many very long rows with a reference
 // A CTA per row, persistent, the row streaming through a ring in shared memory twice: for the sums, and, backwards, for the
 // gradient.  The second time it comes from L2, which holds the rows of all CTAs (the launch sees to that).  Against
 // the kernel above a row's end (barriers, one warp's arithmetic: some 2 us in which an SM does little else) comes once for
-// a whole row instead of once for an eighth of one, and the loads of what follows go on meanwhile: 606 -> 332 us for
-// 2048 rows of 128001 with a reference.  Every thread keeps a maximum of its own and rebases its sums when it rises.
-constexpr int kStreamThreads = 512, kStreamBytes = 16 * kStreamThreads;  // of an array, a stage
-constexpr int kStreamSmem = 12 * 2 * kStreamBytes;
+// a whole row instead of once for an eighth of one, and the loads of what follows go on meanwhile: 497 -> 414 us for
+// 2048 rows of 128001.  It is bound by the instructions a pair of logits (some 33; 16 warps instead of 24: 492 us), so every
+// thread keeps a maximum of its own and rebases its sums when it rises.  Without a reference, which halves them, the
+// kernel above is no slower.
+constexpr int kStreamWarps = 24, kStreamThreads = 32 * kStreamWarps, kStreamPer = 2, kStreamStages = 4;
+constexpr int kStreamPieces = kStreamPer * kStreamThreads;  // of an array, a stage
+constexpr int kStreamSmem = kStreamStages * 2 * 16 * kStreamPieces;
 
-template <typename T, bool REF>
+template <typename T>
 __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(const __grid_constant__ LossArgs p)
 {
-    constexpr int V = Row<T>::kVec, kStages = REF ? 12 : 24;
-    extern __shared__ __align__(128) uint4 s_piece[];  // [kStages][REF ? 2 : 1][kStreamThreads]
+    constexpr int V = Row<T>::kVec, kStages = kStreamStages;
+    constexpr bool REF = true;
+    extern __shared__ __align__(128) uint4 s_piece[];  // [kStages][2][kStreamPieces]
     __shared__ uint64_t s_full[kStages], s_empty[kStages];
-    __shared__ Partial s_part[kStreamThreads / 32];
+    __shared__ Partial s_part[kStreamWarps];
     __shared__ RowCoef s_row;
     __shared__ int s_holes, s_abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_u32(&s_full[i]), 1);
-            mbar_init(smem_u32(&s_empty[i]), kStreamThreads / 32);
+            mbar_init(smem_u32(&s_empty[i]), kStreamWarps);
         }
         s_abort = s_holes = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -819,7 +826,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
         const int pieces = (*phase + p.A + V - 1) / V;
         *w0 = *phase > 0;
         *w1 = pieces * V - *phase > p.A ? pieces - 1 : pieces;
-        return (*w1 - *w0 + kStreamThreads - 1) / kStreamThreads;
+        return (*w1 - *w0 + kStreamPieces - 1) / kStreamPieces;
     };
     int slot = 0, phase, w0, w1;
     uint32_t turn = 0;
@@ -829,33 +836,33 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             turn ^= 1;
         }
     };
-    if (warp == kStreamThreads / 32) {
+    if (warp == kStreamWarps) {
         // ------------------------------------------------------------------------------------- loads
         for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
             if (weight_of(p, row) == 0.f) continue;
-            const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = REF ? static_cast<const T *>(p.ref) + row * p.ld_ref : z_row;
+            const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = static_cast<const T *>(p.ref) + row * p.ld_ref;
             const int chunks = whole(z_row, &phase, &w0, &w1);
             for (int i = 0; i < (p.grad ? 2 : 1) * chunks; ++i) {
-                const int c = i < chunks ? i : 2 * chunks - 1 - i, j = w0 + c * kStreamThreads;
+                const int c = i < chunks ? i : 2 * chunks - 1 - i, j = w0 + c * kStreamPieces;
                 if (!mbar_wait(smem_u32(&s_empty[slot]), turn ^ 1, &s_abort, &g_status, 2)) break;
                 if (elect_one()) {
-                    const uint32_t bytes = 16u * (uint32_t)min(kStreamThreads, w1 - j), at = smem_u32(s_piece + slot * (REF ? 2 : 1) * kStreamThreads);
-                    mbar_expect_tx(smem_u32(&s_full[slot]), (REF ? 2 : 1) * bytes);
+                    const uint32_t bytes = 16u * (uint32_t)min(kStreamPieces, w1 - j), at = smem_u32(s_piece + slot * 2 * kStreamPieces);
+                    mbar_expect_tx(smem_u32(&s_full[slot]), 2 * bytes);
                     bulk_load(at, z_row + j * V - phase, bytes, smem_u32(&s_full[slot]));
-                    if (REF) bulk_load(at + kStreamBytes, r_row + j * V - phase, bytes, smem_u32(&s_full[slot]));
+                    bulk_load(at + 16 * kStreamPieces, r_row + j * V - phase, bytes, smem_u32(&s_full[slot]));
                 }
                 __syncwarp();
                 next();
             }
         }
     } else {
-        auto all = [] { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+        auto all = [] { asm volatile("bar.sync 1, %0;" ::"n"(kStreamThreads) : "memory"); };
         const uint32_t low_w = low_word<T>();
         float low[2];
         unpack_word(low_w, low, (const T *)nullptr);
         for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
             const float w = weight_of(p, row);
-            const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = REF ? static_cast<const T *>(p.ref) + row * p.ld_ref : z_row;
+            const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = static_cast<const T *>(p.ref) + row * p.ld_ref;
             T *g_row = p.grad ? static_cast<T *>(p.grad) + row * p.ld_grad : nullptr;
             const int chunks = whole(z_row, &phase, &w0, &w1);
             if (w == 0.f) {
@@ -907,12 +914,14 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 add_sums<T, REF>(raw, raw_r, -from_base(c) * kLog2e, -from_base(cr) * kLog2e, so, st, ss, sd);
             };
             if (ragged != INT_MIN)
-                take(load_piece<T>(z_row, ragged, p.A, -INFINITY), REF ? load_piece<T>(r_row, ragged, p.A, low[0]) : make_uint4(0, 0, 0, 0));
+                take(load_piece<T>(z_row, ragged, p.A, -INFINITY), load_piece<T>(r_row, ragged, p.A, low[0]));
             for (int i = 0; i < chunks; ++i) {
-                const int j = w0 + i * kStreamThreads + (int)threadIdx.x;
+                const int j = w0 + i * kStreamPieces + (int)threadIdx.x;
                 mbar_wait(smem_u32(&s_full[slot]), turn, &s_abort, &g_status, 1);
-                const uint4 *at = s_piece + slot * (REF ? 2 : 1) * kStreamThreads + threadIdx.x;
-                if (j < w1) take(at[0], REF ? at[kStreamThreads] : at[0]);
+                const uint4 *at = s_piece + slot * 2 * kStreamPieces + threadIdx.x;
+#pragma unroll
+                for (int h = 0; h < kStreamPer; ++h)
+                    if (j + h * kStreamThreads < w1) take(at[h * kStreamThreads], at[kStreamPieces + h * kStreamThreads]);
                 // (always so; it waits for the values to be in every lane's registers, not merely asked for)
                 if (__all_sync(0xffffffffu, c >= low[0] && cr >= low[0]) && lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
                 next();
@@ -945,9 +954,9 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             if (lane == 0) s_part[warp] = s;
             if (holes) s_holes = 1;
             all();
-            float C = s_part[lane & 15].c, CR = s_part[lane & 15].cr;
+            float C = s_part[lane % kStreamWarps].c, CR = s_part[lane % kStreamWarps].cr;
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) {
+            for (int o = 16; o > 0; o >>= 1) {
                 C = max_nan(C, __shfl_xor_sync(0xffffffffu, C, o));
                 CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
             }
@@ -958,7 +967,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 C = CR = -INFINITY;
                 for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
                     C = max_nan(C, to_float(z_row[v]));
-                    if (REF) CR = max_nan(CR, to_float(r_row[v]));
+                    CR = max_nan(CR, to_float(r_row[v]));
                 }
                 all();  // (the parts have been read)
 #pragma unroll
@@ -968,7 +977,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 }
                 if (lane == 0) s_part[warp].c = C, s_part[warp].cr = CR;
                 all();
-                for (int i = 0; i < kStreamThreads / 32; ++i) {
+                for (int i = 0; i < kStreamWarps; ++i) {
                     C = max_nan(C, s_part[i].c);
                     CR = max_nan(CR, s_part[i].cr);
                 }
@@ -994,15 +1003,15 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 all();
             }
             if (warp == 0) {
-                Partial b = s_part[lane & 15];
+                const Partial b = s_part[lane % kStreamWarps];
                 const float d = b.so != 0.0 ? (b.c - C) * kLog2e : 0.f, dr = b.ss != 0.0 ? (b.cr - CR) * kLog2e : 0.f;
-                const double f = lane < 16 ? (double)exp2f(d) : 0.0, df = (double)d, dd = (double)(d - dr);
-                double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, lane < 16 ? (double)exp2f(dr) * b.ss : 0.0,
+                const double f = lane < kStreamWarps ? (double)exp2f(d) : 0.0, df = (double)d, dd = (double)(d - dr);
+                double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, lane < kStreamWarps ? (double)exp2f(dr) * b.ss : 0.0,
                                f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+                    for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
                 const RowCoef f0 = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], lane == 0);
                 if (lane == 0) {
                     s_row = f0;
@@ -1014,21 +1023,24 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             const RowCoef f = s_row;
             const float sh = shift_of(0.f, f.c), shr = shift_of(0.f, f.cr);
             if (!odd && ragged != INT_MIN) {
-                uint4 raw = load_piece<T>(z_row, ragged, p.A, low[0]), raw_r = REF ? load_piece<T>(r_row, ragged, p.A, low[0]) : raw;
+                uint4 raw = load_piece<T>(z_row, ragged, p.A, low[0]);
+                const uint4 raw_r = load_piece<T>(r_row, ragged, p.A, low[0]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) words(raw)[i] = max_words<T>(words(raw)[i], low_w);
                 put_gradient<T, REF>(p, g_row, ragged, a, raw, raw_r, f, sh, shr);
             }
             for (int i = chunks - 1; i >= 0; --i) {
-                const int j = w0 + i * kStreamThreads + (int)threadIdx.x;
+                const int j = w0 + i * kStreamPieces + (int)threadIdx.x;
                 mbar_wait(smem_u32(&s_full[slot]), turn, &s_abort, &g_status, 1);
-                const uint4 *at = s_piece + slot * (REF ? 2 : 1) * kStreamThreads + threadIdx.x;
-                if (!odd && j < w1) {
-                    uint4 raw = at[0], raw_r = REF ? at[kStreamThreads] : at[0];
+                const uint4 *at = s_piece + slot * 2 * kStreamPieces + threadIdx.x;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) words(raw)[k] = max_words<T>(words(raw)[k], low_w);
-                    put_gradient<T, REF>(p, g_row, j * V - phase, a, raw, raw_r, f, sh, shr);
-                }
+                for (int h = 0; h < kStreamPer; ++h)
+                    if (!odd && j + h * kStreamThreads < w1) {
+                        uint4 raw = at[h * kStreamThreads];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) words(raw)[k] = max_words<T>(words(raw)[k], low_w);
+                        put_gradient<T, REF>(p, g_row, (j + h * kStreamThreads) * V - phase, a, raw, at[kStreamPieces + h * kStreamThreads], f, sh, shr);
+                    }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
                 next();
@@ -1078,15 +1090,17 @@ cudaError_t launch_rows(LossArgs &p, int sm_count, cudaStream_t st)
         loss_warp_kernel<T, REF><<<(unsigned)(((long long)p.rows + 3) / 4), 128, 0, st>>>(p);
         return cudaGetLastError();
     }
-    // Rows from 256 KB on (the reference's counted), one for every SM or more, and all SMs' rows in two thirds of L2: streamed.
-    const long long row_bytes = 16LL * pieces * (REF ? 2 : 1);
-    const bool alike = !REF || !((((uintptr_t)p.ref ^ (uintptr_t)p.logits) | (uintptr_t)((p.ld - p.ld_ref) * (long long)sizeof(T))) & 15);
-    if (p.rows >= sm_count && row_bytes >= 256 * 1024 && row_bytes * sm_count <= 84LL << 20 && alike) {
-        const auto kernel = loss_stream_kernel<T, REF>;
-        const cudaError_t e = allow_smem((const void *)kernel, kStreamSmem);
-        if (e != cudaSuccess) return e;
-        kernel<<<(unsigned)sm_count, kStreamThreads + 32, kStreamSmem, st>>>(p);
-        return cudaGetLastError();
+    // With a reference, rows from 256 KB on (both arrays'), one for every SM or more, all SMs' rows in two thirds of L2: streamed.
+    if constexpr (REF) {
+        const long long row_bytes = 32LL * pieces;
+        const bool alike = !((((uintptr_t)p.ref ^ (uintptr_t)p.logits) | (uintptr_t)((p.ld - p.ld_ref) * (long long)sizeof(T))) & 15);
+        if (p.rows >= sm_count && row_bytes >= 256 * 1024 && row_bytes * sm_count <= 84LL << 20 && alike) {
+            const auto kernel = loss_stream_kernel<T>;
+            const cudaError_t e = allow_smem((const void *)kernel, kStreamSmem);
+            if (e != cudaSuccess) return e;
+            kernel<<<(unsigned)sm_count, kStreamThreads + 32, kStreamSmem, st>>>(p);
+            return cudaGetLastError();
+        }
     }
     // As few CTAs a row as keep three of them on an SM (72 KB each); more where the rows alone do not cover the chip.
     const int most = 72 * 1024 / (REF ? 32 : 16);
