@@ -282,6 +282,14 @@ def _check_vector(t, n, like, *dtypes):
         t.dtype in dtypes, "a contiguous CUDA vector of %d %s" % (n, " or ".join(map(str, dtypes)))
 
 
+def _keep_for(mem, stream):
+    """Memory of a call's own is not handed out again before a stream that was named has passed the call."""
+    if mem is not None and stream is not None and mem.numel():
+        import torch
+        mem.record_stream(torch.cuda.ExternalStream(int(stream), device=mem.device) if int(stream) else
+                          torch.cuda.default_stream(mem.device))
+
+
 class _on_device_of:
     """Makes the device of a tensor the current one, where it is not."""
 
@@ -459,11 +467,12 @@ def ckpt_weight_grad(dy, ckpt, cols, out_dtype=None, bias=True, out=None, accumu
                        code, _dtype_code(dw.dtype), int(accumulate))
     lib = library()
     need = lib.accerl_ckpt_weight_grad_workspace(C.byref(a))
+    mem = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
     if need:
-        mem = torch.empty(need, dtype=torch.uint8, device=dy.device)
         a.workspace, a.workspace_bytes = _ptr(mem), need
     with _on_device_of(dy):
         _check(lib.accerl_ckpt_weight_grad(C.byref(a), _stream_of(dy, stream)))
+    _keep_for(mem, stream)
     return dw, db
 
 
@@ -536,6 +545,7 @@ def linear_i8(x, weight, bias=None, relu=False, out_dtype=None, out=None, stream
                      _ld16(xq) if given else _ld(xq), _ld16(wq), _ld(out), need, t, n, k, code, _dtype_code(out.dtype), int(relu))
     with _on_device_of(xq):
         _check(lib.accerl_linear_i8(C.byref(a), _stream_of(xq, stream)))
+    _keep_for(ws_mem, stream)
     return out
 
 

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -308,6 +309,14 @@ bool quantised_of(PyObject *qo, PyObject *so, const at::Tensor &like, Rows *q, c
     return q->ld % 16 == 0 && ((uintptr_t)q->p & 15) == 0 && vector_of(so, q->rows, like, false, s);
 }
 
+// memory of a call's own, which torch may hand out again once the call returns: not before a stream that was named has passed it
+void keep_for(const at::Tensor &t, PyObject *stream_o, void *stream)
+{
+    if (stream_o != Py_None && t.defined() && t.numel())
+        c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(),
+                                                      c10::cuda::getStreamFromExternal((cudaStream_t)stream, t.device().index()));
+}
+
 template <typename F>
 accerl_status on_device_of(const at::Tensor &t, F &&call)
 {
@@ -369,6 +378,7 @@ PyObject *py_linear_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
     g.y_dtype = dtype_code(type);
     g.relu = relu;
     const accerl_status st = on_device_of(*x.t, [&] { return accerl_linear_i8(&g, stream); });
+    keep_for(space, a[6], stream);
     if (st != ACCERL_OK) return PyLong_FromLong(st);
     return wrapped(std::move(y));
 }
@@ -475,6 +485,7 @@ PyObject *py_ckpt_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
         g.workspace = space.data_ptr();
     }
     const accerl_status st = on_device_of(*dy.t, [&] { return accerl_ckpt_weight_grad(&g, stream); });
+    keep_for(space, a[5], stream);
     if (st != ACCERL_OK) return PyLong_FromLong(st);
     PyObject *dbo = Py_None;
     if (bias) dbo = wrapped(std::move(db));

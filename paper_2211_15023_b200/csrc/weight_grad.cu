@@ -9,6 +9,8 @@
 // codes and 32 KB of dy; eight warps turn the codes into 16 KB of operand (one block of 32 values a thread: a byte
 // permutation, a subtraction and a multiplication for every two); one thread issues the four instructions of the
 // stage; four warps write the previous tile out meanwhile (two accumulators of 256 columns fill tensor memory).
+// (8192 x 4096 x 4096 into fp32 388 us this way, 2047 x 2592 x 256 16 us.)
+//
 // Where the tiles do not cover the chip the tokens are split over a cluster, whose CTAs add their parts through
 // distributed shared memory in a fixed order.  db is a tile of its own whose decoded operand is all ones.
 #include <cooperative_groups.h>
@@ -949,7 +951,12 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     const int share = pair ? 2 : std::max(1, std::min({kMaxShare, sm_count / p.tiles, stages / 2}));
     const unsigned grid = pair        ? 2u * (unsigned)std::min(p.tiles, sm_count / 2)
                           : share > 1 ? (unsigned)(p.tiles * share) : (unsigned)std::min(p.tiles, sm_count);
-    const size_t smem = plan.plain ? kPlainSmem : pair ? kPairSmem : 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens;
+    // (never less than a pair's CTA takes: these kernels hold all of tensor memory, and a cluster of which one CTA waits for
+    // another kernel's cluster to give some up, and that for the first's other CTAs, would wait for good; with this much shared
+    // memory no other cluster that uses tensor memory fits beside one of them)
+    const size_t smem = plan.plain ? kPlainSmem
+                        : pair     ? kPairSmem
+                                   : std::max(kPairSmem, 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens);
     const bool half = a->dy_dtype == ACCERL_F16;
     const auto kernel = plan.plain ? (half ? weight_grad_plain_kernel<__half> : weight_grad_plain_kernel<__nv_bfloat16>)
                         : pair ? (half ? weight_grad_pair_kernel<__half> : weight_grad_pair_kernel<__nv_bfloat16>)

@@ -164,7 +164,7 @@ def test_captured_on_two_streams_and_after_the_weights_were_made():
     import paper_2211_15023_b200 as P
     g = torch.Generator("cuda").manual_seed(1)
     w = torch.randn((1000, 900), device="cuda", generator=g)
-    cases = [matrix(t, 900, torch.bfloat16, t) for t in (3, 600)]
+    cases = [matrix(t, 900, torch.bfloat16, t) for t in (3, 600, 1, 12000)]
     call = lambda x: P.linear_i8(x, P.quant_rows(w), relu=True)  # noqa: E731
     want = [call(x) for x in cases]
     side = torch.cuda.Stream()
@@ -183,9 +183,11 @@ def test_captured_on_two_streams_and_after_the_weights_were_made():
         for o in outs:
             o.zero_()
         torch.cuda.synchronize()
-        graphs[0].replay()
+        for gr in graphs[::2]:
+            gr.replay()
         with torch.cuda.stream(side):
-            graphs[1].replay()
+            for gr in graphs[1::2]:
+                gr.replay()
         torch.cuda.synchronize()
         for o, v in zip(outs, want):
             assert torch.equal(o, v)

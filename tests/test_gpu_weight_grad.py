@@ -193,3 +193,41 @@ def test_a_training_step_of_an_int8_token_policy():
         graph.replay()
         verify(o)
     P.device_check()
+
+
+@pytest.mark.parametrize("t,n,k", [(200, 70, 300), (300, 2001, 4000), (1000, 520, 15000)])
+def test_named_streams_captures_and_two_calls_at_once_on_another_stream(t, n, k):
+    """Every kernel's form (small tiles over a cluster, read back first, decoded by pairs): on a stream named by its
+    address while torch reuses what the call gave back, beside a layer's product on another stream, captured and replayed
+    with other inputs."""
+    import paper_2211_15023_b200 as P
+    dy, ckpt = inputs(t, n, k, torch.bfloat16, t, pad=1)  # (rows off 16 bytes: a workspace too)
+    want = P.ckpt_weight_grad(dy, ckpt, k, out_dtype=torch.float32)
+    w = P.quant_rows(torch.randn((3000, 640), device="cuda"))
+    x = torch.randn((40, 640), device="cuda").bfloat16()
+    y = P.linear_i8(x, w)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got, ys = [], []
+    for _ in range(10):
+        got.append(P.ckpt_weight_grad(dy, ckpt, k, out_dtype=torch.float32, stream=side.cuda_stream))
+        ys.append(P.linear_i8(x, w))
+        torch.empty(1 << 22, device="cuda", dtype=torch.uint8).fill_(255)  # (what the first call's workspace was, were it free)
+    torch.cuda.synchronize()
+    for g in got:
+        assert torch.equal(g[0], want[0]) and torch.equal(g[1], want[1])
+    assert all(torch.equal(v, y) for v in ys)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        P.ckpt_weight_grad(dy, ckpt, k, out_dtype=torch.float32)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = P.ckpt_weight_grad(dy, ckpt, k, out_dtype=torch.float32)
+    other, _ = inputs(t, n, k, torch.bfloat16, t + 1, pad=1)
+    for new in (dy.clone(), other):
+        dy.copy_(new)
+        graph.replay()
+        direct = P.ckpt_weight_grad(dy, ckpt, k, out_dtype=torch.float32)
+        assert torch.equal(out[0], direct[0]) and torch.equal(out[1], direct[1])
+    P.device_check()
