@@ -5,7 +5,7 @@
 // to fp32; it is computed as x * (1 / s) and the division is done only where that product lies so near to a tie that
 // its error (below 127 * 2^-22) could matter.
 //
-// (8192 rows of 4096 bf16: 26 us, 3.9 TB/s; of 3136 fp32: 28 us, 4.6 TB/s.)
+// (8192 rows of 4096 bf16: 23 us, 4.4 TB/s; of 3136 fp32: 27 us, 4.8 TB/s.)
 //
 // linear_token_kernel: the product for one token.  linear_few_kernel: for some.  Channels are the M of the tensor-core
 // instructions and tokens their N, so that few tokens need few columns and the weights, which bound this case, stream
@@ -35,25 +35,32 @@ struct QuantArgs {
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+constexpr float kRounder = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer, in the low byte of the sum
+
+__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d)
+{
+    return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+}
+
+// by the definition's own division (rare: out of line, so that the loops stay in the instruction cache)
+__device__ __noinline__ uint32_t divided4(float a, float b, float c, float d, float s)
+{
+    auto code = [&](float v) { return fminf(fmaxf(rintf(__fdiv_rn(v, s)), -127.f), 127.f) + kRounder; };
+    return low_bytes(code(a), code(b), code(c), code(d));
+}
+
 // four values to four int8; `exact`: the scale's reciprocal is not to be trusted
 __device__ __forceinline__ uint32_t quantised4(const float *v, float s, float inv, bool exact)
 {
-    const float magic = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer, in the low byte of the sum
-    float b4[4], d = 0.f;
+    float q[4], d = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const float t = v[k] * inv;
-        b4[k] = t + magic;
-        d = fmaxf(d, fabsf(t - (b4[k] - magic)));
+        q[k] = t + kRounder;
+        d = fmaxf(d, fabsf(t - (q[k] - kRounder)));
     }
-    if (exact || d > 0.49996f) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) b4[k] = fminf(fmaxf(rintf(__fdiv_rn(v[k], s)), -127.f), 127.f) + magic;
-    }
-    uint32_t b[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(b4[k]);
-    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    if (exact || d > 0.49996f) return divided4(v[0], v[1], v[2], v[3], s);
+    return low_bytes(q[0], q[1], q[2], q[3]);
 }
 
 // what a row's largest magnitude makes of it
@@ -138,17 +145,18 @@ template <typename T, bool ALIGNED>
 cudaError_t launch_quant(const QuantArgs &p, int sm_count, cudaStream_t st)
 {
     const long long pieces = ((long long)p.cols + Row<T>::kVec - 1) / Row<T>::kVec;
-    // Few rows: two pieces a thread, the shortest chain.  Many: eight, since what a thread does once for its row (two
-    // divisions, the reduction) is some hundred instructions.
+    // Few rows: two pieces a thread, the shortest chain.  Many: four, since what a thread does once for its row (two
+    // divisions, the reduction) is some hundred instructions (8192 x 4096 bf16: 22.7 us; with eight, which leaves fewer
+    // warps on an SM, 25.4; 8192 x 3136 fp32: 26.8 either way).
     const bool few = p.rows < 2 * sm_count;
     if (!few && pieces <= 32 * 8) {
         quant_rows_kernel<T, 8, true, false, ALIGNED><<<(unsigned)((p.rows + 3) / 4), 128, 0, st>>>(p);
         return cudaGetLastError();
     }
-    const long long want = few ? (pieces + 1) / 2 : (pieces + 7) / 8;
+    const long long want = few ? (pieces + 1) / 2 : (pieces + 3) / 4;
     const int threads = (int)std::min<long long>(1024, (want + 31) / 32 * 32);
     const auto kernel = threads * 2 >= pieces   ? quant_rows_kernel<T, 2, false, false, ALIGNED>
-                        : threads * 8 >= pieces ? quant_rows_kernel<T, 8, false, false, ALIGNED>
+                        : threads * 4 >= pieces ? quant_rows_kernel<T, 4, false, false, ALIGNED>
                                                 : quant_rows_kernel<T, 8, false, true, ALIGNED>;
     kernel<<<(unsigned)p.rows, threads, 0, st>>>(p);
     return cudaGetLastError();
