@@ -309,7 +309,7 @@ constexpr int kFewThreads = 192, kMaxStages = 8, kMaxShare = 8;
 
 // One tile of 128 channels x NT tokens; the CTAs of a cluster share its K.
 // Warps 0..3 drain the accumulator (and finish), warp 4 loads, warp 5 issues the tensor-core instructions.
-template <int NT>
+template <int NT, typename T>
 __global__ void __launch_bounds__(kFewThreads)
 linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                   const __grid_constant__ LinearArgs p)
@@ -320,6 +320,8 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         uint32_t tmem;
         int abort_flag;
     } bars;
+    __shared__ float s_ws[128], s_bias[128];
+    __shared__ __align__(16) float s_xs[NT];
     namespace cg = cooperative_groups;
     constexpr int kStage = 128 * 128 + NT * 128, kCols = NT < 32 ? 32 : NT;
     uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -390,32 +392,42 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
             __syncwarp();
         }
     } else {
+        // what the sums are to be multiplied with, while they are made
+        const int n = n0 + (int)threadIdx.x;
+        s_ws[threadIdx.x] = n < p.n ? p.w_scale[n] : 0.f;
+        s_bias[threadIdx.x] = n < p.n && p.bias ? p.bias[n] : 0.f;
+        asm volatile("griddepcontrol.wait;" ::: "memory");  // (the tokens' scales are the quantiser's)
+        if ((int)threadIdx.x < NT) s_xs[threadIdx.x] = t0 + (int)threadIdx.x < p.tokens ? p.x_scale[t0 + threadIdx.x] : 0.f;
+        asm volatile("bar.sync 1, 128;" ::: "memory");
         mbar_wait(smem_u32(&bars.acc), 0, abort_flag, &g_status, 16);
         fence_after();
     }
-    const int n = n0 + (int)threadIdx.x;  // (the first 128 threads)
-    const bool mine = threadIdx.x < 128 && n < p.n;
-    float ws = 0.f, bias = 0.f;
-    if (mine) {
-        ws = p.w_scale[n];
-        bias = p.bias ? p.bias[n] : 0.f;
-    }
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the tokens' scales are the quantiser's
-    auto finish = [&](int t, int acc) {
-        if (!mine || t >= p.tokens) return;
-        store_y(p, t, n, at_least(fmaf((float)acc, p.x_scale[t] * ws, bias), p.relu ? 0.f : -INFINITY));
-    };
+    const float floor = p.relu ? 0.f : -INFINITY;
     int *part = reinterpret_cast<int *>(smem);  // [NT][128]: every operand has been read
     if (warp < 4) {
+        const int n = n0 + (int)threadIdx.x, have = n < p.n ? min(NT, p.tokens - t0) : 0;
+        const float ws = s_ws[threadIdx.x], bias = s_bias[threadIdx.x];
+        T *y = static_cast<T *>(p.y) + (long long)t0 * p.ld_y + n;
 #pragma unroll
         for (int j = 0; j < NT / 16; ++j) {
+            if (16 * j >= p.tokens - t0) break;
             int acc[16];
             tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + 16 * j, acc);
             tmem_wait_ld();
+            if (share > 1) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if (share == 1) finish(t0 + 16 * j + i, acc[i]);
-                else part[(16 * j + i) * 128 + threadIdx.x] = acc[i];
+                for (int i = 0; i < 16; ++i) part[(16 * j + i) * 128 + threadIdx.x] = acc[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const float4 xs = *reinterpret_cast<const float4 *>(&s_xs[16 * j + i]);
+                    const float sc[4] = {xs.x, xs.y, xs.z, xs.w};
+#pragma unroll
+                    for (int l = 0; l < 4; ++l) {
+                        if (16 * j + i + l < have) *y = from_float<T>(at_least(fmaf((float)acc[i + l], sc[l] * ws, bias), floor));
+                        y += p.ld_y;
+                    }
+                }
             }
         }
         fence_before();
@@ -438,12 +450,11 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                     acc[2] += x[c].z;
                     acc[3] += x[c].w;
                 }
-            const int t = t0 + i / 32, n4 = n0 + i % 32 * 4;
-            const float xs = p.x_scale[t], floor = p.relu ? 0.f : -INFINITY;
+            const int t = i / 32, n4 = i % 32 * 4;
+            T *y = static_cast<T *>(p.y) + (long long)(t0 + t) * p.ld_y + n0 + n4;
 #pragma unroll
             for (int l = 0; l < 4; ++l)
-                if (n4 + l < p.n)
-                    store_y(p, t, n4 + l, at_least(fmaf((float)acc[l], xs * p.w_scale[n4 + l], p.bias ? p.bias[n4 + l] : 0.f), floor));
+                if (n0 + n4 + l < p.n) y[l] = from_float<T>(at_least(fmaf((float)acc[l], s_xs[t] * s_ws[n4 + l], s_bias[n4 + l]), floor));
         }
         cg::this_cluster().sync();
     }
@@ -476,8 +487,11 @@ accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArg
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = after_quant ? 2 : 1;
-    ACCERL_CUDA_TRY(allow_smem((const void *)linear_few_kernel<NT>, smem));
-    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_few_kernel<NT>, mw, mx, p));
+    const auto kernel = p.y_dtype == ACCERL_F32    ? linear_few_kernel<NT, float>
+                        : p.y_dtype == ACCERL_BF16 ? linear_few_kernel<NT, __nv_bfloat16>
+                                                   : linear_few_kernel<NT, __half>;
+    ACCERL_CUDA_TRY(allow_smem((const void *)kernel, smem));
+    ACCERL_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, mw, mx, p));
     return ACCERL_OK;
 }
 
@@ -769,8 +783,11 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
         xq = a->workspace;
         xs = reinterpret_cast<const float *>(static_cast<char *>(a->workspace) + quantised_bytes(a->tokens, a->k));
     }
+    // From 65 tokens on pairs, but for few tiles of a long K, which needs to be split (us, few-token kernel / pairs, bf16 out: 1024 x
+    // 1024 x 2048 20.3 / 10.9, 2047 x 2592 x 256 17.6 / 14.5, 512 x 4096 x 2048 19.7 / 17.3, 100 x 4096 x 14336 23.7 / 17.1, 65 x
+    // 1024 x 1024 13.5 / 8.9, 8192 x 3136 x 512 32.4 / 16.3; 300 x 8192 x 512 16.2 / 26.1).
     const long long pair_tiles = ((a->n + kPairTile - 1LL) / kPairTile) * ((a->tokens + kPairTile - 1LL) / kPairTile);
-    const bool pair = a->tokens > 256 && 4 * pair_tiles >= sm_count;
+    const bool pair = a->tokens > 64 && !(pair_tiles <= 8 && a->k > 32 * 128);
     const int nt = a->tokens <= 16 ? 16 : a->tokens <= 32 ? 32 : a->tokens <= 64 ? 64 : 128;
     accerl_status s = tc_make_map(&mw, a->w, a->n, a->k, a->ld_w, 128, 128);
     if (s == ACCERL_OK) s = tc_make_map(&mx, xq, a->tokens, a->k, ld_xq, nt, 128);
