@@ -105,6 +105,9 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) quant_rows_kernel(const __g
 {
     constexpr int V = Row<T>::kVec;
     __shared__ uint32_t s_top[32];
+    // (the launch before is done with everything it reads and writes; and the product, which fetches its weights as soon as it
+    // starts, starts only after that)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long row = WARP ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
@@ -149,17 +152,26 @@ cudaError_t launch_quant(const QuantArgs &p, int sm_count, cudaStream_t st)
     // divisions, the reduction) is some hundred instructions (8192 x 4096 bf16: 22.7 us; with eight, which leaves fewer
     // warps on an SM, 25.4; 8192 x 3136 fp32: 26.8 either way).
     const bool few = p.rows < 2 * sm_count;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     if (!few && pieces <= 32 * 8) {
-        quant_rows_kernel<T, 8, true, false, ALIGNED><<<(unsigned)((p.rows + 3) / 4), 128, 0, st>>>(p);
-        return cudaGetLastError();
+        cfg.gridDim = dim3((unsigned)((p.rows + 3) / 4));
+        cfg.blockDim = dim3(128);
+        return cudaLaunchKernelEx(&cfg, quant_rows_kernel<T, 8, true, false, ALIGNED>, p);
     }
     const long long want = few ? (pieces + 1) / 2 : (pieces + 3) / 4;
     const int threads = (int)std::min<long long>(1024, (want + 31) / 32 * 32);
     const auto kernel = threads * 2 >= pieces   ? quant_rows_kernel<T, 2, false, false, ALIGNED>
                         : threads * 4 >= pieces ? quant_rows_kernel<T, 4, false, false, ALIGNED>
                                                 : quant_rows_kernel<T, 8, false, true, ALIGNED>;
-    kernel<<<(unsigned)p.rows, threads, 0, st>>>(p);
-    return cudaGetLastError();
+    cfg.gridDim = dim3((unsigned)p.rows);
+    cfg.blockDim = dim3((unsigned)threads);
+    return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 cudaError_t launch_quant(const QuantArgs &p, int dtype, int sm_count, cudaStream_t st)
