@@ -6,8 +6,8 @@
 //
 // x^ is the M operand (128 values of k a tile), dy the N operand (up to 256 channels): a decoded value then meets 256
 // others, and a warp's 32 accumulator lanes are neighbours in a row of dw.  Per stage of 64 tokens the TMA fetches 8 KB of
-// codes and 32 KB of dy; eight warps turn the codes into 16 KB of operand (one block of 32 values a thread: a byte
-// permutation, a subtraction and a multiplication for every two); one thread issues the four instructions of the
+// codes and 32 KB of dy; eight warps (two groups of them, in turn) turn the codes into 16 KB of operand (one block of 32 values a thread: a
+// byte permutation, a subtraction and a multiplication for every two); one thread issues the four instructions of the
 // stage; four warps write the previous tile out meanwhile (two accumulators of 256 columns fill tensor memory).
 // (8192 x 4096 x 4096 into fp32 388 us this way, 2047 x 2592 x 256 16 us.)
 //
@@ -31,7 +31,8 @@ constexpr int kRaw = 4, kDec = 3, kDy = 4;       // stages of the three rings
 constexpr int kRawBytes = kTokens * kTileK, kDecBytes = 2 * kRawBytes;
 constexpr int kAhead = 6;                        // stages whose exponents are on their way
 constexpr int kMaxShare = 8;                     // CTAs of a cluster
-constexpr int kConvWarps = 8, kThreads = 32 * (4 + kConvWarps + 4);
+constexpr int kConvWarps = 8, kGroups = 2;        // warps that decode a stage; groups of them that take stages in turn
+constexpr int kFirstOut = 4 + kGroups * kConvWarps, kThreads = 32 * (kFirstOut + 4);
 
 struct GradArgs {
     const uint8_t *e;
@@ -312,48 +313,52 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 a.next();
             }
-    } else if (warp >= 4 && warp < 4 + kConvWarps) {
+    } else if (warp >= 4 && warp < kFirstOut) {
         // ------------------------------------------------------------------------------------ decoding
-        const int w = warp - 4, b = w & 3, t = (w >> 2) * 32 + lane;  // block of 32 values, token of the stage
-        Ring<kRaw> r;
-        Ring<kDec> c;
+        const int group = (warp - 4) / kConvWarps, w = (warp - 4) % kConvWarps;
+        const int b = w & 3, t = (w >> 2) * 32 + lane;  // block of 32 values, token of the stage
+        int seq = 0, raws = 0;                          // stages so far, of the CTA; those with codes
         for (int u = first; u < p.tiles && ok; u += stride) {
             const int kt = u / p.n_tiles;
+            const bool codes = kt < p.k_tiles;
             const int col = kt * kTileK + 32 * b;
-            const uint8_t *e_col = p.e + col / 32;
-            const bool in = kt < p.k_tiles && col < p.cols32;
-            auto exponent = [&](int g) { return in && g < g1 && g * kTokens + t < p.tokens ? (int)__ldg(e_col + (long long)(g * kTokens + t) * p.ld_e) : 127; };
-            int ahead[kAhead];  // a load takes as long as some stages
+            const bool in = codes && col < p.cols32;
+            const uint8_t *e_at = p.e + col / 32 + (long long)t * p.ld_e;
+            const long long e_step = (long long)kTokens * p.ld_e;
+            const int g_first = g0 + (group - seq % kGroups + kGroups) % kGroups;  // this group's stages of the tile
+            auto exponent = [&](int g) { return in && g < g1 && g * kTokens + t < p.tokens ? (int)__ldg(e_at + g * e_step) : 127; };
+            int ahead[kAhead / kGroups];  // a load takes as long as some stages
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) ahead[i] = exponent(g0 + i);
-            for (int g = g0; g < g1 && ok;) {
+            for (int i = 0; i < kAhead / kGroups; ++i) ahead[i] = exponent(g_first + kGroups * i);
+            for (int g = g_first; g < g1 && ok;) {
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {  // (unrolled: a value on its way is not to be moved)
+                for (int i = 0; i < kAhead / kGroups; ++i) {  // (unrolled: a value on its way is not to be moved)
                     if (g >= g1 || !ok) break;
                     const int e = ahead[i];
                     ahead[i] = exponent(g + kAhead);
+                    const int n = seq + g - g0, rn = raws + g - g0, rs = rn % kRaw, ds = n % kDec;
                     uint32_t q[8] = {};
-                    if (kt < p.k_tiles) {
-                        ok = mbar_wait(bar(bars.raw_full[r.slot]), r.phase, abort_flag, &g_status, 16);
-                        load_codes<T>(raw0 + r.slot * kRawBytes, b, t, q);
+                    if (codes) {
+                        ok = mbar_wait(bar(bars.raw_full[rs]), (uint32_t)(rn / kRaw & 1), abort_flag, &g_status, 16);
+                        load_codes<T>(raw0 + rs * kRawBytes, b, t, q);
                     }
-                    if (ok) ok = mbar_wait(bar(bars.dec_empty[c.slot]), c.phase ^ 1, abort_flag, &g_status, 32);
+                    if (ok) ok = mbar_wait(bar(bars.dec_empty[ds]), (uint32_t)(n / kDec & 1) ^ 1, abort_flag, &g_status, 32);
                     ok = __all_sync(0xffffffffu, ok);
-                    put_values<T>(dec0 + c.slot * kDecBytes, b, t, q, e, kt == p.k_tiles);
+                    put_values<T>(dec0 + ds * kDecBytes, b, t, q, e, !codes);
                     fence_async();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(bar(bars.dec_full[c.slot]));
+                        mbar_arrive(bar(bars.dec_full[ds]));
                         // (only now: the codes have arrived in registers, not merely been asked for)
-                        if (kt < p.k_tiles) mbar_arrive(bar(bars.raw_empty[r.slot]));
+                        if (codes) mbar_arrive(bar(bars.raw_empty[rs]));
                     }
-                    if (kt < p.k_tiles) r.next();
-                    c.next();
-                    ++g;
+                    g += kGroups;
                 }
             }
+            seq += g1 - g0;
+            if (codes) raws += g1 - g0;
         }
-    } else if (warp >= 4 + kConvWarps) {
+    } else if (warp >= kFirstOut) {
         // ---------------------------------------------------------------------------------------- out
         const int q = warp & 3;
         const int kl = 32 * q + lane;
@@ -449,7 +454,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // shared memory instead of 56, and 24 KB instead of 40 from L2.  Decoding is a chain of some 700 cycles a stage (wait,
 // load, about 100 instructions, store, fence): two groups of eight warps take stages in turn.
 constexpr int kPairTile = 256;
-constexpr int kPairRaw = 4, kPairDec = 5, kPairDy = 5, kPairDyBytes = 2 * 128 * kTokens, kGroups = 2;
+constexpr int kPairRaw = 4, kPairDec = 5, kPairDy = 5, kPairDyBytes = 2 * 128 * kTokens;
 constexpr int kPairOut = 8, kPairThreads = 32 * (4 + kGroups * kConvWarps + kPairOut);
 constexpr size_t kPairSmem = 1024 + kPairRaw * kRawBytes + kPairDec * kDecBytes + kPairDy * kPairDyBytes;
 
