@@ -481,12 +481,12 @@ __device__ __forceinline__ bool without_q(const T *z_row, const T *r_row, int be
     return found;
 }
 
-// Rows of up to 128 pieces of 16 bytes: a warp per row, the row in its registers.
-constexpr int kWarpPieces = 4;
-template <typename T, bool REF>
-__global__ void __launch_bounds__(128, 4) loss_warp_kernel(const __grid_constant__ LossArgs p)
+// Rows of up to 256 pieces of 16 bytes: a warp per row, the row in its registers.
+constexpr int kWarpPieces = 8;
+template <typename T, bool REF, int NV>
+__global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ? 2 : 1) <= 8 ? 5 : 4) loss_warp_kernel(const __grid_constant__ LossArgs p)
 {
-    constexpr int V = Row<T>::kVec, NV = kWarpPieces;
+    constexpr int V = Row<T>::kVec;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
@@ -503,12 +503,12 @@ __global__ void __launch_bounds__(128, 4) loss_warp_kernel(const __grid_constant
             for (int i = 0; i < NV; ++i) store_piece<T>(g_row, first + i * step, p.A, zero);
         return;
     }
-    uint4 raw[NV], raw_r[NV];
+    uint4 raw[NV], raw_r[REF ? NV : 1];
+    raw_r[0] = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         raw[i] = load_piece<T, true>(z_row, first + i * step, p.A, -INFINITY);
         if constexpr (REF) raw_r[i] = load_piece<T>(r_row, first + i * step, p.A, low_value<T>());
-        else raw_r[i] = raw[i];
     }
     const long long wanted = action_of(p, row);
     const int a = wanted >= 0 && wanted < p.A ? (int)wanted : -1;
@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(128, 4) loss_warp_kernel(const __grid_constant
     float low[2];
     unpack_word(low_w, low, (const T *)nullptr);
     // the maximum; -inf raised to the low value; pieces are relative to `base` (0 but where all lies at that value or below)
-    auto prepare = [&](uint4 (&x)[NV], const T *x_row, float &base) {
+    auto prepare = [&](auto &x, const T *x_row, float &base) {
         uint32_t m = low_w;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -566,7 +566,7 @@ __global__ void __launch_bounds__(128, 4) loss_warp_kernel(const __grid_constant
     float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f;
     float sh = shift_of(base, C), shr = shift_of(base_r, CR);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) add_sums<T, REF>(raw[i], raw_r[i], sh, shr, so, st, ss, sd);
+    for (int i = 0; i < NV; ++i) add_sums<T, REF>(raw[i], raw_r[REF ? i : 0], sh, shr, so, st, ss, sd);
     if (REF && __any_sync(0xffffffffu, holes) && without_q(z_row, r_row, lane, p.A, 32, C)) sd = INFINITY;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -580,7 +580,7 @@ __global__ void __launch_bounds__(128, 4) loss_warp_kernel(const __grid_constant
     const RowCoef f = row_coef<REF>(p, row, w, a >= 0, za, C, CR, so, st, CR == -INFINITY ? 0.0 : (double)ss, sd, lane == 0);
     if (!g_row) return;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) put_gradient<T, REF>(p, g_row, first + i * step, a, raw[i], raw_r[i], f, sh, shr);
+    for (int i = 0; i < NV; ++i) put_gradient<T, REF>(p, g_row, first + i * step, a, raw[i], raw_r[REF ? i : 0], f, sh, shr);
 }
 
 struct Partial {  // of one CTA: maxima, and sums relative to them
@@ -1088,7 +1088,11 @@ cudaError_t launch_rows(LossArgs &p, int sm_count, cudaStream_t st)
     constexpr int V = Row<T>::kVec;
     const int pieces = (p.A + V - 1 + V - 1) / V;  // a row may start up to V - 1 elements behind a multiple of 16 bytes
     if (pieces <= 32 * kWarpPieces) {
-        loss_warp_kernel<T, REF><<<(unsigned)(((long long)p.rows + 3) / 4), 128, 0, st>>>(p);
+        const auto kernel = pieces <= 32     ? loss_warp_kernel<T, REF, 1>
+                            : pieces <= 64   ? loss_warp_kernel<T, REF, 2>
+                            : pieces <= 128  ? loss_warp_kernel<T, REF, 4>
+                                             : loss_warp_kernel<T, REF, 8>;
+        kernel<<<(unsigned)(((long long)p.rows + 3) / 4), 128, 0, st>>>(p);
         return cudaGetLastError();
     }
     // With a reference, rows from 256 KB on (both arrays'), one for every SM or more, all SMs' rows in two thirds of L2: streamed.
