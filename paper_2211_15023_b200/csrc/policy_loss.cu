@@ -221,6 +221,7 @@ loss_stats_kernel(const __grid_constant__ LossArgs p, float *__restrict__ stats)
 // ------------------------------------------------------------------------------------------ narrow rows
 // Up to 64 actions: a group of G lanes per row, at most 8 elements a lane, in double (two exponentials an element are
 // free beside the latencies here, and whether a ratio is clipped is decided where the definition decides it).
+// (100000 rows of 128 fp32: 94 us this way, 64 by the warp kernel below; 131072 of 18: 38 us.)
 constexpr int kNarrow = 64, kNarrowPer = 8;
 
 //
@@ -481,7 +482,8 @@ __device__ __forceinline__ bool without_q(const T *z_row, const T *r_row, int be
     return found;
 }
 
-// Rows of up to 256 pieces of 16 bytes: a warp per row, the row in its registers.
+// Rows of up to 256 pieces of 16 bytes: a warp per row, the row in its registers (45486 rows of 551 fp32: 75 us, a CTA a
+// row 214; its wait for memory and its shuffles are a chain, so registers are kept few: 1, 2, 4 or 8 pieces a lane).
 constexpr int kWarpPieces = 8;
 template <typename T, bool REF, int NV>
 __global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ? 2 : 1) <= 8 ? 5 : 4) loss_warp_kernel(const __grid_constant__ LossArgs p)
