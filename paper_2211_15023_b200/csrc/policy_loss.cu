@@ -863,6 +863,12 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
         const uint32_t low_w = low_word<T>();
         float low[2];
         unpack_word(low_w, low, (const T *)nullptr);
+        // (both arrays' words, in both passes: a logarithm far below the rest, times a coefficient, is to stay finite, since it
+        // meets a probability of 0)
+        auto raise = [&](uint4 &x) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) words(x)[i] = max_words<T>(words(x)[i], low_w);
+        };
         for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
             const float w = weight_of(p, row);
             const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = static_cast<const T *>(p.ref) + row * p.ld_ref;
@@ -1026,10 +1032,9 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             const RowCoef f = s_row;
             const float sh = shift_of(0.f, f.c), shr = shift_of(0.f, f.cr);
             if (!odd && ragged != INT_MIN) {
-                uint4 raw = load_piece<T>(z_row, ragged, p.A, low[0]);
-                const uint4 raw_r = load_piece<T>(r_row, ragged, p.A, low[0]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) words(raw)[i] = max_words<T>(words(raw)[i], low_w);
+                uint4 raw = load_piece<T>(z_row, ragged, p.A, low[0]), raw_r = load_piece<T>(r_row, ragged, p.A, low[0]);
+                raise(raw);
+                raise(raw_r);
                 put_gradient<T, REF>(p, g_row, ragged, a, raw, raw_r, f, sh, shr);
             }
             for (int i = chunks - 1; i >= 0; --i) {
@@ -1039,10 +1044,10 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
 #pragma unroll
                 for (int h = 0; h < kStreamPer; ++h)
                     if (!odd && j + h * kStreamThreads < w1) {
-                        uint4 raw = at[h * kStreamThreads];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) words(raw)[k] = max_words<T>(words(raw)[k], low_w);
-                        put_gradient<T, REF>(p, g_row, (j + h * kStreamThreads) * V - phase, a, raw, at[kStreamPieces + h * kStreamThreads], f, sh, shr);
+                        uint4 raw = at[h * kStreamThreads], raw_r = at[kStreamPieces + h * kStreamThreads];
+                        raise(raw);
+                        raise(raw_r);
+                        put_gradient<T, REF>(p, g_row, (j + h * kStreamThreads) * V - phase, a, raw, raw_r, f, sh, shr);
                     }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));

@@ -1,0 +1,60 @@
+"""The clipped policy loss where masks, references and offsets are extreme, over widths that reach each of its kernels."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_gpu_policy_loss import TYPES, check, definition, inputs, scale_of  # noqa: E402
+
+# (rows, actions): a group of lanes a row, a warp, a CTA, a cluster, streamed (148 rows and more, 256 KB of both arrays)
+WIDTHS = [(8, 18), (8, 300), (8, 9000), (8, 60000), (301, 70001)]
+
+
+def some_of(s, rows=16):
+    """The first rows, where a case puts what it is about, for the definition in 64 bits."""
+    return {k: x[:rows] for k, x in s.items()}
+
+
+def loss(s, ref="logits", grad=True, **kw):
+    import paper_2211_15023_b200 as P
+    kw.update(dict(logits_ref=s["zr"]) if ref == "logits" else dict(logp_ref=s["logp_ref"]) if ref == "logp" else {})
+    out = P.policy_loss(s["z"], s["a"], s["logp_old"], s["adv"], weights=s["w"], grad=grad, **kw)
+    P.device_check()
+    return out
+
+
+def against_definition(s, out, dtype, ref="logits", rows=16, **kw):
+    """The first rows' outputs and gradients (and the sums, where these are all rows)."""
+    part = some_of(s, rows)
+    want = definition(part["z"], part["a"], part["logp_old"], part["adv"], part["w"], part["zr"] if ref == "logits" else None,
+                      part["logp_ref"] if ref == "logp" else None, **kw)
+    z = part["z"].double().cpu()
+    want["z"] = torch.nan_to_num(z, nan=0.0, neginf=-1e30)
+    want["onehot"] = torch.nn.functional.one_hot(part["a"].long().cpu(), z.shape[1]).double()
+    got = {k: out[k][:rows] for k in ("logp", "kl", "entropy", "grad")}
+    got["stats"] = out["stats"]
+    if s["z"].shape[0] > rows:
+        got["stats"], want["stats"] = torch.zeros(8), torch.zeros(8, dtype=torch.float64)
+    check(got, want, dtype, scale_of(part))
+    return want
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_vocabulary_padded_with_the_lowest_value_in_both_arrays(t, v, dtype):
+    """Weights of a scaled loss: the reference's coefficient times the lowest value goes beyond fp32, the probability is 0."""
+    dt = TYPES[dtype]
+    s = inputs(t, v, dt, v)
+    pad = max(1, v // 20)
+    s["z"][:, -pad:] = torch.finfo(dt).min
+    s["zr"][:, -pad:] = torch.finfo(dt).min
+    s["a"].zero_()
+    s["z"][1::2, 0] += 20.0  # (a sum of probabilities near the largest)
+    s["zr"][1::2, 0] += 20.0
+    lp = torch.log_softmax(s["z"].double(), 1)[:, 0]
+    s["logp_old"], s["w"] = (lp + 0.1).float(), torch.full_like(s["w"], 64.0)
+    out = loss(s, kl_coef=0.05, entropy_coef=0.02)
+    assert torch.isfinite(out["grad"]).all() and not out["grad"][:, -pad:].any()
+    against_definition(s, out, dt, kl_coef=0.05, entropy_coef=0.02)
