@@ -1057,7 +1057,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
                     const float z = to_float(z_row[v]), t = z == -INFINITY || f.c == -INFINITY ? -1e30f : (z - f.c) * kLog2e, e = exp2_fast(t);
                     float b = fmaf(f.kt, t, f.k0);
-                    if (REF) b = fmaf(-f.kr, (to_float(r_row[v]) - f.cr) * kLog2e, b);
+                    if (REF && p.kl_coef != 0.f) b = fmaf(-f.kr, (to_float(r_row[v]) - f.cr) * kLog2e, b);  // (may be infinite)
                     g_row[v] = from_float<T>((e != 0.f ? e * b : 0.f) + (v == a ? f.at_a : 0.f));
                 }
             }

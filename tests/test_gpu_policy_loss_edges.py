@@ -58,3 +58,19 @@ def test_a_vocabulary_padded_with_the_lowest_value_in_both_arrays(t, v, dtype):
     out = loss(s, kl_coef=0.05, entropy_coef=0.02)
     assert torch.isfinite(out["grad"]).all() and not out["grad"][:, -pad:].any()
     against_definition(s, out, dt, kl_coef=0.05, entropy_coef=0.02)
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_a_divergence_that_is_only_watched_does_not_touch_the_gradient(t, v, dtype):
+    """kl_coef 0 and a reference without a probability that the policy has: an infinite KL, the loss without it."""
+    dt = TYPES[dtype]
+    s = inputs(t, v, dt, v + 1)
+    s["w"][:] = 0.5
+    s["zr"][2, 3], s["zr"][5, v - 1], s["zr"][6, :] = -math.inf, -math.inf, -math.inf
+    out = loss(s, kl_coef=0.0, entropy_coef=0.02)
+    assert out["kl"][2] == math.inf and out["kl"][5] == math.inf and not torch.isfinite(out["kl"][6])
+    assert torch.isfinite(out["grad"]).all() and torch.isfinite(out["stats"][[0, 1, 3, 4, 5, 7]]).all()
+    out["kl"] = torch.zeros_like(out["kl"])
+    out["stats"][[2, 6]] = 0.0
+    against_definition(s, out, dt, ref="none", kl_coef=0.0, entropy_coef=0.02)
