@@ -91,8 +91,8 @@ __device__ __forceinline__ RowResult<R> finish_row(const LossArgs &p, long long 
         slope = inside ? -plain : (R)0;
         if (p.logp_ref) {
             const R d = (R)((double)p.logp_ref[row] - logp), e = expm1_of(d);
-            kl = e - d;
-            slope -= (R)p.kl_coef * e;
+            kl = e == (R)INFINITY ? e : e - d;  // (d may be infinite too)
+            if (p.kl_coef != 0.f) slope -= (R)p.kl_coef * e;  // (e may be infinite)
         }
     }
     RowResult<R> o;

@@ -74,3 +74,27 @@ def test_a_divergence_that_is_only_watched_does_not_touch_the_gradient(t, v, dty
     out["kl"] = torch.zeros_like(out["kl"])
     out["stats"][[2, 6]] = 0.0
     against_definition(s, out, dt, ref="none", kl_coef=0.0, entropy_coef=0.02)
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_a_watched_divergence_of_the_actions_taken_does_not_touch_the_gradient(t, v, dtype):
+    """kl_coef 0 and an action that the reference's log-probs hold for likely and the policy for (next to) impossible:
+    exp(logp_ref - logp) goes beyond the range, the loss does without it."""
+    dt = TYPES[dtype]
+    s = inputs(t, v, dt, v + 2)
+    s["w"][:] = 0.5
+    s["a"][:8] = 1
+    s["z"][2, 1], s["z"][5, 1], s["z"][6, 1] = -100.0, -1000.0, -math.inf
+    s["logp_old"][:8] = -3.0
+    s["logp_ref"][:8] = -1.0
+    out = loss(s, ref="logp", kl_coef=0.0, entropy_coef=0.02)
+    assert out["kl"][2] > 1e38 and out["kl"][5] == math.inf and out["kl"][6] == math.inf
+    assert torch.isfinite(out["grad"]).all() and torch.isfinite(out["stats"][[0, 1, 3, 4, 5, 7]]).all()
+    s["z"][6, 1] = -200.0  # (the definition has no derivative at -inf; a probability of e^-200 moves nothing)
+    part = some_of(s, 8)
+    want = definition(part["z"], part["a"], part["logp_old"], part["adv"], part["w"], kl_coef=0.0, entropy_coef=0.02)["grad"]
+    # (rounded once, with the tolerance of check() for the factors)
+    p = torch.softmax(part["z"].double().cpu(), 1) + 0.5 * torch.nn.functional.one_hot(part["a"].cpu(), v)
+    slack = 2e-5 * scale_of(part) * p + torch.finfo(dt).smallest_normal * torch.finfo(dt).eps
+    assert ((out["grad"][:8].double().cpu() - want).abs() <= torch.finfo(dt).eps / 2 * 1.01 * want.abs() + slack).all()
