@@ -259,8 +259,8 @@ __global__ void __launch_bounds__(STATS ? 1024 : 128) loss_narrow_kernel(const _
         mo = fmax(mo, __shfl_xor_sync(0xffffffffu, mo, o));
         if (REF) mr = fmax(mr, __shfl_xor_sync(0xffffffffu, mr, o));
     }
-    const bool empty = mo == -INFINITY;
-    if (empty) mo = 0.0;
+    const bool none = mo == -INFINITY;
+    if (none) mo = 0.0;
     if (mr == -INFINITY) mr = 0.0;
     double so = 0.0, ss = 0.0, sd = 0.0, st = 0.0, e[kNarrowPer];
 #pragma unroll
@@ -284,6 +284,7 @@ __global__ void __launch_bounds__(STATS ? 1024 : 128) loss_narrow_kernel(const _
             sd += __shfl_xor_sync(0xffffffffu, sd, o);
         }
     }
+    const bool empty = none && so == 0.0;  // (the maximum passes over a NaN, the sum does not)
     // the action's logit from the lane that holds it (`grad` may be `logits`: memory is not read again)
     const long long a = work ? action_of(p, row) : -1;
     const bool known = a >= 0 && a < p.A;

@@ -98,3 +98,24 @@ def test_a_watched_divergence_of_the_actions_taken_does_not_touch_the_gradient(t
     p = torch.softmax(part["z"].double().cpu(), 1) + 0.5 * torch.nn.functional.one_hot(part["a"].cpu(), v)
     slack = 2e-5 * scale_of(part) * p + torch.finfo(dt).smallest_normal * torch.finfo(dt).eps
     assert ((out["grad"][:8].double().cpu() - want).abs() <= torch.finfo(dt).eps / 2 * 1.01 * want.abs() + slack).all()
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("ref", ["none", "logp", "logits"])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_that_hold_nan_are_not_rows_that_a_mask_empties(t, v, ref, dtype):
+    s = inputs(t, v, TYPES[dtype], v + 3)
+    s["w"][:] = 0.5
+    s["z"][1, :] = math.nan
+    s["z"][2, :] = -math.inf
+    s["z"][2, v // 2] = math.nan
+    s["z"][3, v - 1] = math.nan
+    s["z"][4, :] = -math.inf
+    s["a"][1:5] = 0
+    s["logp_old"][4] = -1.0
+    out = loss(s, ref=ref, kl_coef=0.05 if ref != "none" else 0.0, entropy_coef=0.02)
+    assert torch.isnan(out["logp"][1:4]).all() and torch.isnan(out["entropy"][1:4]).all() and torch.isnan(out["stats"][[0, 1, 3]]).all()
+    assert torch.isnan(out["stats"][2]) == (ref != "none") and torch.isnan(out["kl"][1:4]).all() == (ref != "none")  # (0 with neither)
+    assert torch.isnan(out["grad"][1]).all() and torch.isnan(out["grad"][2, v // 2]) and torch.isnan(out["grad"][3, v - 1])
+    assert out["logp"][4] == -math.inf and not out["grad"][4].any() and not out["entropy"][4] and not out["kl"][4]
+    assert torch.isfinite(out["grad"][5:]).all() and torch.isfinite(out["logp"][5:]).all()
