@@ -49,6 +49,13 @@ __device__ __forceinline__ float exp2_fast(float x)  // 2 ulp, and 0 below -126 
     return y;
 }
 
+__device__ __forceinline__ float max_nan(float a, float b)  // a NaN wins
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+
 __device__ __forceinline__ long long action_of(const LossArgs &p, long long row)
 {
     return p.actions64 ? static_cast<const long long *>(p.actions)[row] : (long long)static_cast<const int *>(p.actions)[row];
@@ -134,7 +141,7 @@ struct RowSums {
         sum[4] += signbit(r) ? w : 0.0;
         sum[5] += w;
         sum[6] += w * fabs(r);
-        most = fmaxf(most, (float)kl);
+        most = max_nan(most, (float)kl);
     }
 };
 
@@ -152,7 +159,7 @@ __device__ __forceinline__ void write_stats(RowSums s, float *__restrict__ stats
     for (int o = 16; o > 0; o >>= 1) {
 #pragma unroll
         for (int j = 0; j < kSums; ++j) s.sum[j] += __shfl_xor_sync(0xffffffffu, s.sum[j], o);
-        s.most = fmaxf(s.most, __shfl_xor_sync(0xffffffffu, s.most, o));
+        s.most = max_nan(s.most, __shfl_xor_sync(0xffffffffu, s.most, o));
     }
     if (lane == 0) {
 #pragma unroll
@@ -169,7 +176,7 @@ __device__ __forceinline__ void write_stats(RowSums s, float *__restrict__ stats
         for (int o = 16; o > 0; o >>= 1) {
 #pragma unroll
             for (int j = 0; j < kSums; ++j) s.sum[j] += __shfl_xor_sync(0xffffffffu, s.sum[j], o);
-            s.most = fmaxf(s.most, __shfl_xor_sync(0xffffffffu, s.most, o));
+            s.most = max_nan(s.most, __shfl_xor_sync(0xffffffffu, s.most, o));
         }
         if (lane == 0) {
             const unsigned rank = cg::this_cluster().block_rank();
@@ -186,7 +193,7 @@ __device__ __forceinline__ void write_stats(RowSums s, float *__restrict__ stats
         stats[j < 6 ? j : 7] = (float)v;
         if (j == 0) {
             float most = -INFINITY;
-            for (unsigned i = 0; i < gridDim.x; ++i) most = fmaxf(most, c_max[i]);
+            for (unsigned i = 0; i < gridDim.x; ++i) most = max_nan(most, c_max[i]);
             stats[6] = most == -INFINITY ? 0.f : most;
         }
     }
@@ -327,12 +334,6 @@ __global__ void __launch_bounds__(STATS ? 1024 : 128) loss_narrow_kernel(const _
 }
 
 // -------------------------------------------------------------------------------------------- long rows
-__device__ __forceinline__ float max_nan(float a, float b)  // a NaN wins
-{
-    float m;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-    return m;
-}
 template <typename T>
 __device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b)
 {

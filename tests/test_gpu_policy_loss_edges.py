@@ -119,3 +119,15 @@ def test_rows_that_hold_nan_are_not_rows_that_a_mask_empties(t, v, ref, dtype):
     assert torch.isnan(out["grad"][1]).all() and torch.isnan(out["grad"][2, v // 2]) and torch.isnan(out["grad"][3, v - 1])
     assert out["logp"][4] == -math.inf and not out["grad"][4].any() and not out["entropy"][4] and not out["kl"][4]
     assert torch.isfinite(out["grad"][5:]).all() and torch.isfinite(out["logp"][5:]).all()
+
+
+@pytest.mark.parametrize("t,v", [(8, 18), (2000, 18), (9000, 18), (8, 300)])
+def test_the_largest_divergence_is_nan_where_a_row_has_none(t, v):
+    """(sums in the same launch, by one CTA, by a cluster)"""
+    s = inputs(t, v, torch.float32, v + 4)
+    s["w"][:] = 0.5
+    s["zr"][1, 1] = math.nan
+    assert torch.isnan(loss(s, kl_coef=0.05)["stats"][6])
+    s["w"][1] = 0.0
+    out = loss(s, kl_coef=0.05)
+    assert out["stats"][6] == out["kl"].max()
