@@ -92,7 +92,9 @@ __device__ __forceinline__ RowResult<R> finish_row(const LossArgs &p, long long 
         r = exp_of((R)(logp - (double)p.logp_old[row]));
         const R lo = (R)1 - (R)p.clip_low, hi = (R)1 + (R)p.clip_high;
         const R rc = r < lo ? lo : r > hi ? hi : r;  // (a NaN stays one)
-        const R plain = r * adv, clipped = rc * adv;
+        R plain = r * adv;
+        if (r == (R)INFINITY) plain = adv == (R)0 ? (R)0 : (R)(exp(logp - (double)p.logp_old[row]) * (double)adv);  // (a small one may fit)
+        const R clipped = rc * adv;
         inside = !(plain > clipped);
         pg = -(inside ? plain : clipped);
         slope = inside ? -plain : (R)0;

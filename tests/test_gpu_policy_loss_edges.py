@@ -131,3 +131,24 @@ def test_the_largest_divergence_is_nan_where_a_row_has_none(t, v):
     s["w"][1] = 0.0
     out = loss(s, kl_coef=0.05)
     assert out["stats"][6] == out["kl"].max()
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_ratios_beyond_fp32_times_small_advantages(t, v, dtype):
+    """A behaviour log-prob of some -95: the ratio is infinite in fp32, its product with an advantage of 0 is 0, with one of
+    -1e-3 it fits, with a positive one the clamp decides."""
+    dt = TYPES[dtype]
+    s = inputs(t, v, dt, v + 5)
+    s["w"][:] = 0.5
+    lp = torch.log_softmax(s["z"][:8].double(), 1).gather(1, s["a"][:8, None])[:, 0]
+    s["logp_old"][1:5] = (lp[1:5] - 92.0).float()
+    s["adv"][1:5] = torch.tensor([0.0, -1e-3, 0.5, -0.0])
+    out = loss(s, ref="none")
+    part = some_of(s, 8)
+    want = definition(part["z"], part["a"], part["logp_old"], part["adv"], part["w"])["grad"]
+    # (a ratio carries the absolute error of the two log-probs, some 1e-5; the rest as in check())
+    tol = torch.finfo(dt).eps / 2 * 1.01 * want.abs() + 5e-5 * want.abs().amax(1, keepdim=True) + torch.finfo(dt).smallest_normal
+    assert ((out["grad"][:8].double().cpu() - want).abs() <= tol).all()
+    assert not out["grad"][1].any() and not out["grad"][3].any() and not out["grad"][4].any() and out["grad"][2].any()
+    assert float(out["stats"][0]) > 1e36 and torch.isfinite(out["stats"][[0, 1, 4, 5]]).all()
