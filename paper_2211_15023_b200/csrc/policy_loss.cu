@@ -89,11 +89,15 @@ __device__ __forceinline__ RowResult<R> finish_row(const LossArgs &p, long long 
         kl = H = 0;
     } else {
         const R adv = (R)p.advantages[row];
-        r = exp_of((R)(logp - (double)p.logp_old[row]));
+        const R x = (R)(logp - (double)p.logp_old[row]);
+        r = exp_of(x);
         const R lo = (R)1 - (R)p.clip_low, hi = (R)1 + (R)p.clip_high;
         const R rc = r < lo ? lo : r > hi ? hi : r;  // (a NaN stays one)
         R plain = r * adv;
-        if (r == (R)INFINITY) plain = adv == (R)0 ? (R)0 : (R)(exp(logp - (double)p.logp_old[row]) * (double)adv);  // (a small one may fit)
+        if (r == (R)INFINITY) {  // (its product may be a number all the same)
+            const R h = exp_of(x * (R)0.5);
+            plain = adv == (R)0 ? (R)0 : h * adv * h;
+        }
         const R clipped = rc * adv;
         inside = !(plain > clipped);
         pg = -(inside ? plain : clipped);
@@ -404,9 +408,15 @@ __device__ __forceinline__ double log2_of(double x)
     return (double)((hi >> 20) - 1023) + (double)log2f((float)m);
 }
 
+// What every t of a row with maximum c is too large by, since its shift is rounded (half a step of c log2(e): at logits around
+// 1000 some 1e-4).  Sums, KL, entropy and the gradient hold differences of t and lose it, a log-probability does not.
+// (The rounding error of a product is a float, so this is exact.)
+__device__ __forceinline__ float excess_of(float base, float c, float sh) { return base == 0.f && c != -INFINITY ? fmaf(c, kLog2e, sh) : 0.f; }
+
+// `excess`: of the policy's t, of which the sums are made
 template <bool REF>
 __device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, float w, bool known, float za, float C, float CR, double so,
-                                            double st, double ss, double sd, bool writer)
+                                            double st, double ss, double sd, float excess, bool writer)
 {
     const bool empty = known && C == -INFINITY;
     const float fo = (float)so, fs = (float)ss, inv = 1.f / fo;
@@ -414,7 +424,7 @@ __device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, fl
     // log2(S / S') from the difference of the sums where they are near each other
     const float d = (float)(so - ss) / fs, ratio = REF ? (fabsf(d) < 0.5f ? log1pf(d) * kLog2e : (float)(lso - log2_of(ss))) : 0.f;
     const float H = (float)kLn2 * (float)(lso - (double)((float)st * inv)), kl = REF ? (float)kLn2 * ((float)sd * inv - ratio) : 0.f;
-    const double logp = empty ? (double)-INFINITY : known ? ((double)za - (double)C) - kLn2 * lso : (double)NAN;
+    const double logp = empty ? (double)-INFINITY : known ? ((double)za - (double)C) - kLn2 * (lso - (double)excess) : (double)NAN;
     const RowResult<float> f = finish_row<float>(p, row, logp, kl, H, empty, writer);
     const float scale = w * inv, kk = REF ? p.kl_coef * (float)kLn2 : 0.f, ke = p.entropy_coef * (float)kLn2;
     RowCoef r;
@@ -429,7 +439,10 @@ __device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, fl
 
 // t of a piece's logits kept relative to `base`, when the row's maximum is c (a part far below the rest: its probabilities
 // are 0, their logarithms kept finite)
-__device__ __forceinline__ float shift_of(float base, float c) { return c == -INFINITY ? 0.f : max_nan((base - c) * kLog2e, -1e30f); }
+__device__ __forceinline__ float shift_of(float base, float c)
+{
+    return c == -INFINITY ? 0.f : base == 0.f ? -c * kLog2e : max_nan((base - c) * kLog2e, -1e30f);
+}
 
 template <typename T, bool REF>
 __device__ __forceinline__ void add_sums(const uint4 &raw, const uint4 &raw_r, float nc, float ncr, float &so, float &st, float &ss, float &sd)
@@ -583,16 +596,23 @@ __global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ?
             sd += __shfl_xor_sync(0xffffffffu, sd, o);
         }
     }
-    const RowCoef f = row_coef<REF>(p, row, w, a >= 0, za, C, CR, so, st, CR == -INFINITY ? 0.0 : (double)ss, sd, lane == 0);
+    const RowCoef f = row_coef<REF>(p, row, w, a >= 0, za, C, CR, so, st, CR == -INFINITY ? 0.0 : (double)ss, sd, excess_of(base, C, sh), lane == 0);
     if (!g_row) return;
 #pragma unroll
     for (int i = 0; i < NV; ++i) put_gradient<T, REF>(p, g_row, first + i * step, a, raw[i], raw_r[REF ? i : 0], f, sh, shr);
 }
 
-struct Partial {  // of one CTA: maxima, and sums relative to them
+struct Partial {  // of one CTA: maxima, and sums relative to their shifts
     double so, st, ss, sd;
     float c, cr;
 };
+
+// what t of a part with maximum c lacks to t of the row, whose maximum is C (parts of the low value and below, and so rows,
+// are relative to their maxima themselves)
+__device__ __forceinline__ double rebase(float c, float C, float low)
+{
+    return c > low ? (double)shift_of(0.f, C) - (double)shift_of(0.f, c) : ((double)c - (double)C) * (double)kLog2e;
+}
 
 // Longer rows: the CTAs of a cluster share a row (one CTA up to 72 KB of it, the reference's included), each keeps its part in
 // shared memory from one read of it to the gradient.  Bulk copies bring it in; what is not whole 16 bytes, or lies otherwise
@@ -772,15 +792,17 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
             C = max_nan(C, __shfl_xor_sync(0xffffffffu, C, o));
             CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
         }
-        // a part's sums, relative to the row's maxima
-        const float d = b.so != 0.0 ? (b.c - C) * kLog2e : 0.f, dr = b.ss != 0.0 ? (b.cr - CR) * kLog2e : 0.f;
-        const double f = (double)exp2f(d), df = (double)d, dd = (double)(d - dr);
-        double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, (double)exp2f(dr) * b.ss, f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
+        // a part's sums, relative to the row's shifts (as the gradient takes them) instead of its own
+        const double d = b.so != 0.0 ? rebase(b.c, C, low[0]) : 0.0, dr = b.ss != 0.0 ? rebase(b.cr, CR, low[0]) : 0.0;
+        const double f = (double)exp2f((float)d);
+        double v[4] = {f * b.so, f != 0.0 ? f * (b.st + d * b.so) : 0.0, (double)exp2f((float)dr) * b.ss,
+                       f != 0.0 ? f * (b.sd + (d - dr) * b.so) : 0.0};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int o = kMaxCluster / 2; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        const RowCoef r = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], rank == 0 && lane == 0);
+        const RowCoef r = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], excess_of(C <= low[0] ? C : 0.f, C, shift_of(0.f, C)),
+                                          rank == 0 && lane == 0);
         if (lane == 0) s_row = r;
     }
     __syncthreads();
@@ -894,7 +916,8 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f, c = low[0], cr = low[0];
             bool holes = false;  // -inf among the reference's logits
             // what a thread's sums are relative to: its maximum, or 0 as long as it has met nothing above the low value
-            auto from_base = [&](float most) { return most <= low[0] ? 0.f : most; };
+            auto shift = [&](float most) { return most <= low[0] ? 0.f : -most * kLog2e; };
+            float nc = 0.f, ncr = 0.f;  // their shifts
             auto take = [&](uint4 raw, uint4 raw_r) {
                 uint32_t m = low_w, mr = low_w, least = low_w;
 #pragma unroll
@@ -909,22 +932,25 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 }
                 const float top = word_max<T>(m);
                 if (top > c) {
-                    const float d = so != 0.f ? (c - top) * kLog2e : 0.f, f = exp2_fast(d);
+                    const float to = -top * kLog2e, d = so != 0.f ? to - nc : 0.f, f = exp2_fast(d);
                     st = f * (st + d * so);
                     sd = f * (sd + d * so);
                     so *= f;
                     c = top;
+                    nc = to;
                 }
                 if constexpr (REF) {
                     holes |= word_min<T>(least) == -INFINITY;
                     const float top_r = word_max<T>(mr);
                     if (top_r > cr) {
-                        sd -= (from_base(cr) - top_r) * kLog2e * so;
-                        ss *= exp2_fast(ss != 0.f ? (cr - top_r) * kLog2e : 0.f);
+                        const float to = -top_r * kLog2e;
+                        sd -= (to - ncr) * so;
+                        ss *= exp2_fast(ss != 0.f ? to - ncr : 0.f);
                         cr = top_r;
+                        ncr = to;
                     }
                 }
-                add_sums<T, REF>(raw, raw_r, -from_base(c) * kLog2e, -from_base(cr) * kLog2e, so, st, ss, sd);
+                add_sums<T, REF>(raw, raw_r, nc, ncr, so, st, ss, sd);
             };
             if (ragged != INT_MIN)
                 take(load_piece<T>(z_row, ragged, p.A, -INFINITY), load_piece<T>(r_row, ragged, p.A, low[0]));
@@ -948,7 +974,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 s.cr = max_nan(s.cr, __shfl_xor_sync(0xffffffffu, s.cr, o));
             }
             {
-                const float d = so != 0.f ? (c - s.c) * kLog2e : 0.f, dr = (from_base(cr) - from_base(s.cr)) * kLog2e, f = exp2f(d);
+                const float d = so != 0.f ? shift(s.c) - nc : 0.f, dr = shift(s.cr) - ncr, f = exp2f(d);
                 st = f != 0.f ? f * (st + d * so) : 0.f;
                 sd = f != 0.f ? f * (sd + (d - dr) * so) : 0.f;
                 so *= f;
@@ -1017,15 +1043,16 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             }
             if (warp == 0) {
                 const Partial b = s_part[lane % kStreamWarps];
-                const float d = b.so != 0.0 ? (b.c - C) * kLog2e : 0.f, dr = b.ss != 0.0 ? (b.cr - CR) * kLog2e : 0.f;
-                const double f = lane < kStreamWarps ? (double)exp2f(d) : 0.0, df = (double)d, dd = (double)(d - dr);
-                double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, lane < kStreamWarps ? (double)exp2f(dr) * b.ss : 0.0,
-                               f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
+                // (an odd row's sums are all relative to its maxima)
+                const double d = b.so != 0.0 && !odd ? rebase(b.c, C, low[0]) : 0.0, dr = b.ss != 0.0 && !odd ? rebase(b.cr, CR, low[0]) : 0.0;
+                const double f = lane < kStreamWarps ? (double)exp2f((float)d) : 0.0;
+                double v[4] = {f * b.so, f != 0.0 ? f * (b.st + d * b.so) : 0.0, lane < kStreamWarps ? (double)exp2f((float)dr) * b.ss : 0.0,
+                               f != 0.0 ? f * (b.sd + (d - dr) * b.so) : 0.0};
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-                const RowCoef f0 = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], lane == 0);
+                const RowCoef f0 = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], odd ? 0.f : excess_of(0.f, C, shift_of(0.f, C)), lane == 0);
                 if (lane == 0) {
                     s_row = f0;
                     if (s_holes) s_holes = 0;  // (then every warp has come past two barriers since it looked)

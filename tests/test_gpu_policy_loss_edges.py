@@ -152,3 +152,21 @@ def test_ratios_beyond_fp32_times_small_advantages(t, v, dtype):
     assert ((out["grad"][:8].double().cpu() - want).abs() <= tol).all()
     assert not out["grad"][1].any() and not out["grad"][3].any() and not out["grad"][4].any() and out["grad"][2].any()
     assert float(out["stats"][0]) > 1e36 and torch.isfinite(out["stats"][[0, 1, 4, 5]]).all()
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("offset", [100.0, -1000.0, 3000.0])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_log_probabilities_do_not_depend_on_the_logits_offset(t, v, offset, dtype):
+    """Logits around `offset` (one more offset a row: a part's maximum is not the row's), with every reference."""
+    dt = TYPES[dtype]
+    s = inputs(t, v, dt, v + 6)
+    for x in ("z", "zr"):
+        s[x].copy_(s[x].float() + offset + torch.arange(t, device="cuda")[:, None] % 7)
+    lp = torch.log_softmax(s["z"][:16].double(), 1).gather(1, s["a"][:16, None])[:, 0]
+    s["logp_old"][:16] = (lp + 0.1).float()
+    s["logp_ref"][:16] = (lp - 0.2).float()
+    s["w"][1] = 1.0
+    for ref in ("none", "logp", "logits"):
+        out = loss(s, ref=ref, kl_coef=0.05, entropy_coef=0.02)
+        against_definition(s, out, dt, ref=ref, kl_coef=0.05, entropy_coef=0.02)
