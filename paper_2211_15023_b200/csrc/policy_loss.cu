@@ -366,8 +366,22 @@ __device__ __forceinline__ uint32_t min_words(uint32_t a, uint32_t b)
         return *reinterpret_cast<const uint32_t *>(&m);
     }
 }
-// What -inf is taken for (finite, so that its probability of 0 times its logarithm is 0), as a word of one or two
-// elements; a row or part of a row with nothing above it is looked at again, see `low_part`.
+// one or two logits: is one of the policy's above the low value where the reference's is below it?
+template <typename T>
+__device__ __forceinline__ bool meets(uint32_t z, uint32_t r, uint32_t low)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __uint_as_float(z) > __uint_as_float(low) && __uint_as_float(r) < __uint_as_float(low);
+    } else {
+        using T2 = std::conditional_t<std::is_same<T, __half>::value, __half2, __nv_bfloat162>;
+        const T2 l = *reinterpret_cast<const T2 *>(&low);
+        return (__hgt2_mask(*reinterpret_cast<const T2 *>(&z), l) & __hlt2_mask(*reinterpret_cast<const T2 *>(&r), l)) != 0;
+    }
+}
+// What -inf, and anything below, is taken for (finite, so that its probability of 0 times its logarithm is 0), as a word of
+// one or two elements; a row or part of a row with nothing above it is looked at again, see `low_part`.  Where the reference
+// lies below it and the policy above, its logarithm counts: such rows (parts) are `odd`, summed up and differentiated element by
+// element in double.
 template <typename T>
 __device__ __forceinline__ constexpr float low_value() { return std::is_same<T, __half>::value ? -65504.f : -1e30f; }
 template <typename T>
@@ -391,6 +405,7 @@ __device__ __forceinline__ float word_min(uint32_t w)
     return sizeof(T) == 4 ? v[0] : fminf(v[0], v[1]);
 }
 __device__ __forceinline__ uint32_t *words(uint4 &v) { return reinterpret_cast<uint32_t *>(&v); }
+__device__ __forceinline__ const uint32_t *words(const uint4 &v) { return reinterpret_cast<const uint32_t *>(&v); }
 
 // Gradient coefficients of a row for sums relative to maxima C and CR:  w p_v (base + kl_coef delta_v + entropy_coef lp_v)
 // = e_v (k0 + kt t_v - kr t'_v), logarithms in base 2; and what the action's logit gets on top.
@@ -423,8 +438,11 @@ __device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, fl
     const double lso = log2_of(so);
     // log2(S / S') from the difference of the sums where they are near each other
     const float d = (float)(so - ss) / fs, ratio = REF ? (fabsf(d) < 0.5f ? log1pf(d) * kLog2e : (float)(lso - log2_of(ss))) : 0.f;
-    const float H = (float)kLn2 * (float)(lso - (double)((float)st * inv)), kl = REF ? (float)kLn2 * ((float)sd * inv - ratio) : 0.f;
-    const double logp = empty ? (double)-INFINITY : known ? ((double)za - (double)C) - kLn2 * (lso - (double)excess) : (double)NAN;
+    const float H = (float)kLn2 * (float)(lso - (double)((float)st * inv));
+    float kl = REF ? (float)kLn2 * ((float)sd * inv - ratio) : 0.f;
+    if (REF && fabsf(kl) > 1e37f) kl = (float)(kLn2 * (double)inv * sd - kLn2 * (double)ratio);  // (its parts may lie beyond fp32)
+    const double at_c = (double)za - (double)C + kLn2 * (double)excess;  // (apart from the sums, which take longer)
+    const double logp = empty ? (double)-INFINITY : known ? at_c - kLn2 * lso : (double)NAN;
     const RowResult<float> f = finish_row<float>(p, row, logp, kl, H, empty, writer);
     const float scale = w * inv, kk = REF ? p.kl_coef * (float)kLn2 : 0.f, ke = p.entropy_coef * (float)kLn2;
     RowCoef r;
@@ -437,11 +455,14 @@ __device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, fl
     return r;
 }
 
+// -c log2(e) rounded, and not as part of a multiply-add: the same everywhere
+__device__ __forceinline__ float minus_log2(float c) { return -__fmul_rn(c, kLog2e); }
+
 // t of a piece's logits kept relative to `base`, when the row's maximum is c (a part far below the rest: its probabilities
 // are 0, their logarithms kept finite)
 __device__ __forceinline__ float shift_of(float base, float c)
 {
-    return c == -INFINITY ? 0.f : base == 0.f ? -c * kLog2e : max_nan((base - c) * kLog2e, -1e30f);
+    return c == -INFINITY ? 0.f : base == 0.f ? minus_log2(c) : max_nan((base - c) * kLog2e, -1e30f);
 }
 
 template <typename T, bool REF>
@@ -488,15 +509,68 @@ __device__ __forceinline__ void put_gradient(const LossArgs &p, T *g_row, int at
     store_piece<T>(g_row, at, p.A, g);
 }
 
-// is there a probability of the policy where the reference has none?  (elements lane, lane + step ... of the row's part)
-template <typename T>
-__device__ __forceinline__ bool without_q(const T *z_row, const T *r_row, int begin, int end, int step, float c)
+// t of one logit in double, relative to what the sums of a row or part with maximum c are relative to
+__device__ __forceinline__ double t_of(float x, float c, float low)
 {
-    bool found = false;
-    for (int v = begin; v < end; v += step)
-        if (to_float(r_row[v]) == -INFINITY && to_float(z_row[v]) != -INFINITY && exp2_fast((to_float(z_row[v]) - c) * kLog2e) != 0.f)
-            found = true;
-    return found;
+    return x == -INFINITY ? (double)-INFINITY : c > low ? fma((double)x, (double)kLog2e, (double)shift_of(0.f, c)) : ((double)x - (double)c) * (double)kLog2e;
+}
+
+// the sums of elements begin, begin + step ... of an odd row or part: e, e t, e', e (t - t')
+template <typename T>
+__device__ __forceinline__ void odd_sums(const T *z_row, const T *r_row, int begin, int end, int step, float c, float cr, double (&sum)[4])
+{
+    sum[0] = sum[1] = sum[2] = sum[3] = 0.0;
+    for (int v = begin; v < end; v += step) {
+        const double t = t_of(to_float(z_row[v]), c, low_value<T>()), tr = t_of(to_float(r_row[v]), cr, low_value<T>());
+        const float e = exp2_fast((float)t);
+        sum[0] += e;
+        sum[2] += exp2_fast((float)tr);
+        if (e != 0.f) {
+            sum[1] += (double)e * t;
+            sum[3] += (double)e * (t - tr);
+        }
+    }
+}
+
+// and their gradients (f: of the row)
+template <typename T>
+__device__ __noinline__ void odd_gradient(const T *z_row, const T *r_row, T *g_row, int begin, int end, int step, int a, const RowCoef &f)
+{
+    for (int v = begin; v < end; v += step) {
+        const double t = t_of(to_float(z_row[v]), f.c, low_value<T>());
+        const float e = exp2_fast((float)t);
+        double b = (double)f.k0 + (double)f.kt * t;
+        if (f.kr != 0.f) b -= (double)f.kr * t_of(to_float(r_row[v]), f.cr, low_value<T>());
+        g_row[v] = from_float<T>((e != 0.f ? (float)((double)e * b) : 0.f) + (v == a ? f.at_a : 0.f));
+    }
+}
+
+// A whole odd row by a warp.  (Apart, and with nothing of the caller's to come back to: what is kept across a call costs the
+// rows that are not odd registers, 8 to 14 % of their time.)
+template <typename T>
+__device__ __noinline__ void odd_row(const LossArgs &p, long long row, float w, int a, float za)
+{
+    const int lane = threadIdx.x & 31;
+    const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = static_cast<const T *>(p.ref) + row * p.ld_ref;
+    float C = -INFINITY, CR = -INFINITY;
+    for (int v = lane; v < p.A; v += 32) {
+        C = max_nan(C, to_float(z_row[v]));
+        CR = max_nan(CR, to_float(r_row[v]));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        C = max_nan(C, __shfl_xor_sync(0xffffffffu, C, o));
+        CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
+    }
+    double sum[4];
+    odd_sums<T>(z_row, r_row, lane, p.A, 32, C, CR, sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+    const RowCoef f = row_coef<true>(p, row, w, a >= 0, za, C, CR, sum[0], sum[1], sum[2], sum[3],
+                                     excess_of(C <= low_value<T>() ? C : 0.f, C, shift_of(0.f, C)), lane == 0);
+    if (p.grad) odd_gradient<T>(z_row, r_row, static_cast<T *>(p.grad) + row * p.ld_grad, lane, p.A, 32, a, f);
 }
 
 // Rows of up to 256 pieces of 16 bytes: a warp per row, the row in its registers (45486 rows of 551 fp32: 75 us, a CTA a
@@ -569,24 +643,30 @@ __global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ?
         }
         return c;
     };
-    bool holes = false;
+    float base, base_r = 0.f;
+    const float C = prepare(raw, z_row, base);
+    float CR = -INFINITY;
     if constexpr (REF) {
-        uint32_t least = raw_r[0].x;
+        uint32_t least = low_w;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) least = min_words<T>(least, words(raw_r[i])[j]);
-        holes = word_min<T>(least) == -INFINITY;
+        bool odd = false;
+        if (word_min<T>(least) < low[0]) {
+            odd = C <= low[0];  // (what the policy's words stand for is not in them)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) odd |= meets<T>(words(raw[i])[j], words(raw_r[i])[j], low_w);
+        }
+        if (__any_sync(0xffffffffu, odd)) return odd_row<T>(p, row, w, a, za);
+        CR = prepare(raw_r, r_row, base_r);
     }
-    float base, base_r = 0.f;
-    const float C = prepare(raw, z_row, base);
-    float CR = -INFINITY;
-    if constexpr (REF) CR = prepare(raw_r, r_row, base_r);
     float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f;
     float sh = shift_of(base, C), shr = shift_of(base_r, CR);
 #pragma unroll
     for (int i = 0; i < NV; ++i) add_sums<T, REF>(raw[i], raw_r[REF ? i : 0], sh, shr, so, st, ss, sd);
-    if (REF && __any_sync(0xffffffffu, holes) && without_q(z_row, r_row, lane, p.A, 32, C)) sd = INFINITY;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         so += __shfl_xor_sync(0xffffffffu, so, o);
@@ -609,9 +689,11 @@ struct Partial {  // of one CTA: maxima, and sums relative to their shifts
 
 // what t of a part with maximum c lacks to t of the row, whose maximum is C (parts of the low value and below, and so rows,
 // are relative to their maxima themselves)
-__device__ __forceinline__ double rebase(float c, float C, float low)
+__device__ __forceinline__ float rebase(float c, float C, float low) { return c > low ? shift_of(0.f, C) - shift_of(0.f, c) : (c - C) * kLog2e; }
+// what t - t' lacks (in double where the reference's part lies so low that its distance may be beyond fp32)
+__device__ __forceinline__ double rebase_difference(float d, float dr, const Partial &b, float CR, float low)
 {
-    return c > low ? (double)shift_of(0.f, C) - (double)shift_of(0.f, c) : ((double)c - (double)C) * (double)kLog2e;
+    return b.ss != 0.0 && b.cr <= low ? (double)d - ((double)b.cr - (double)CR) * (double)kLog2e : (double)(d - dr);
 }
 
 // Longer rows: the CTAs of a cluster share a row (one CTA up to 72 KB of it, the reference's included), each keeps its part in
@@ -631,6 +713,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
     __shared__ Partial parts[kMaxCluster];
     __shared__ float4 s_sum[kRowThreads / 32];
     __shared__ float s_max[2][kRowThreads / 32];
+    __shared__ double s_odd[kRowThreads / 32];
     __shared__ RowCoef s_row;
     __shared__ uint64_t s_bar;
     __shared__ int s_abort;
@@ -691,15 +774,24 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
     float low[2];
     unpack_word(low_w, low, (const T *)nullptr);
     // a pass of the part: -inf raised to the low value, the maximum; in every thread of the CTA
+    bool lower = false, odd = false;  // the reference below the low value; and the policy above it there
     auto prepare = [&](uint4 *x_s, int which) {
-        uint32_t m = low_w, least = low_w;
+        uint32_t m = low_w;
         for (int j = threadIdx.x; j < n; j += blockDim.x) {
-            uint4 v = x_s[j];
+            const uint4 was = x_s[j];
+            uint4 v = was;
+            uint32_t below = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (which) least = min_words<T>(least, words(v)[i]);
                 words(v)[i] = max_words<T>(words(v)[i], low_w);
                 m = max_words<T>(m, words(v)[i]);
+                below |= words(v)[i] ^ words(was)[i];
+            }
+            if (which && below) {
+                lower = true;
+                const uint4 z = z_s[j];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) odd |= meets<T>(words(z)[i], words(was)[i], low_w);
             }
             x_s[j] = v;
         }
@@ -707,7 +799,6 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) c = max_nan(c, __shfl_xor_sync(0xffffffffu, c, o));
         if (lane == 0) s_max[which][warp] = c;
-        return which && word_min<T>(least) == -INFINITY;
     };
     auto block_max = [&](int which) {
         float c = s_max[which][lane & (kRowThreads / 32 - 1)];
@@ -735,14 +826,14 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
             }
         return c;
     };
-    bool holes = false;
     prepare(z_s, 0);
-    if (REF) holes = prepare(r_s, 1);
-    holes = __syncthreads_or(holes);
+    if (REF) prepare(r_s, 1);
+    odd = __syncthreads_or(odd);
     float c = block_max(0), cr = REF ? block_max(1) : -INFINITY, base = 0.f, base_r = 0.f;
     if (c <= low[0]) {
         c = low_part(z_s, z_row, 0);
         base = c == -INFINITY ? 0.f : c;
+        if (REF) odd = __syncthreads_or(lower);  // (what the policy's words stood for was not in them)
     }
     if (REF && cr <= low[0]) {
         cr = low_part(r_s, r_row, 1);
@@ -754,7 +845,14 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
 #pragma unroll 2
         for (int j = threadIdx.x; j < n; j += blockDim.x) add_sums<T, REF>(z_s[j], r_s[j], sh, shr, so, st, ss, sd);
     }
-    if (holes && without_q(z_row, r_row, max(first, 0) + (int)threadIdx.x, min(first + n * V, p.A), (int)blockDim.x, c)) sd = INFINITY;
+    const int from = max(first, 0) + (int)threadIdx.x, end = min(first + n * V, p.A);
+    if (REF && odd) {
+        double sum[4];
+        odd_sums(z_row, r_row, from, end, (int)blockDim.x, c, cr, sum);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum[3] += __shfl_xor_sync(0xffffffffu, sum[3], o);
+        if (lane == 0) s_odd[warp] = sum[3];
+    }
     float sums[4] = {so, st, ss, sd};
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
@@ -767,6 +865,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
         Partial mine;
         const float4 part = lane < warps ? s_sum[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
         double v[4] = {part.x, part.y, part.z, part.w};
+        if (REF && odd) v[3] = lane < warps ? s_odd[lane] : 0.0;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -793,10 +892,9 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
             CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
         }
         // a part's sums, relative to the row's shifts (as the gradient takes them) instead of its own
-        const double d = b.so != 0.0 ? rebase(b.c, C, low[0]) : 0.0, dr = b.ss != 0.0 ? rebase(b.cr, CR, low[0]) : 0.0;
-        const double f = (double)exp2f((float)d);
-        double v[4] = {f * b.so, f != 0.0 ? f * (b.st + d * b.so) : 0.0, (double)exp2f((float)dr) * b.ss,
-                       f != 0.0 ? f * (b.sd + (d - dr) * b.so) : 0.0};
+        const float d = b.so != 0.0 ? rebase(b.c, C, low[0]) : 0.f, dr = b.ss != 0.0 ? rebase(b.cr, CR, low[0]) : 0.f;
+        const double f = (double)exp2f(d), df = (double)d, dd = rebase_difference(d, dr, b, CR, low[0]);
+        double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, (double)exp2f(dr) * b.ss, f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -808,9 +906,12 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
     __syncthreads();
     if (g_row) {
         const RowCoef f = s_row;
+        if (REF && odd) {
+            odd_gradient(z_row, r_row, g_row, from, end, (int)blockDim.x, a, f);
+        }
         const float sh = shift_of(base, f.c), shr = shift_of(base_r, f.cr);
 #pragma unroll 2
-        for (int j = threadIdx.x; j < n; j += blockDim.x) put_gradient<T, REF>(p, g_row, first + j * V, a, z_s[j], r_s[j], f, sh, shr);
+        for (int j = REF && odd ? n : (int)threadIdx.x; j < n; j += blockDim.x) put_gradient<T, REF>(p, g_row, first + j * V, a, z_s[j], r_s[j], f, sh, shr);
     }
     if (s_abort)
         for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
@@ -837,14 +938,14 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
     __shared__ uint64_t s_full[kStages], s_empty[kStages];
     __shared__ Partial s_part[kStreamWarps];
     __shared__ RowCoef s_row;
-    __shared__ int s_holes, s_abort;
+    __shared__ int s_odd, s_abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_u32(&s_full[i]), 1);
             mbar_init(smem_u32(&s_empty[i]), kStreamWarps);
         }
-        s_abort = s_holes = 0;
+        s_abort = s_odd = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -914,25 +1015,26 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             const float za = a >= 0 ? to_float(z_row[a]) : NAN;
             Partial s;
             float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f, c = low[0], cr = low[0];
-            bool holes = false;  // -inf among the reference's logits
+            bool meet = false;  // the reference below the low value where the policy is above it
             // what a thread's sums are relative to: its maximum, or 0 as long as it has met nothing above the low value
-            auto shift = [&](float most) { return most <= low[0] ? 0.f : -most * kLog2e; };
+            auto shift = [&](float most) { return most <= low[0] ? 0.f : minus_log2(most); };
             float nc = 0.f, ncr = 0.f;  // their shifts
             auto take = [&](uint4 raw, uint4 raw_r) {
-                uint32_t m = low_w, mr = low_w, least = low_w;
+                uint32_t m = low_w, mr = low_w, below = 0;
+                const uint4 was = raw_r;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     words(raw)[i] = max_words<T>(words(raw)[i], low_w);
                     m = max_words<T>(m, words(raw)[i]);
                     if constexpr (REF) {
-                        least = min_words<T>(least, words(raw_r)[i]);
                         words(raw_r)[i] = max_words<T>(words(raw_r)[i], low_w);
                         mr = max_words<T>(mr, words(raw_r)[i]);
+                        below |= words(raw_r)[i] ^ words(was)[i];
                     }
                 }
                 const float top = word_max<T>(m);
                 if (top > c) {
-                    const float to = -top * kLog2e, d = so != 0.f ? to - nc : 0.f, f = exp2_fast(d);
+                    const float to = minus_log2(top), d = so != 0.f ? to - nc : 0.f, f = exp2_fast(d);
                     st = f * (st + d * so);
                     sd = f * (sd + d * so);
                     so *= f;
@@ -940,10 +1042,13 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                     nc = to;
                 }
                 if constexpr (REF) {
-                    holes |= word_min<T>(least) == -INFINITY;
+                    if (below) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) meet |= meets<T>(words(raw)[i], words(was)[i], low_w);
+                    }
                     const float top_r = word_max<T>(mr);
                     if (top_r > cr) {
-                        const float to = -top_r * kLog2e;
+                        const float to = minus_log2(top_r);
                         sd -= (to - ncr) * so;
                         ss *= exp2_fast(ss != 0.f ? to - ncr : 0.f);
                         cr = top_r;
@@ -991,7 +1096,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             }
             s.so = so, s.st = st, s.ss = ss, s.sd = sd;
             if (lane == 0) s_part[warp] = s;
-            if (holes) s_holes = 1;
+            if (meet) s_odd = 1;
             all();
             float C = s_part[lane % kStreamWarps].c, CR = s_part[lane % kStreamWarps].cr;
 #pragma unroll
@@ -999,9 +1104,9 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 C = max_nan(C, __shfl_xor_sync(0xffffffffu, C, o));
                 CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
             }
-            // Nothing above the low value in one of the rows, or no probability where the policy may have one: the row is
-            // done from memory, value by value (masks of the type's lowest value only, or none left at all).
-            const bool odd = C <= low[0] || (REF && (CR <= low[0] || s_holes));
+            // Nothing above the low value in one of the rows (masks of the type's lowest value only, or none left at all), or
+            // the reference below it where the policy is not: the row is done from memory, value by value.
+            const bool odd = C <= low[0] || (REF && (CR <= low[0] || s_odd));
             if (odd) {
                 C = CR = -INFINITY;
                 for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
@@ -1021,17 +1126,8 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                     CR = max_nan(CR, s_part[i].cr);
                 }
                 all();
-                double v4[4] = {};
-                for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
-                    const float z = to_float(z_row[v]), t = z == -INFINITY ? -1e30f : (z - C) * kLog2e, e = exp2_fast(t);
-                    v4[0] += e;
-                    if (e != 0.f) v4[1] += (double)e * t;
-                    if (REF) {
-                        const float zr = to_float(r_row[v]), tr = zr == -INFINITY ? -INFINITY : (zr - CR) * kLog2e;
-                        v4[2] += exp2_fast(tr);
-                        if (e != 0.f) v4[3] += (double)e * ((double)t - (double)tr);
-                    }
-                }
+                double v4[4];
+                odd_sums(z_row, r_row, threadIdx.x, p.A, kStreamThreads, C, CR, v4);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
@@ -1043,19 +1139,19 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             }
             if (warp == 0) {
                 const Partial b = s_part[lane % kStreamWarps];
-                // (an odd row's sums are all relative to its maxima)
-                const double d = b.so != 0.0 && !odd ? rebase(b.c, C, low[0]) : 0.0, dr = b.ss != 0.0 && !odd ? rebase(b.cr, CR, low[0]) : 0.0;
-                const double f = lane < kStreamWarps ? (double)exp2f((float)d) : 0.0;
-                double v[4] = {f * b.so, f != 0.0 ? f * (b.st + d * b.so) : 0.0, lane < kStreamWarps ? (double)exp2f((float)dr) * b.ss : 0.0,
-                               f != 0.0 ? f * (b.sd + (d - dr) * b.so) : 0.0};
+                const float d = b.so != 0.0 ? rebase(b.c, C, low[0]) : 0.f, dr = b.ss != 0.0 ? rebase(b.cr, CR, low[0]) : 0.f;
+                const double f = lane < kStreamWarps ? (double)exp2f(d) : 0.0, df = (double)d, dd = rebase_difference(d, dr, b, CR, low[0]);
+                double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, lane < kStreamWarps ? (double)exp2f(dr) * b.ss : 0.0,
+                               f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-                const RowCoef f0 = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], odd ? 0.f : excess_of(0.f, C, shift_of(0.f, C)), lane == 0);
+                const RowCoef f0 = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], excess_of(C <= low[0] ? C : 0.f, C, shift_of(0.f, C)),
+                                                   lane == 0);
                 if (lane == 0) {
                     s_row = f0;
-                    if (s_holes) s_holes = 0;  // (then every warp has come past two barriers since it looked)
+                    if (s_odd) s_odd = 0;  // (then every warp has come past two barriers since it looked)
                 }
             }
             all();
@@ -1084,14 +1180,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 if (lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
                 next();
             }
-            if (odd) {
-                for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
-                    const float z = to_float(z_row[v]), t = z == -INFINITY || f.c == -INFINITY ? -1e30f : (z - f.c) * kLog2e, e = exp2_fast(t);
-                    float b = fmaf(f.kt, t, f.k0);
-                    if (REF && p.kl_coef != 0.f) b = fmaf(-f.kr, (to_float(r_row[v]) - f.cr) * kLog2e, b);  // (may be infinite)
-                    g_row[v] = from_float<T>((e != 0.f ? e * b : 0.f) + (v == a ? f.at_a : 0.f));
-                }
-            }
+            if (odd) odd_gradient(z_row, r_row, g_row, threadIdx.x, p.A, kStreamThreads, a, f);
         }
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

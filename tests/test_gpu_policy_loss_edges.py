@@ -170,3 +170,51 @@ def test_log_probabilities_do_not_depend_on_the_logits_offset(t, v, offset, dtyp
     for ref in ("none", "logp", "logits"):
         out = loss(s, ref=ref, kl_coef=0.05, entropy_coef=0.02)
         against_definition(s, out, dt, ref=ref, kl_coef=0.05, entropy_coef=0.02)
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("value", ["lowest", -1e33, -2e30])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_a_reference_far_below_where_the_policy_is_not(t, v, value, dtype):
+    """Finite reference logits below -1e30 in entries that the policy does not mask count as they are: the KL is p times
+    them.  Beside entries that both mask, rows of which one or both hold nothing else, and a row of the reference with one
+    further below than the rest."""
+    dt = TYPES[dtype]
+    value = torch.finfo(dt).min if value == "lowest" else value
+    s = inputs(t, v, dt, v + 7)
+    s["w"][:] = 0.5
+    s["a"][:] = 0
+    pad = max(1, v // 20)
+    s["z"][:, -pad:] = torch.finfo(dt).min
+    s["zr"][:, -pad:] = torch.finfo(dt).min
+    s["zr"][1, 3] = value
+    s["zr"][2, 2:v // 2] = value
+    s["zr"][3, :-pad] = value                     # (what is masked in the policy lies below, or alike)
+    s["z"][4, :], s["zr"][4, 1:] = value, value   # uniform, against one action
+    s["z"][5, 2:], s["zr"][5, 1] = -math.inf, value
+    s["zr"][6, 5] = -math.inf                     # an infinite divergence
+    s["z"][7, :], s["zr"][7, :] = value, value    # uniform both
+    s["zr"][7, 4] = torch.finfo(dt).min
+    lp = torch.log_softmax(s["z"].double(), 1)[:, 0]
+    s["logp_old"] = (lp + 0.1).float()
+    out = loss(s, kl_coef=0.03125, entropy_coef=0.02)
+    assert out["kl"][6] == math.inf and not torch.isfinite(out["grad"][6]).all()
+    rows = [0, 1, 2, 3, 4, 5, 7]
+    part = {k: x[rows] for k, x in s.items()}
+    want = definition(part["z"], part["a"], part["logp_old"], part["adv"], part["w"], part["zr"], kl_coef=0.03125, entropy_coef=0.02)
+    got = out["kl"][rows].double().cpu()
+    torch.testing.assert_close(got, want["kl"], rtol=8e-6, atol=1e-5)
+    torch.testing.assert_close(out["logp"][rows].double().cpu(), want["logp"], rtol=4e-6, atol=1e-5)
+    # a gradient is w p (base + kl_coef (delta - KL) + ...): once rounded, with the relative error of p (some 2^-20, of an fp32
+    # exponential and a sum of them) and of delta and KL, which cancel
+    z, zr = part["z"].double().cpu(), part["zr"].double().cpu()
+    p = torch.softmax(z, 1)
+    delta = torch.where(p > 0, torch.log_softmax(z, 1) - torch.log_softmax(zr, 1), torch.zeros_like(p)).abs()
+    slack = 2e-5 * p * (scale_of(part) + 0.5 * 0.03125 * (delta + want["kl"][:, None]))
+    slack[:, 0] += 1e-5 * scale_of(part)
+    g = out["grad"][rows].double().cpu()
+    tol = torch.finfo(dt).eps / 2 * 1.01 * want["grad"].abs() + slack + torch.finfo(dt).smallest_normal * torch.finfo(dt).eps
+    assert torch.isfinite(g).all() and ((g - want["grad"]).abs() <= tol).all()
+    assert not g[[0, 1, 2], -pad:].any()
+    again = loss(s, grad=s["z"], kl_coef=0.03125, entropy_coef=0.02)
+    assert torch.equal(torch.nan_to_num(again["grad"]), torch.nan_to_num(out["grad"])) and torch.equal(again["kl"], out["kl"])
