@@ -162,6 +162,38 @@ def _stream_of(t, stream):
     return torch.cuda.current_stream(t.device).cuda_stream if stream is None else stream
 
 
+class _Memory:
+    """Where a call's memory comes from: the pool of the stream that it runs on.  What torch's current stream has given back
+    may be in use by work that waits there, and a stream that was named does not wait for it.  Results are the caller's, who
+    may give them back while its current stream still reads them."""
+
+    def __init__(self, like, stream):
+        import torch
+        self._torch, self._device, self._caller = torch, like.device, None
+        if stream is not None and like.is_cuda:
+            at, current = int(getattr(stream, "value", stream) or 0), self._torch.cuda.current_stream(like.device)
+            if at != current.cuda_stream:
+                self._caller = current
+                self._named = self._torch.cuda.ExternalStream(at, device=like.device) if at else \
+                    self._torch.cuda.default_stream(like.device)
+
+    def _made(self, make):
+        if self._caller is None:
+            return make()
+        with self._torch.cuda.stream(self._named):
+            return make()
+
+    def result(self, shape, dtype, stride=None):
+        t = self._made(lambda: self._torch.empty(shape, dtype=dtype, device=self._device) if stride is None else
+                       self._torch.empty_strided(shape, stride, dtype=dtype, device=self._device))
+        if self._caller is not None and t.numel():
+            t.record_stream(self._caller)
+        return t
+
+    def workspace(self, nbytes):
+        return self._made(lambda: self._torch.empty(nbytes, dtype=self._torch.uint8, device=self._device)) if nbytes else None
+
+
 def _check_batch(frames, obs, *per_state):
     """What a kernel reads as a batch of observations and floats per state must be that, on the device."""
     import torch
@@ -181,8 +213,8 @@ def kl(logits_original, logits_smaller, stream=None):
         logits_smaller.is_contiguous() and logits_original.dtype == logits_smaller.dtype == torch.float32 and \
         logits_original.is_cuda and logits_smaller.is_cuda
     b, a = logits_original.shape
-    out = torch.empty(b, dtype=torch.float32, device=logits_original.device)
-    stats = torch.empty(2, dtype=torch.float32, device=logits_original.device)
+    memory = _Memory(logits_original, stream)
+    out, stats = memory.result(b, torch.float32), memory.result(2, torch.float32)
     _check(library().accerl_policy_kl(logits_original.data_ptr(), logits_smaller.data_ptr(), b, a,
                                       out.data_ptr(), stats.data_ptr(), _stream_of(out, stream)))
     return out, stats
@@ -205,7 +237,8 @@ def vtrace(logp_smaller, logp_original, rewards, values, bootstrap, gamma, rho_h
             bootstrap.is_cuda
         assert discounts is None or (discounts.shape == (n, b) and discounts.is_contiguous() and
                                      discounts.dtype == torch.float32 and discounts.is_cuda)
-    vs, adv = (torch.empty_like(values), torch.empty_like(values)) if out is None else out
+    memory = _Memory(values, stream) if out is None else None
+    vs, adv = (memory.result(values.shape, values.dtype), memory.result(values.shape, values.dtype)) if out is None else out
     _check(library().accerl_vtrace(logp_smaller.data_ptr(), logp_original.data_ptr(), rewards.data_ptr(),
                                    values.data_ptr(), bootstrap.data_ptr(),
                                    None if discounts is None else discounts.data_ptr(), n, b,
@@ -223,14 +256,12 @@ def act_mixed(smaller, original, obs, uniforms, select_uniforms, alpha, stream=N
         return _done(r)
     import torch
     _check_batch(smaller.in_kind == "u8", obs, uniforms, select_uniforms)
-    b, dev = int(obs.shape[0]), obs.device
-    out = dict(logits=torch.empty((b, smaller.n_actions), dtype=torch.float32, device=dev),
-               actions=torch.empty(b, dtype=torch.int32, device=dev),
-               logp=torch.empty(b, dtype=torch.float32, device=dev),
-               entropy=torch.empty(b, dtype=torch.float32, device=dev),
-               use_smaller=torch.empty(b, dtype=torch.uint8, device=dev))
+    b, memory = int(obs.shape[0]), _Memory(obs, stream)
+    out = dict(logits=memory.result((b, smaller.n_actions), torch.float32), actions=memory.result(b, torch.int32),
+               logp=memory.result(b, torch.float32), entropy=memory.result(b, torch.float32),
+               use_smaller=memory.result(b, torch.uint8))
     if smaller.value_head and original.value_head:
-        out["value"] = torch.empty(b, dtype=torch.float32, device=dev)
+        out["value"] = memory.result(b, torch.float32)
     _check(library().accerl_policy_act_mixed(
         smaller._h, original._h, obs.data_ptr(), uniforms.data_ptr(), select_uniforms.data_ptr(),
         float(alpha), b, out["logits"].data_ptr(), out["actions"].data_ptr(), out["logp"].data_ptr(),
@@ -282,14 +313,6 @@ def _check_vector(t, n, like, *dtypes):
         t.dtype in dtypes, "a contiguous CUDA vector of %d %s" % (n, " or ".join(map(str, dtypes)))
 
 
-def _keep_for(mem, stream):
-    """Memory of a call's own is not handed out again before a stream that was named has passed the call."""
-    if mem is not None and stream is not None and mem.numel():
-        import torch
-        mem.record_stream(torch.cuda.ExternalStream(int(stream), device=mem.device) if int(stream) else
-                          torch.cuda.default_stream(mem.device))
-
-
 class _on_device_of:
     """Makes the device of a tensor the current one, where it is not."""
 
@@ -333,15 +356,15 @@ def policy_loss(logits, actions, logp_old, advantages, weights=None, logits_ref=
         if x is not None:
             _check_vector(x, t, logits, torch.float32)
     assert logp_old is not None and advantages is not None
-    dev = logits.device
+    memory = _Memory(logits, stream)
     if grad is True:
-        grad = torch.empty_strided(logits.shape, (_ld(logits), 1), dtype=logits.dtype, device=dev)
+        grad = memory.result(logits.shape, logits.dtype, (_ld(logits), 1))
     elif grad is False:
         grad = None
     if grad is not None:
         _check_rows(grad, logits, logits.dtype)
         assert grad.shape == logits.shape
-    f = torch.empty(8 + 5 * t, dtype=torch.float32, device=dev)
+    f = memory.result(8 + 5 * t, torch.float32)
     out = dict(stats=f[:8], logp=f[8 + 2 * t:8 + 3 * t], kl=f[8 + 3 * t:8 + 4 * t], entropy=f[8 + 4 * t:], grad=grad)
     a = PolicyLossArgs(_ptr(logits), _ptr(logits_ref), _ptr(actions), _ptr(logp_old), _ptr(advantages), _ptr(logp_ref),
                        _ptr(weights), _ld(logits), 0 if logits_ref is None else _ld(logits_ref),
@@ -381,12 +404,12 @@ def ckpt_save(x, act="none", out=None, stream=None):
     _check_rows(x)
     t, k = int(x.shape[0]), int(x.shape[1])
     k32 = -(-k // 32) * 32
-    q = torch.empty((t, k32), dtype=torch.int8, device=x.device)
-    e = torch.empty((t, k32 // 32), dtype=torch.uint8, device=x.device)
+    memory = _Memory(x, stream)
+    q, e = memory.result((t, k32), torch.int8), memory.result((t, k32 // 32), torch.uint8)
     if out is not None:
         _check_rows(out, x, x.dtype)
         assert out.shape == x.shape
-    y = out if out is not None else x if act == "none" else torch.empty((t, k), dtype=x.dtype, device=x.device)
+    y = out if out is not None else x if act == "none" else memory.result((t, k), x.dtype)
     with _on_device_of(x):
         _check(library().accerl_ckpt_save(_ptr(x), _ld(x), code, t, k, _ACTS[act],
                                           None if act == "none" and out is None else _ptr(y), _ld(y), _ptr(q), k32, _ptr(e),
@@ -403,7 +426,7 @@ def ckpt_load(ckpt, cols, dtype, out=None, stream=None):
     import torch
     t = int(ckpt[0].shape[0])
     if out is None:
-        out = torch.empty((t, cols), dtype=dtype, device=ckpt[0].device)
+        out = _Memory(ckpt[0], stream).result((t, cols), dtype)
     code = _dtype_code(out.dtype)
     _check_rows(out)
     assert out.dtype == dtype and tuple(out.shape) == (t, cols)
@@ -426,7 +449,7 @@ def ckpt_act_backward(dy, ckpt, act, out=None, stream=None):
     t, k = int(dy.shape[0]), int(dy.shape[1])
     q, e = _check_ckpt(ckpt, t, k, dy)
     if out is None:
-        out = torch.empty((t, k), dtype=dy.dtype, device=dy.device)
+        out = _Memory(dy, stream).result((t, k), dy.dtype)
     _check_rows(out, dy, dy.dtype)
     assert out.shape == dy.shape
     with _on_device_of(dy):
@@ -455,9 +478,10 @@ def ckpt_weight_grad(dy, ckpt, cols, out_dtype=None, bias=True, out=None, accumu
     t, n, k = int(dy.shape[0]), int(dy.shape[1]), int(cols)
     q, e = _check_ckpt(ckpt, t, k, dy)
     assert out is not None or not accumulate, "accumulate adds to `out`"
+    memory = _Memory(dy, stream)
     if out is None:
         dt = out_dtype or dy.dtype
-        out = (torch.empty((n, k), dtype=dt, device=dy.device), torch.empty(n, dtype=dt, device=dy.device) if bias else None)
+        out = memory.result((n, k), dt), memory.result(n, dt) if bias else None
     dw, db = out
     _check_rows(dw, dy)
     assert tuple(dw.shape) == (n, k) and (out_dtype is None or dw.dtype == out_dtype)
@@ -467,12 +491,11 @@ def ckpt_weight_grad(dy, ckpt, cols, out_dtype=None, bias=True, out=None, accumu
                        code, _dtype_code(dw.dtype), int(accumulate))
     lib = library()
     need = lib.accerl_ckpt_weight_grad_workspace(C.byref(a))
-    mem = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
+    mem = memory.workspace(need)
     if need:
         a.workspace, a.workspace_bytes = _ptr(mem), need
     with _on_device_of(dy):
         _check(lib.accerl_ckpt_weight_grad(C.byref(a), _stream_of(dy, stream)))
-    _keep_for(mem, stream)
     return dw, db
 
 
@@ -494,8 +517,8 @@ def quant_rows(x, stream=None):
     _check_rows(x)
     t, k = int(x.shape[0]), int(x.shape[1])
     k16 = -(-k // 16) * 16
-    q = torch.empty((t, k16), dtype=torch.int8, device=x.device)
-    scale = torch.empty(t, dtype=torch.float32, device=x.device)
+    memory = _Memory(x, stream)
+    q, scale = memory.result((t, k16), torch.int8), memory.result(t, torch.float32)
     with _on_device_of(x):
         _check(library().accerl_quant_rows(_ptr(x), _ld(x), code, t, k, _ptr(q), k16, _ptr(scale), _stream_of(x, stream)))
     return q[:, :k], scale
@@ -534,18 +557,18 @@ def linear_i8(x, weight, bias=None, relu=False, out_dtype=None, out=None, stream
     assert wq.shape[1] == k, "weights of rows of %d for tokens of %d" % (wq.shape[1], k)
     if bias is not None:
         _check_vector(bias, n, xq, torch.float32)
+    memory = _Memory(xq, stream)
     if out is None:
-        out = torch.empty((t, n), dtype=out_dtype or (torch.float32 if given else xq.dtype), device=xq.device)
+        out = memory.result((t, n), out_dtype or (torch.float32 if given else xq.dtype))
     _check_rows(out, xq)
     assert tuple(out.shape) == (t, n) and (out_dtype is None or out.dtype == out_dtype)
     lib = library()
     need = lib.accerl_linear_i8_workspace(t, k, code)
-    ws_mem = torch.empty(need, dtype=torch.uint8, device=xq.device) if need else None
+    ws_mem = memory.workspace(need)
     a = LinearI8Args(_ptr(xq), _ptr(xs), _ptr(wq), _ptr(ws), _ptr(bias), _ptr(out), _ptr(ws_mem),
                      _ld16(xq) if given else _ld(xq), _ld16(wq), _ld(out), need, t, n, k, code, _dtype_code(out.dtype), int(relu))
     with _on_device_of(xq):
         _check(lib.accerl_linear_i8(C.byref(a), _stream_of(xq, stream)))
-    _keep_for(ws_mem, stream)
     return out
 
 
@@ -660,10 +683,9 @@ class Policy:
         import torch
         b = int(obs.shape[0])
         if out is None:
-            dev = obs.device
-            out = (torch.empty((b, self.n_actions), dtype=torch.float32, device=dev),
-                   torch.empty(b, dtype=torch.int32, device=dev),
-                   torch.empty(b, dtype=torch.float32, device=dev))
+            memory = _Memory(obs, stream)
+            out = (memory.result((b, self.n_actions), torch.float32), memory.result(b, torch.int32),
+                   memory.result(b, torch.float32))
         if stream is None:
             stream = torch.cuda.current_stream(obs.device).cuda_stream
         assert obs.is_contiguous() and uniforms.is_contiguous() and obs.is_cuda and uniforms.is_cuda
@@ -682,13 +704,11 @@ class Policy:
             return _done(r)
         import torch
         _check_batch(self.in_kind == "u8", obs, uniforms)
-        b, dev = int(obs.shape[0]), obs.device
-        out = dict(logits=torch.empty((b, self.n_actions), dtype=torch.float32, device=dev),
-                   actions=torch.empty(b, dtype=torch.int32, device=dev),
-                   logp=torch.empty(b, dtype=torch.float32, device=dev),
-                   entropy=torch.empty(b, dtype=torch.float32, device=dev))
+        b, memory = int(obs.shape[0]), _Memory(obs, stream)
+        out = dict(logits=memory.result((b, self.n_actions), torch.float32), actions=memory.result(b, torch.int32),
+                   logp=memory.result(b, torch.float32), entropy=memory.result(b, torch.float32))
         if self.value_head:
-            out["value"] = torch.empty(b, dtype=torch.float32, device=dev)
+            out["value"] = memory.result(b, torch.float32)
         _check(library().accerl_policy_act_ex(
             self._h, obs.data_ptr(), uniforms.data_ptr(), b, out["logits"].data_ptr(),
             out["actions"].data_ptr(), out["logp"].data_ptr(),

@@ -16,6 +16,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <optional>
+
 #include "accerl.h"
 
 namespace {
@@ -47,10 +49,46 @@ bool stream_of(PyObject *o, c10::DeviceIndex device, void **stream)
     return *stream || !not_for_us();
 }
 
-at::Tensor empty(at::IntArrayRef size, at::ScalarType type, const at::Tensor &like)
-{
-    return at::detail::empty_cuda(size, type, like.device(), std::nullopt);
-}
+// Where a call's memory comes from: the pool of the stream that it runs on.  What torch's current stream has given back may be
+// in use by work that waits there, and a stream that was named does not wait for it.  Results are the caller's, who may give
+// them back while its current stream still reads them.
+class Memory {
+  public:
+    Memory(PyObject *stream_o, const at::Tensor &like, void *stream) : device_(like.device())
+    {
+        if (stream_o == Py_None) return;
+        const auto current = c10::cuda::getCurrentCUDAStream(device_.index());
+        if ((void *)current.stream() == stream) return;
+        caller_ = current;
+        named_ = c10::cuda::getStreamFromExternal((cudaStream_t)stream, device_.index());
+    }
+    at::Tensor result(at::IntArrayRef size, at::ScalarType type) const
+    {
+        return kept([&] { return at::detail::empty_cuda(size, type, device_, std::nullopt); });
+    }
+    at::Tensor result_strided(at::IntArrayRef size, at::IntArrayRef stride, at::ScalarType type) const
+    {
+        return kept([&] { return at::detail::empty_strided_cuda(size, stride, type, device_); });
+    }
+    at::Tensor workspace(int64_t bytes) const
+    {
+        const c10::cuda::OptionalCUDAStreamGuard guard(stream());
+        return at::detail::empty_cuda({bytes}, at::kByte, device_, std::nullopt);
+    }
+
+  private:
+    std::optional<c10::Stream> stream() const { return named_ ? std::optional<c10::Stream>(named_->unwrap()) : std::nullopt; }
+    template <typename F>
+    at::Tensor kept(F &&make) const
+    {
+        const c10::cuda::OptionalCUDAStreamGuard guard(stream());
+        at::Tensor t = make();
+        if (caller_ && t.numel()) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), *caller_);
+        return t;
+    }
+    const c10::Device device_;
+    std::optional<c10::cuda::CUDAStream> named_, caller_;  // where they differ
+};
 
 template <typename F>
 accerl_status without_gil(F &&call)
@@ -96,12 +134,13 @@ PyObject *py_act(PyObject *, PyObject *const *a, Py_ssize_t n)
     void *stream;
     if (not_for_us()) Py_RETURN_NONE;
     if (!act_inputs(a[2], a[3], a[4], &obs, &u, &b) || !stream_of(a[6], obs->device().index(), &stream)) Py_RETURN_NONE;
+    const Memory memory(a[6], *obs, stream);
     void *dst[3];
     at::Tensor t[3];
     if (a[5] == Py_None) {
-        t[0] = empty({b, A}, at::kFloat, *obs);
-        t[1] = empty({b}, at::kInt, *obs);
-        t[2] = empty({b}, at::kFloat, *obs);
+        t[0] = memory.result({b, A}, at::kFloat);
+        t[1] = memory.result({b}, at::kInt);
+        t[2] = memory.result({b}, at::kFloat);
         for (int i = 0; i < 3; ++i) dst[i] = t[i].data_ptr();
     } else {
         if (!PyTuple_Check(a[5]) || PyTuple_GET_SIZE(a[5]) != 3) Py_RETURN_NONE;
@@ -139,9 +178,10 @@ PyObject *py_act_ex(PyObject *, PyObject *const *a, Py_ssize_t n)
     void *stream;
     if (not_for_us()) Py_RETURN_NONE;
     if (!act_inputs(a[2], a[4], a[5], &obs, &u, &b) || !stream_of(a[6], obs->device().index(), &stream)) Py_RETURN_NONE;
-    at::Tensor logits = empty({b, A}, at::kFloat, *obs), actions = empty({b}, at::kInt, *obs),
-               logp = empty({b}, at::kFloat, *obs), entropy = empty({b}, at::kFloat, *obs), value;
-    if (a[3] == Py_True) value = empty({b}, at::kFloat, *obs);
+    const Memory memory(a[6], *obs, stream);
+    at::Tensor logits = memory.result({b, A}, at::kFloat), actions = memory.result({b}, at::kInt),
+               logp = memory.result({b}, at::kFloat), entropy = memory.result({b}, at::kFloat), value;
+    if (a[3] == Py_True) value = memory.result({b}, at::kFloat);
     const void *obs_p = obs->data_ptr();
     const float *u_p = (const float *)u->data_ptr();
     float *value_p = value.defined() ? (float *)value.data_ptr() : nullptr;
@@ -176,10 +216,11 @@ PyObject *py_act_mixed(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!act_inputs(a[3], a[5], a[6], &obs, &u, &b) || !select || select->numel() != b ||
         !stream_of(a[9], obs->device().index(), &stream))
         Py_RETURN_NONE;
-    at::Tensor logits = empty({b, A}, at::kFloat, *obs), actions = empty({b}, at::kInt, *obs),
-               logp = empty({b}, at::kFloat, *obs), entropy = empty({b}, at::kFloat, *obs),
-               use = empty({b}, at::kByte, *obs), value;
-    if (a[4] == Py_True) value = empty({b}, at::kFloat, *obs);
+    const Memory memory(a[9], *obs, stream);
+    at::Tensor logits = memory.result({b, A}, at::kFloat), actions = memory.result({b}, at::kInt),
+               logp = memory.result({b}, at::kFloat), entropy = memory.result({b}, at::kFloat),
+               use = memory.result({b}, at::kByte), value;
+    if (a[4] == Py_True) value = memory.result({b}, at::kFloat);
     const void *obs_p = obs->data_ptr();
     const float *u_p = (const float *)u->data_ptr(), *sel_p = (const float *)select->data_ptr();
     float *value_p = value.defined() ? (float *)value.data_ptr() : nullptr;
@@ -210,7 +251,8 @@ PyObject *py_kl(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!zo || !zs || zo->dim() != 2 || zo->sizes() != zs->sizes() || zo->size(0) > INT32_MAX ||
         zo->size(1) > INT32_MAX || !stream_of(a[2], zo->device().index(), &stream))
         Py_RETURN_NONE;
-    at::Tensor out = empty({zo->size(0)}, at::kFloat, *zo), stats = empty({2}, at::kFloat, *zo);
+    const Memory memory(a[2], *zo, stream);
+    at::Tensor out = memory.result({zo->size(0)}, at::kFloat), stats = memory.result({2}, at::kFloat);
     const float *zo_p = (const float *)zo->data_ptr(), *zs_p = (const float *)zs->data_ptr();
     const int32_t b = (int32_t)zo->size(0), A = (int32_t)zo->size(1);
     const accerl_status st = without_gil([&] {
@@ -239,7 +281,8 @@ PyObject *py_vtrace(PyObject *, PyObject *const *a, Py_ssize_t n)
         Py_RETURN_NONE;
     const double gamma = PyFloat_AsDouble(a[6]), rho = PyFloat_AsDouble(a[7]), c = PyFloat_AsDouble(a[8]);
     if (not_for_us()) Py_RETURN_NONE;
-    at::Tensor vs = empty(in[0]->sizes(), at::kFloat, *in[0]), adv = empty(in[0]->sizes(), at::kFloat, *in[0]);
+    const Memory memory(a[9], *in[0], stream);
+    at::Tensor vs = memory.result(in[0]->sizes(), at::kFloat), adv = memory.result(in[0]->sizes(), at::kFloat);
     const float *p[6];
     for (int i = 0; i < 6; ++i) p[i] = in[i] ? (const float *)in[i]->data_ptr() : nullptr;
     const int32_t steps = (int32_t)in[0]->size(0), b = (int32_t)in[0]->size(1);
@@ -309,14 +352,6 @@ bool quantised_of(PyObject *qo, PyObject *so, const at::Tensor &like, Rows *q, c
     return q->ld % 16 == 0 && ((uintptr_t)q->p & 15) == 0 && vector_of(so, q->rows, like, false, s);
 }
 
-// memory of a call's own, which torch may hand out again once the call returns: not before a stream that was named has passed it
-void keep_for(const at::Tensor &t, PyObject *stream_o, void *stream)
-{
-    if (stream_o != Py_None && t.defined() && t.numel())
-        c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(),
-                                                      c10::cuda::getStreamFromExternal((cudaStream_t)stream, t.device().index()));
-}
-
 template <typename F>
 accerl_status on_device_of(const at::Tensor &t, F &&call)
 {
@@ -331,7 +366,8 @@ PyObject *py_quant_rows(PyObject *, PyObject *const *a, Py_ssize_t n)
     void *stream;
     if (n != 2 || !rows_of(a[0], &x) || x.code < 0 || !stream_of(a[1], x.t->device().index(), &stream)) Py_RETURN_NONE;
     const int64_t ld = (x.cols + 15) / 16 * 16;
-    at::Tensor q = empty({x.rows, ld}, at::kChar, *x.t), scale = empty({x.rows}, at::kFloat, *x.t);
+    const Memory memory(a[1], *x.t, stream);
+    at::Tensor q = memory.result({x.rows, ld}, at::kChar), scale = memory.result({x.rows}, at::kFloat);
     const accerl_status st = on_device_of(*x.t, [&] {
         return accerl_quant_rows(x.p, x.ld, x.code, x.rows, (int32_t)x.cols, (int8_t *)q.data_ptr(), ld, (float *)scale.data_ptr(), stream);
     });
@@ -359,10 +395,11 @@ PyObject *py_linear_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
         type = reinterpret_cast<THPDtype *>(a[5])->scalar_type;
     }
     if (dtype_code(type) < 0) Py_RETURN_NONE;
-    at::Tensor y = empty({x.rows, w.rows}, type, *x.t), space;
+    const Memory memory(a[6], *x.t, stream);
+    at::Tensor y = memory.result({x.rows, w.rows}, type), space;
     g.workspace_bytes = accerl_linear_i8_workspace((int32_t)x.rows, (int32_t)x.cols, x.code);
     if (g.workspace_bytes) {
-        space = empty({g.workspace_bytes}, at::kByte, *x.t);
+        space = memory.workspace(g.workspace_bytes);
         g.workspace = space.data_ptr();
     }
     g.x = x.p;
@@ -378,7 +415,6 @@ PyObject *py_linear_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
     g.y_dtype = dtype_code(type);
     g.relu = relu;
     const accerl_status st = on_device_of(*x.t, [&] { return accerl_linear_i8(&g, stream); });
-    keep_for(space, a[6], stream);
     if (st != ACCERL_OK) return PyLong_FromLong(st);
     return wrapped(std::move(y));
 }
@@ -392,8 +428,9 @@ PyObject *py_ckpt_save(PyObject *, PyObject *const *a, Py_ssize_t n)
     const long act = PyLong_AsLong(a[1]);
     if (not_for_us()) Py_RETURN_NONE;
     const int64_t cols32 = (x.cols + 31) / 32 * 32;
-    at::Tensor q = empty({x.rows, cols32}, at::kChar, *x.t), e = empty({x.rows, cols32 / 32}, at::kByte, *x.t), y;
-    if (act != ACCERL_ACT_NONE) y = empty({x.rows, x.cols}, x.t->scalar_type(), *x.t);
+    const Memory memory(a[2], *x.t, stream);
+    at::Tensor q = memory.result({x.rows, cols32}, at::kChar), e = memory.result({x.rows, cols32 / 32}, at::kByte), y;
+    if (act != ACCERL_ACT_NONE) y = memory.result({x.rows, x.cols}, x.t->scalar_type());
     const accerl_status st = on_device_of(*x.t, [&] {
         return accerl_ckpt_save(x.p, x.ld, x.code, x.rows, (int32_t)x.cols, (int32_t)act, y.defined() ? y.data_ptr() : nullptr, x.cols,
                                 (int8_t *)q.data_ptr(), cols32, (uint8_t *)e.data_ptr(), cols32 / 32, stream);
@@ -416,7 +453,8 @@ PyObject *py_ckpt_load(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (not_for_us() || cols < 1 || cols > INT32_MAX || dtype_code(type) < 0 || !rows_of(PyTuple_GET_ITEM(a[0], 0), &like) ||
         !ckpt_of(a[0], like.rows, cols, *like.t, &q, &e) || !stream_of(a[3], like.t->device().index(), &stream))
         Py_RETURN_NONE;
-    at::Tensor x = empty({q.rows, cols}, type, *q.t);
+    const Memory memory(a[3], *q.t, stream);
+    at::Tensor x = memory.result({q.rows, cols}, type);
     const accerl_status st = on_device_of(*q.t, [&] {
         return accerl_ckpt_load((const int8_t *)q.p, q.ld, (const uint8_t *)e.p, e.ld, q.rows, (int32_t)cols, x.data_ptr(), cols,
                                 dtype_code(type), stream);
@@ -435,7 +473,8 @@ PyObject *py_ckpt_act_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         Py_RETURN_NONE;
     const long act = PyLong_AsLong(a[2]);
     if (not_for_us()) Py_RETURN_NONE;
-    at::Tensor dx = empty({dy.rows, dy.cols}, dy.t->scalar_type(), *dy.t);
+    const Memory memory(a[3], *dy.t, stream);
+    at::Tensor dx = memory.result({dy.rows, dy.cols}, dy.t->scalar_type());
     const accerl_status st = on_device_of(*dy.t, [&] {
         return accerl_ckpt_act_backward(dy.p, dy.ld, dy.code, (const int8_t *)q.p, q.ld, (const uint8_t *)e.p, e.ld, dy.rows, (int32_t)dy.cols,
                                         (int32_t)act, dx.data_ptr(), dy.cols, stream);
@@ -462,8 +501,9 @@ PyObject *py_ckpt_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int bias = PyObject_IsTrue(a[4]);
     if (bias < 0) PyErr_Clear();
     if (bias < 0 || dtype_code(type) < 0) Py_RETURN_NONE;
-    at::Tensor dw = empty({dy.cols, k}, type, *dy.t), db, space;
-    if (bias) db = empty({dy.cols}, type, *dy.t);
+    const Memory memory(a[5], *dy.t, stream);
+    at::Tensor dw = memory.result({dy.cols, k}, type), db, space;
+    if (bias) db = memory.result({dy.cols}, type);
     accerl_weight_grad_args g = {};
     g.dy = dy.p;
     g.q = (const int8_t *)q.p;
@@ -481,11 +521,10 @@ PyObject *py_ckpt_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     g.out_dtype = dtype_code(type);
     g.workspace_bytes = accerl_ckpt_weight_grad_workspace(&g);
     if (g.workspace_bytes) {
-        space = empty({g.workspace_bytes}, at::kByte, *dy.t);
+        space = memory.workspace(g.workspace_bytes);
         g.workspace = space.data_ptr();
     }
     const accerl_status st = on_device_of(*dy.t, [&] { return accerl_ckpt_weight_grad(&g, stream); });
-    keep_for(space, a[5], stream);
     if (st != ACCERL_OK) return PyLong_FromLong(st);
     PyObject *dbo = Py_None;
     if (bias) dbo = wrapped(std::move(db));
@@ -512,9 +551,10 @@ PyObject *py_policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
         Py_RETURN_NONE;
     const double c[4] = {PyFloat_AsDouble(a[7]), PyFloat_AsDouble(a[8]), PyFloat_AsDouble(a[9]), PyFloat_AsDouble(a[10])};
     if (not_for_us()) Py_RETURN_NONE;
+    const Memory memory(a[12], like, stream);
     at::Tensor grad;
     if (a[11] == Py_True) {
-        grad = at::detail::empty_strided_cuda({z.rows, z.cols}, {z.ld, 1}, like.scalar_type(), like.device());
+        grad = memory.result_strided({z.rows, z.cols}, {z.ld, 1}, like.scalar_type());
         g.grad = grad.data_ptr();
         g.ld_grad = z.ld;
     } else if (a[11] != Py_False) {
@@ -523,7 +563,7 @@ PyObject *py_policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
         g.ld_grad = gr.ld;
     }
     const int64_t t = z.rows;
-    at::Tensor f = empty({8 + 5 * t}, at::kFloat, like);
+    at::Tensor f = memory.result({8 + 5 * t}, at::kFloat);
     float *fp = (float *)f.data_ptr();
     g.logits = z.p;
     g.logits_ref = zr.p;
