@@ -499,7 +499,7 @@ accerl_status accerl_policy_loss(const accerl_policy_loss_args *args, void *cuda
  * Gradient of a layer's weights from the checkpoint of its input, on the tensor cores:
  *   dw[n][k] = sum_t dy[t][n] x^[t][k],   db[n] = sum_t dy[t][n]
  * with products of the exact 16-bit values and sums in fp32, in an order that depends on the sizes alone (the same
- * call gives the same bits), rounded once to out_dtype.  `accumulate`: added to what dw and db hold (out_dtype
+ * call gives the same bits, and dw's are the same whether db is wanted), rounded once to out_dtype.  `accumulate`: added to what dw and db hold (out_dtype
  * ACCERL_F32 only), as a sum over micro-batches needs it.  With ACCERL_F16 gradients x^ is taken as fp16: beyond its
  * range it is infinite.  Needs bf16 or fp16 dy.
  */

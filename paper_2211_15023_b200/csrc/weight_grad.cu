@@ -855,7 +855,7 @@ struct Plan {
 Plan plan_of(const accerl_weight_grad_args *a)
 {
     Plan r;
-    const long long n_tiles = (a->n + kPairTile - 1LL) / kPairTile, k_tiles = (a->k + kPairTile - 1LL) / kPairTile;  // (whether db is wanted changes no bit of dw)
+    const long long n_tiles = (a->n + kPairTile - 1LL) / kPairTile, k_tiles = (a->k + kPairTile - 1LL) / kPairTile;  // (whether db is wanted does not count: it is to change no bit of dw)
     r.pair = n_tiles * k_tiles >= 111;  // three tiles for every two pairs of a B200's 148 SMs
     r.plain = r.pair && n_tiles >= 5;
     if (((uintptr_t)a->dy & 15) || a->ld_dy % 8) r.dy_bytes = (2LL * a->tokens * padded_n(a->n) + 255) / 256 * 256;
@@ -953,7 +953,12 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     }
     p.tiles = (int)tiles;
     const int stages = (a->tokens + kTokens - 1) / kTokens;
-    const int share = pair ? 2 : std::max(1, std::min({kMaxShare, sm_count / p.tiles, stages / 2}));
+    // CTAs a tile of dw: the same whether db is wanted or not, and so the order of dw's sums.  As many as let db's tiles run beside
+    // dw's (more do not pay without db either: not all clusters of three or more then run at once, 2048 x 768 x 768 takes 26.6 us
+    // by fours, 16.4 by threes).  But two where dw's tiles alone leave room for two: db's tiles come second then (8192 x 1024 x 2304
+    // with / without db 74 / 45 us by twos, 78 / 78 by ones; 2048 x 512 x 2304 30.7 / 20.5 and 26.7 / 26.7).
+    const int dw_tiles = p.n_tiles * p.k_tiles, alone = sm_count / dw_tiles, with_db = sm_count / (dw_tiles + p.n_tiles);
+    const int share = pair ? 2 : std::max(1, std::min({kMaxShare, alone == 2 ? alone : with_db, stages / 2}));
     const unsigned grid = pair        ? 2u * (unsigned)std::min(p.tiles, sm_count / 2)
                           : share > 1 ? (unsigned)(p.tiles * share) : (unsigned)std::min(p.tiles, sm_count);
     // (never less than a pair's CTA takes: these kernels hold all of tensor memory, and a cluster of which one CTA waits for
