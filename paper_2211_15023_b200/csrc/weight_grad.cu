@@ -824,7 +824,17 @@ __global__ void __launch_bounds__(256) realign_kernel(const uint16_t *__restrict
 {
     for (long long t = blockIdx.y; t < tokens; t += gridDim.y)
         for (int i = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 8; i < n; i += (int)(gridDim.x * blockDim.x) * 8) {
-            const uint4 v = load_piece<__half>(reinterpret_cast<const __half *>(src + t * ld_src), i, n, 0.f);
+            const uint16_t *row = src + t * ld_src + i;
+            uint4 v;
+            if (i + 8 <= n) {
+                v = load16(row);
+            } else {  // (bits, whichever type they are of)
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    w[k] = (i + 2 * k < n ? (uint32_t)row[2 * k] : 0u) | (i + 2 * k + 1 < n ? (uint32_t)row[2 * k + 1] << 16 : 0u);
+                v = make_uint4(w[0], w[1], w[2], w[3]);
+            }
             *reinterpret_cast<uint4 *>(dst + t * ld_dst + i) = v;
         }
 }

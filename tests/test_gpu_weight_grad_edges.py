@@ -22,3 +22,28 @@ def test_dw_is_the_same_whether_db_is_wanted(t, n, k, out):
     assert none is None and torch.equal(dw, alone)
     want, mag = sums(dy, ckpt, k)
     check((dw, db), want, mag, TYPES[out])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, 0.9, 0.24])
+def test_gradients_beyond_the_ordinary_in_rows_off_16_bytes(dtype, value):
+    """Infinities and values near the type's end in the last columns of rows that are copied for the TMA: they keep their bits.
+    (0.24: bf16 values whose bits are an infinity's or a NaN's of fp16.)"""
+    import paper_2211_15023_b200 as P
+    t, n, k = 70, 37, 64
+    info = torch.finfo(TYPES[dtype])
+    dy, ckpt = inputs(t, n, k, TYPES[dtype], 5, pad=2)
+    dy[11, 36] = dy[12, 33] = dy[13, 35] = value if math.isinf(value) else value * info.max if value > 0.5 else 2.0 ** 122 if dtype == "bf16" else 1.0
+    dw, db = P.ckpt_weight_grad(dy, ckpt, k, out_dtype=torch.float32)
+    x = P.ckpt_load(ckpt, k, torch.float32).double()
+    want, want_b = dy.double().t() @ x, dy.double().sum(0)
+    if math.isinf(value):
+        for got, w in ((dw, want), (db, want_b)):
+            assert torch.equal(torch.isnan(got), torch.isnan(w)) and torch.equal(torch.isinf(got), torch.isinf(w))
+            assert torch.equal(got[torch.isinf(got)], w[torch.isinf(w)].float())
+        return
+    # (sums in fp32 of at most 70 products: each addition cuts off at most 2^-22 of what it holds)
+    for got, w, mag in ((dw, want, dy.double().abs().t() @ x.abs()), (db, want_b, dy.double().abs().sum(0))):
+        fits = mag < torch.finfo(torch.float32).max  # (0.9 of bf16's largest times a value above 1 is infinite)
+        assert torch.isfinite(got[fits]).all() and ((got.double() - w).abs()[fits] <= 70 * 2.0 ** -22 * mag[fits]).all()
+        assert torch.isinf(got[w.abs() > 1.001 * torch.finfo(torch.float32).max]).all()
