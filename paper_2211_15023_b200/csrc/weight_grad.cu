@@ -134,9 +134,15 @@ __device__ __forceinline__ void put_values(uint32_t dec, int b, int t, const uin
 // norm (4e-7 with an fp32 product's rounding).  So an accumulator covers at most kChunk stages, and its parts are
 // added in fp32 by the warps that write: 5e-7.  The sum lies in the other half of tensor memory (adding in memory instead
 // cost 634 us with loads and 379 with reductions, for 8192 x 4096 x 4096), and the tensor cores wait while a part is
-// added, some 5 % of a part's time.  Results of one part, and 16-bit ones, have two accumulators in turn instead.
-constexpr int kChunk = 24;
-__host__ __device__ __forceinline__ int chunks_of(int out_dtype, int stages) { return out_dtype == ACCERL_F32 ? (stages + kChunk - 1) / kChunk : 1; }
+// added, some 5 % of a part's time.  Results of one part have two accumulators in turn instead.  16-bit results are in one
+// part up to kChunk16 stages (8192 tokens), whose loss is far below their rounding; without an end to it the sums of 2^22 tokens
+// of one sign would lose more than half a step of fp16.
+constexpr int kChunk = 24, kChunk16 = 128;
+__host__ __device__ __forceinline__ int chunks_of(int out_dtype, int stages)
+{
+    const int most = out_dtype == ACCERL_F32 ? kChunk : kChunk16;
+    return (stages + most - 1) / most;
+}
 
 // the accumulators in turn: two, or always the first
 struct Acc {

@@ -47,3 +47,25 @@ def test_gradients_beyond_the_ordinary_in_rows_off_16_bytes(dtype, value):
         fits = mag < torch.finfo(torch.float32).max  # (0.9 of bf16's largest times a value above 1 is infinite)
         assert torch.isfinite(got[fits]).all() and ((got.double() - w).abs()[fits] <= 70 * 2.0 ** -22 * mag[fits]).all()
         assert torch.isinf(got[w.abs() > 1.001 * torch.finfo(torch.float32).max]).all()
+
+
+@pytest.mark.parametrize("t,n,k", [(1 << 22, 64, 64), (40000, 2050, 2570), (40000, 520, 15000)])
+@pytest.mark.parametrize("dtype,out", [("fp16", "fp16"), ("bf16", "bf16"), ("fp16", "fp32")])
+def test_long_sums_of_one_sign(t, n, k, dtype, out):
+    """A sum in the tensor cores is cut off at each of its additions (16 tokens), by less than 2^-23 of itself: a part of
+    8192 tokens loses less than 512 2^-23 = 6.2e-5, the parts' additions in fp32 next to nothing."""
+    import paper_2211_15023_b200 as P
+    g = torch.Generator("cuda").manual_seed(t)
+    make = lambda c, scale: ((torch.rand((t, c), device="cuda", generator=g) + 1.0) * scale).to(TYPES[dtype])  # noqa: E731
+    dy, (_, ckpt) = make(n, 0.125 * 16384.0 / t), P.ckpt_save(make(k, 1.0))
+    dw, db = P.ckpt_weight_grad(dy, ckpt, k, out_dtype=TYPES[out])
+    P.device_check()
+    want, want_b = torch.zeros((n, k), device="cuda", dtype=torch.float64), torch.zeros(n, device="cuda", dtype=torch.float64)
+    x = P.ckpt_load(ckpt, k, TYPES[dtype])
+    for i in range(0, t, 1 << 16):
+        d = dy[i:i + (1 << 16)].double()
+        want += d.t() @ x[i:i + (1 << 16)].double()
+        want_b += d.sum(0)
+    half = torch.finfo(TYPES[out]).eps / 2
+    for got, w in ((dw, want), (db, want_b)):
+        assert ((got.double() - w).abs() <= (half * 1.01 + 6.2e-5) * w.abs()).all()
