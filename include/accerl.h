@@ -511,7 +511,7 @@ typedef struct {
     void *db;         /* [n] of out_dtype, or NULL */
     void *workspace;  /* accerl_ckpt_weight_grad_workspace bytes, 256-byte aligned; may be NULL where that is 0 */
     int64_t ld_dy, ld_q, ld_e, ld_dw, workspace_bytes;
-    int32_t tokens, n, k;
+    int32_t tokens, n, k; /* tokens below 2^31 - 2^16, n and k at most 2^27, n * k at most 2^40 */
     int32_t dy_dtype, out_dtype, accumulate;
 } accerl_weight_grad_args;
 
@@ -554,7 +554,7 @@ typedef struct {
     void *y;               /* [tokens][n] */
     void *workspace;       /* accerl_linear_i8_workspace bytes, 256-byte aligned; NULL where that is 0 */
     int64_t ld_x, ld_w, ld_y, workspace_bytes;
-    int32_t tokens, n, k;  /* k at most 131072 */
+    int32_t tokens, n, k;  /* k at most 131072, tokens and n below 2^31 - 2^16 */
     int32_t x_dtype, y_dtype, relu;
 } accerl_linear_i8_args;
 

@@ -10,6 +10,9 @@
 
 namespace accerl {
 
+// rows of the products: tiles past the last row are counted in an int
+constexpr int kMostRows = INT32_MAX - 65535;
+
 inline int dtype_size(int dtype) { return dtype == ACCERL_F32 ? 4 : 2; }
 inline bool good_dtype(int dtype) { return dtype == ACCERL_F32 || dtype == ACCERL_BF16 || dtype == ACCERL_F16; }
 

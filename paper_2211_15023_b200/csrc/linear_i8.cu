@@ -756,8 +756,8 @@ extern "C" accerl_status accerl_linear_i8(const accerl_linear_i8_args *a, void *
         set_error("linear_i8: tokens * n is too large");
         return ACCERL_ERR_INVALID_ARG;
     }
-    if (a->tokens < 1 || a->n < 1 || a->k < 1 || a->k > 131072) {
-        set_error("linear_i8: tokens, n and k must be positive, k at most 131072 (an int32 sum of products of 127)");
+    if (a->tokens < 1 || a->n < 1 || a->k < 1 || a->k > 131072 || a->tokens >= kMostRows || a->n >= kMostRows) {
+        set_error("linear_i8: tokens, n and k must be positive, k at most 131072 (an int32 sum of products of 127), the others below 2^31 - 2^16");
         return ACCERL_ERR_INVALID_ARG;
     }
     const bool given = a->x_dtype == ACCERL_I8;

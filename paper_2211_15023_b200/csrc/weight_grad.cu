@@ -825,7 +825,7 @@ weight_grad_plain_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
 }
 
 // dy at rows of a multiple of 16 bytes, for the TMA
-__global__ void __launch_bounds__(256) realign_kernel(const uint16_t *__restrict__ src, long long ld_src, uint16_t *__restrict__ dst, int ld_dst,
+__global__ void __launch_bounds__(256) realign_kernel(const uint16_t *__restrict__ src, long long ld_src, uint16_t *__restrict__ dst, long long ld_dst,
                                                       int tokens, int n)
 {
     for (long long t = blockIdx.y; t < tokens; t += gridDim.y)
@@ -845,7 +845,7 @@ __global__ void __launch_bounds__(256) realign_kernel(const uint16_t *__restrict
         }
 }
 
-int padded_n(int n) { return (n + 7) / 8 * 8; }
+long long padded_n(long long n) { return (n + 7) / 8 * 8; }
 
 }  // namespace
 
@@ -894,8 +894,8 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
         set_error("ckpt_weight_grad: null argument");
         return ACCERL_ERR_INVALID_ARG;
     }
-    if (a->tokens < 1 || a->n < 1 || a->k < 1 || a->k > (1 << 27) || a->n > (1 << 27) || (long long)a->n * a->k > (1LL << 40)) {
-        set_error("ckpt_weight_grad: tokens, n and k must be positive, n and k at most 2^27, n * k at most 2^40");
+    if (a->tokens < 1 || a->tokens >= kMostRows || a->n < 1 || a->k < 1 || a->k > (1 << 27) || a->n > (1 << 27) || (long long)a->n * a->k > (1LL << 40)) {
+        set_error("ckpt_weight_grad: tokens, n and k must be positive, tokens below 2^31 - 2^16, n and k at most 2^27, n * k at most 2^40");
         return ACCERL_ERR_INVALID_ARG;
     }
     if (a->dy_dtype == ACCERL_F32) {
@@ -935,16 +935,6 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
                                  : tc_make_map(&mq, a->q, a->tokens, cols32, a->ld_q, kTokens, 128);
     if (s == ACCERL_OK) s = tc_make_map(&md, dy, a->tokens, 2 * a->n, 2 * ld_dy, kTokens, 128);
     if (s != ACCERL_OK) return s;
-    if (copy) {
-        const dim3 grid((unsigned)std::min((a->n + 2047) / 2048, 1024), (unsigned)std::min(a->tokens, 65535));
-        realign_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(a->dy), a->ld_dy, static_cast<uint16_t *>(a->workspace),
-                                             padded_n(a->n), a->tokens, a->n);
-        ACCERL_CUDA_TRY(cudaGetLastError());
-    }
-    if (plan.plain) {
-        s = accerl_ckpt_load(a->q, a->ld_q, a->e, a->ld_e, a->tokens, a->k, x, padded_n(a->k), a->dy_dtype, cuda_stream);
-        if (s != ACCERL_OK) return s;
-    }
     GradArgs p;
     p.e = a->e;
     p.dw = a->dw;
@@ -969,6 +959,10 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     }
     p.tiles = (int)tiles;
     const int stages = (a->tokens + kTokens - 1) / kTokens;
+    if ((tiles / std::max(1, sm_count / 2) + 1) * stages > (1 << 30)) {  // (a CTA counts its stages in an int)
+        set_error("ckpt_weight_grad: tokens * n * k is too large");
+        return ACCERL_ERR_INVALID_ARG;
+    }
     // CTAs a tile of dw: the same whether db is wanted or not, and so the order of dw's sums.  As many as let db's tiles run beside
     // dw's (more do not pay without db either: not all clusters of three or more then run at once, 2048 x 768 x 768 takes 26.6 us
     // by fours, 16.4 by threes).  But two where dw's tiles alone leave room for two: db's tiles come second then (8192 x 1024 x 2304
@@ -983,6 +977,16 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     const size_t smem = plan.plain ? kPlainSmem
                         : pair     ? kPairSmem
                                    : std::max(kPairSmem, 1024 + kRaw * kRawBytes + kDec * kDecBytes + (size_t)kDy * p.n_tile * 2 * kTokens);
+    if (copy) {
+        const dim3 grid((unsigned)std::min((a->n + 2047) / 2048, 1024), (unsigned)std::min(a->tokens, 65535));
+        realign_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(a->dy), a->ld_dy, static_cast<uint16_t *>(a->workspace),
+                                             padded_n(a->n), a->tokens, a->n);
+        ACCERL_CUDA_TRY(cudaGetLastError());
+    }
+    if (plan.plain) {
+        s = accerl_ckpt_load(a->q, a->ld_q, a->e, a->ld_e, a->tokens, a->k, x, padded_n(a->k), a->dy_dtype, cuda_stream);
+        if (s != ACCERL_OK) return s;
+    }
     const bool half = a->dy_dtype == ACCERL_F16;
     const auto kernel = plan.plain ? (half ? weight_grad_plain_kernel<__half> : weight_grad_plain_kernel<__nv_bfloat16>)
                         : pair ? (half ? weight_grad_pair_kernel<__half> : weight_grad_pair_kernel<__nv_bfloat16>)
