@@ -138,6 +138,8 @@ __global__ void __launch_bounds__(kThreads, 5) ckpt_kernel(const __grid_constant
     uint32_t code[MODE != kSave ? kAhead : 1][kWords];
     int kept = 0;
     if constexpr (MODE != kSave) kept = lane < n32 / 32 ? e[lane] : 0;  // a unit has at most 32 blocks
+    // (slopes far out are 0 or 1: values there stay finite, so that 0 times them is 0)
+    if constexpr (MODE == kBackward && (ACT == ACCERL_ACT_GELU || ACT == ACCERL_ACT_SILU)) kept = kept == 255 ? 255 : min(kept, 200);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
         const int at = (i * 32 + lane) * V;
