@@ -589,10 +589,10 @@ typedef enum { ACCERL_ACT_NONE = 0, ACCERL_ACT_RELU = 1, ACCERL_ACT_GELU = 2, AC
  *   q   int8_t [rows][ld_q], e uint8_t [rows][ld_e]; with cols32 = cols rounded up to 32: ld_q >= cols32 and a
  *       multiple of 16, ld_e >= cols32 / 32, q aligned to 16 bytes.  Columns cols .. cols32 of q are written as 0.
  *
- * accerl_ckpt_save          y = act(x) (y may be x itself, or NULL), and the checkpoint of x, in one pass
+ * accerl_ckpt_save          y = act(x) (y may be x itself, with the same ld, or NULL), and the checkpoint of x, in one pass
  * accerl_ckpt_load          x = x^; infinite where x^ is beyond `dtype`: fp16 from 65520 on (a value kept from 65280 on reads
  *                           back as 65536), bf16 and fp32 where a value kept from 255/256 2^128 on rounded to 2^128
- * accerl_ckpt_act_backward  dx = dy act'(x^) (dx may be dy itself); relu'(0) = 0, GELU is x Phi(x)
+ * accerl_ckpt_act_backward  dx = dy act'(x^) (dx may be dy itself, with the same ld); relu'(0) = 0, GELU is x Phi(x)
  * Results are computed in fp32 and rounded once to `dtype` (an accerl_dtype; the same for both arrays of a call).
  * GELU's Phi has a relative error below 2e-6 (fp32) or 2e-5 (16-bit types) down to x = -13.
  * Asynchronous on `cuda_stream`, one launch.  Errors: INVALID_ARG, CUDA.

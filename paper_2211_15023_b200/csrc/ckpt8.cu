@@ -299,6 +299,10 @@ extern "C" accerl_status accerl_ckpt_save(const void *x, int64_t ld_x, int32_t d
     if (!good_sizes(who, rows, cols, dtype, act) || !good_rows(who, "x", x, ld_x, cols, dtype) ||
         (y && !good_rows(who, "y", y, ld_y, cols, dtype)) || !good_ckpt(who, q, ld_q, e, ld_e, cols))
         return ACCERL_ERR_INVALID_ARG;
+    if (y == x && ld_y != ld_x && rows > 1) {
+        set_error("ckpt_save: y in place of x needs the same ld");
+        return ACCERL_ERR_INVALID_ARG;
+    }
     CkptArgs p{x, y, q, e, ld_x, ld_y, ld_q, ld_e, rows, cols, 0, 0, 0};
     return launch<kSave>(p, dtype, act, cuda_stream);
 }
@@ -322,6 +326,10 @@ extern "C" accerl_status accerl_ckpt_act_backward(const void *dy, int64_t ld_dy,
     if (!good_sizes(who, rows, cols, dtype, act) || !good_rows(who, "dy", dy, ld_dy, cols, dtype) ||
         !good_rows(who, "dx", dx, ld_dx, cols, dtype) || !good_ckpt(who, q, ld_q, e, ld_e, cols))
         return ACCERL_ERR_INVALID_ARG;
+    if (dx == dy && ld_dx != ld_dy && rows > 1) {
+        set_error("ckpt_act_backward: dx in place of dy needs the same ld");
+        return ACCERL_ERR_INVALID_ARG;
+    }
     CkptArgs p{dy, dx, const_cast<int8_t *>(q), const_cast<uint8_t *>(e), ld_dy, ld_dx, ld_q, ld_e, rows, cols, 0, 0, 0};
     return launch<kBackward>(p, dtype, act, cuda_stream);
 }

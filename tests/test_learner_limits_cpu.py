@@ -28,3 +28,11 @@ def test_ckpt_weight_grad_refuses_tokens_whose_stages_pass_int32(lib, change):  
 def test_the_workspace_of_the_largest_sizes_is_not_negative(lib, n, k):  # noqa: F811
     need = lib.accerl_ckpt_weight_grad_workspace(C.byref(grad_args(n=n, k=k, ld_dy=n + 1, dy=AT + 2)))
     assert need >= 2 * 4 * n
+
+
+def test_checkpoints_in_place_need_the_same_row_distance(lib):  # noqa: F811
+    from test_learner_args_cpu import save_args
+    a = save_args(y=AT, ld_y=48)
+    assert lib.accerl_ckpt_save(*a.values()) == INVALID and b"same ld" in lib.accerl_last_error()
+    args = [a[k] for k in ("x", "ld_x", "dtype", "q", "ld_q", "e", "ld_e", "rows", "cols", "act", "y", "ld_y", "stream")]
+    assert lib.accerl_ckpt_act_backward(*args) == INVALID and b"same ld" in lib.accerl_last_error()
