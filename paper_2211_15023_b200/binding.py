@@ -358,7 +358,8 @@ def policy_loss(logits, actions, logp_old, advantages, weights=None, logits_ref=
     assert logp_old is not None and advantages is not None
     memory = _Memory(logits, stream)
     if grad is True:
-        grad = memory.result(logits.shape, logits.dtype, (_ld(logits), 1))
+        # rows as far apart as the logits', which then lie alike to 16 bytes; but not those of the last token of sequences
+        grad = memory.result(logits.shape, logits.dtype, (_ld(logits) if _ld(logits) < 2 * v else -(-v // 8) * 8, 1))
     elif grad is False:
         grad = None
     if grad is not None:

@@ -554,9 +554,10 @@ PyObject *py_policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
     const Memory memory(a[12], like, stream);
     at::Tensor grad;
     if (a[11] == Py_True) {
-        grad = memory.result_strided({z.rows, z.cols}, {z.ld, 1}, like.scalar_type());
+        // rows as far apart as the logits', which then lie alike to 16 bytes; but not those of the last token of sequences
+        g.ld_grad = z.ld < 2 * z.cols ? z.ld : (z.cols + 7) / 8 * 8;
+        grad = memory.result_strided({z.rows, z.cols}, {g.ld_grad, 1}, like.scalar_type());
         g.grad = grad.data_ptr();
-        g.ld_grad = z.ld;
     } else if (a[11] != Py_False) {
         if (!rows_of(a[11], &gr) || gr.code != z.code || gr.rows != z.rows || gr.cols != z.cols || !same_device(*gr.t, like)) Py_RETURN_NONE;
         g.grad = gr.p;

@@ -218,3 +218,25 @@ def test_a_reference_far_below_where_the_policy_is_not(t, v, value, dtype):
     assert not g[[0, 1, 2], -pad:].any()
     again = loss(s, grad=s["z"], kl_coef=0.03125, entropy_coef=0.02)
     assert torch.equal(torch.nan_to_num(again["grad"]), torch.nan_to_num(out["grad"])) and torch.equal(again["kl"], out["kl"])
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_the_gradient_of_each_sequence_s_last_token_takes_its_own_memory(native, monkeypatch):
+    """Rows of a [batch, length, vocabulary] tensor that lie a whole sequence apart; on both ways in."""
+    import types
+
+    import paper_2211_15023_b200 as P
+    from paper_2211_15023_b200 import binding
+    s = inputs(64, 5003, torch.bfloat16, 1)
+    whole = torch.zeros((64, 40, 5003), device="cuda", dtype=torch.bfloat16)
+    whole[:, -1] = s["z"]
+    call = lambda z: P.policy_loss(z, s["a"], s["logp_old"], s["adv"], weights=s["w"], entropy_coef=0.1)  # noqa: E731
+    want = call(s["z"])
+    if not native:
+        monkeypatch.setattr(binding, "_CALLS", types.SimpleNamespace(policy_loss=lambda *a: None))
+    before = torch.cuda.memory_allocated()
+    got = call(whole[:, -1])
+    assert torch.cuda.memory_allocated() - before < 2 * 64 * 5003 * 2
+    # (rows that lie otherwise to 16 bytes are summed in another order: a gradient may round to its neighbour)
+    torch.testing.assert_close(got["grad"].float(), want["grad"].float(), rtol=2.0 ** -7, atol=1e-8)
+    torch.testing.assert_close(got["stats"], want["stats"], rtol=1e-5, atol=1e-6)
