@@ -94,7 +94,7 @@ __device__ __forceinline__ RowResult<R> finish_row(const LossArgs &p, long long 
         const R lo = (R)1 - (R)p.clip_low, hi = (R)1 + (R)p.clip_high;
         const R rc = r < lo ? lo : r > hi ? hi : r;  // (a NaN stays one)
         R plain = r * adv;
-        if (r == (R)INFINITY) {  // (its product may be a number all the same)
+        if (__builtin_expect(r == (R)INFINITY, 0)) {  // (its product may be a number all the same)
             const R h = exp_of(x * (R)0.5);
             plain = adv == (R)0 ? (R)0 : h * adv * h;
         }
@@ -366,16 +366,17 @@ __device__ __forceinline__ uint32_t min_words(uint32_t a, uint32_t b)
         return *reinterpret_cast<const uint32_t *>(&m);
     }
 }
-// one or two logits: is one of the policy's above the low value where the reference's is below it?
-template <typename T>
+// one or two logits: is one of the policy's above the low value where the reference's is below it (OR_AT: or there)?
+template <typename T, bool OR_AT = false>
 __device__ __forceinline__ bool meets(uint32_t z, uint32_t r, uint32_t low)
 {
     if constexpr (sizeof(T) == 4) {
-        return __uint_as_float(z) > __uint_as_float(low) && __uint_as_float(r) < __uint_as_float(low);
+        const float l = __uint_as_float(low), q = __uint_as_float(r);
+        return __uint_as_float(z) > l && (OR_AT ? q <= l : q < l);
     } else {
         using T2 = std::conditional_t<std::is_same<T, __half>::value, __half2, __nv_bfloat162>;
-        const T2 l = *reinterpret_cast<const T2 *>(&low);
-        return (__hgt2_mask(*reinterpret_cast<const T2 *>(&z), l) & __hlt2_mask(*reinterpret_cast<const T2 *>(&r), l)) != 0;
+        const T2 l = *reinterpret_cast<const T2 *>(&low), q = *reinterpret_cast<const T2 *>(&r);
+        return (__hgt2_mask(*reinterpret_cast<const T2 *>(&z), l) & (OR_AT ? __hle2_mask(q, l) : __hlt2_mask(q, l))) != 0;
     }
 }
 // What -inf, and anything below, is taken for (finite, so that its probability of 0 times its logarithm is 0), as a word of
@@ -440,7 +441,7 @@ __device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, fl
     const float d = (float)(so - ss) / fs, ratio = REF ? (fabsf(d) < 0.5f ? log1pf(d) * kLog2e : (float)(lso - log2_of(ss))) : 0.f;
     const float H = (float)kLn2 * (float)(lso - (double)((float)st * inv));
     float kl = REF ? (float)kLn2 * ((float)sd * inv - ratio) : 0.f;
-    if (REF && fabsf(kl) > 1e37f) kl = (float)(kLn2 * (double)inv * sd - kLn2 * (double)ratio);  // (its parts may lie beyond fp32)
+    if (REF && __builtin_expect(fabsf(kl) > 1e37f, 0)) kl = (float)(kLn2 * (double)inv * sd - kLn2 * (double)ratio);  // (its parts may lie beyond fp32)
     const double at_c = (double)za - (double)C + kLn2 * (double)excess;  // (apart from the sums, which take longer)
     const double logp = empty ? (double)-INFINITY : known ? at_c - kLn2 * lso : (double)NAN;
     const RowResult<float> f = finish_row<float>(p, row, logp, kl, H, empty, writer);
@@ -530,6 +531,41 @@ __device__ __forceinline__ void odd_sums(const T *z_row, const T *r_row, int beg
             sum[3] += (double)e * (t - tr);
         }
     }
+}
+
+// Does the policy lie above the low value where the reference lies below?  A thread's pieces of a part, both raised; the
+// reference's memory is looked at only where its word is at the low value.  Elements begin .. end of `r` are the row's.
+template <typename T>
+__device__ __noinline__ bool odd_meets(const uint4 *z_s, const uint4 *r_s, const T *r, int n, int begin, int end)
+{
+    constexpr int V = Row<T>::kVec;
+    const uint32_t low_w = low_word<T>();
+    for (int j = threadIdx.x; j < n; j += blockDim.x) {
+        const uint4 z = z_s[j], q = r_s[j];
+        bool may = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) may |= meets<T, true>(words(z)[i], words(q)[i], low_w);
+        if (!may) continue;
+        float zv[V];
+        unpack<T>(z, zv);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int v = j * V + k;
+            if (v >= begin && v < end && zv[k] > low_value<T>() && to_float(r[v]) < low_value<T>()) return true;
+        }
+    }
+    return false;
+}
+
+// the last of them, of a CTA's part: a warp's share
+template <typename T>
+__device__ __noinline__ double odd_part(const T *z_row, const T *r_row, int begin, int end, float c, float cr)
+{
+    double sum[4];
+    odd_sums(z_row, r_row, begin, end, (int)blockDim.x, c, cr, sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum[3] += __shfl_xor_sync(0xffffffffu, sum[3], o);
+    return sum[3];
 }
 
 // and their gradients (f: of the row)
@@ -706,7 +742,7 @@ __device__ __forceinline__ double rebase_difference(float d, float dr, const Par
 // TB/s; 2048 of 128001 with a reference: 497 us.
 constexpr int kMaxCluster = 16, kRowThreads = 256;
 template <typename T, bool REF>
-__global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_constant__ LossArgs p)
+__global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_constant__ LossArgs p)
 {
     constexpr int V = Row<T>::kVec;
     extern __shared__ __align__(128) uint4 s_piece[];  // [REF ? 2 : 1][pieces of a part]
@@ -776,24 +812,20 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
     // a pass of the part: -inf raised to the low value, the maximum; in every thread of the CTA
     bool lower = false, odd = false;  // the reference below the low value; and the policy above it there
     auto prepare = [&](uint4 *x_s, int which) {
-        uint32_t m = low_w;
+        uint32_t m = low_w, least = low_w;
         for (int j = threadIdx.x; j < n; j += blockDim.x) {
-            const uint4 was = x_s[j];
-            uint4 v = was;
-            uint32_t below = 0;
+            uint4 v = x_s[j];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                if (which) least = min_words<T>(least, words(v)[i]);
                 words(v)[i] = max_words<T>(words(v)[i], low_w);
                 m = max_words<T>(m, words(v)[i]);
-                below |= words(v)[i] ^ words(was)[i];
-            }
-            if (which && below) {
-                lower = true;
-                const uint4 z = z_s[j];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) odd |= meets<T>(words(z)[i], words(was)[i], low_w);
             }
             x_s[j] = v;
+        }
+        if (which && word_min<T>(least) < low[0]) {  // (apart from the loop above, which is every row's)
+            lower = true;
+            odd = odd_meets<T>(z_s, x_s, r_row + first, n, first < 0 ? -first : 0, p.A - first);
         }
         float c = word_max<T>(m);
 #pragma unroll
@@ -847,11 +879,8 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
     }
     const int from = max(first, 0) + (int)threadIdx.x, end = min(first + n * V, p.A);
     if (REF && odd) {
-        double sum[4];
-        odd_sums(z_row, r_row, from, end, (int)blockDim.x, c, cr, sum);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum[3] += __shfl_xor_sync(0xffffffffu, sum[3], o);
-        if (lane == 0) s_odd[warp] = sum[3];
+        const double sum = odd_part(z_row, r_row, from, end, c, cr);
+        if (lane == 0) s_odd[warp] = sum;
     }
     float sums[4] = {so, st, ss, sd};
 #pragma unroll
@@ -907,7 +936,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) loss_rows_kernel(const __grid_
     if (g_row) {
         const RowCoef f = s_row;
         if (REF && odd) {
-            odd_gradient(z_row, r_row, g_row, from, end, (int)blockDim.x, a, f);
+            odd_gradient(z_row, r_row, g_row, from, end, (int)blockDim.x, a, s_row);
         }
         const float sh = shift_of(base, f.c), shr = shift_of(base_r, f.cr);
 #pragma unroll 2
