@@ -948,7 +948,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
 
 // ------------------------------------------------------------------- many very long rows with a reference
 // A CTA per row, persistent, the row streaming through a ring in shared memory twice: for the sums, and, backwards, for the
-// gradient.  The second time it comes from L2, which holds the rows of all CTAs (the launch sees to that).  Against
+// gradient.  The second time it comes from L2, as far as that holds the rows of all CTAs.  Against
 // the kernel above a row's end (barriers, one warp's arithmetic: some 2 us in which an SM does little else) comes once for
 // a whole row instead of once for an eighth of one, and the loads of what follows go on meanwhile: 497 -> 414 us for
 // 2048 rows of 128001.  It is bound by the instructions a pair of logits (some 33; 16 warps instead of 24: 492 us), so every
@@ -1251,11 +1251,14 @@ cudaError_t launch_rows(LossArgs &p, int sm_count, cudaStream_t st)
         kernel<<<(unsigned)(((long long)p.rows + 3) / 4), 128, 0, st>>>(p);
         return cudaGetLastError();
     }
-    // With a reference, rows from 256 KB on (both arrays'), one for every SM or more, all SMs' rows in two thirds of L2: streamed.
+    // With a reference, rows from 256 KB on (both arrays'), one for every SM or more: streamed.  By the cluster kernel / streamed, us:
+    // 148 rows of 128000 bf16 51 / 41, 150 51 / 64 (a second turn for two rows), 200 64 / 66, 300 86 / 92, 444 120 / 98, 888 225 / 184;
+    // 2048 of 151936 679 / 467, of 262128 (whose second reading L2 does not serve) 1118 / 820; 2048 of 64000 fp32 414 / 339; shorter
+    // ones, 4096 of 32000 bf16, 225 / 274.
     if constexpr (REF) {
         const long long row_bytes = 32LL * pieces;
         const bool alike = !((((uintptr_t)p.ref ^ (uintptr_t)p.logits) | (uintptr_t)((p.ld - p.ld_ref) * (long long)sizeof(T))) & 15);
-        if (p.rows >= sm_count && row_bytes >= 256 * 1024 && row_bytes * sm_count <= 84LL << 20 && alike) {
+        if (p.rows >= sm_count && row_bytes >= 256 * 1024 && alike) {
             const auto kernel = loss_stream_kernel<T>;
             const cudaError_t e = allow_smem((const void *)kernel, kStreamSmem);
             if (e != cudaSuccess) return e;

@@ -240,3 +240,17 @@ def test_the_gradient_of_each_sequence_s_last_token_takes_its_own_memory(native,
     # (rows that lie otherwise to 16 bytes are summed in another order: a gradient may round to its neighbour)
     torch.testing.assert_close(got["grad"].float(), want["grad"].float(), rtol=2.0 ** -7, atol=1e-8)
     torch.testing.assert_close(got["stats"], want["stats"], rtol=1e-5, atol=1e-6)
+
+
+@pytest.mark.parametrize("dtype,t,v", [("bf16", 301, 151937), ("fp16", 299, 262128), ("fp32", 150, 131072)])
+def test_streamed_rows_of_which_l2_does_not_hold_all(dtype, t, v):
+    import paper_2211_15023_b200 as P
+    s = inputs(t, v, TYPES[dtype], v)
+    out = loss(s, kl_coef=0.05, entropy_coef=0.02)
+    against_definition(s, out, TYPES[dtype], rows=6, kl_coef=0.05, entropy_coef=0.02)
+    few = {k: x[-40:] for k, x in s.items()}  # (fewer rows than SMs: a cluster a row)
+    other = loss(few, kl_coef=0.05, entropy_coef=0.02)
+    for k in ("logp", "kl", "entropy"):
+        torch.testing.assert_close(out[k][-40:], other[k], rtol=8e-6, atol=2e-5)
+    assert torch.equal(loss(s, grad=s["z"], kl_coef=0.05, entropy_coef=0.02)["grad"], out["grad"])
+    P.device_check()
