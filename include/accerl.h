@@ -484,7 +484,7 @@ typedef struct {
     float *kl;      /* [rows] */
     float *entropy; /* [rows] */
     float *stats;   /* [8]: loss, then the sums over t of w_t times pg, kl, H, (1 where the clamp decided); then
-                       sum w, the largest kl of a row of non-zero weight, sum w r */
+                       sum w, the largest kl of a row of non-zero weight (NaN if one is), sum w r */
     float *terms;   /* [rows][2]: pg and r of the row (workspace of the sums; 8-byte aligned) */
 } accerl_policy_loss_args;
 

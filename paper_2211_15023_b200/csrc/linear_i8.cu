@@ -512,7 +512,7 @@ accerl_status launch_few(const CUtensorMap &mw, const CUtensorMap &mx, LinearArg
 // SM in 128 cycles, half of what a single CTA's 128 x 256 tile would.  Two accumulators fill tensor memory, so that eight
 // warps (each 32 channels by 128 tokens, neighbouring lanes neighbours in a row of y) write a tile out while the next
 // one is computed; that takes some 8 instructions a value, and with four warps bounded the kernel (525 us for
-// 8192 x 4096 x 14336 with the quantiser).  Now 370 to 386 us, the product alone 283 (3.4 POP/s, tensor pipe 81 % busy).
+// 8192 x 4096 x 14336 with the quantiser).  Now 358 to 386 us by box (power), the product alone 283 (3.4 POP/s, tensor pipe 80 % busy).
 constexpr int kPairTile = 256, kPairStages = 6, kPairStage = 2 * 128 * 128, kPairOut = 8, kPairThreads = 32 * (kPairOut + 2);
 constexpr int kGroup = 8;  // token tiles whose channel tiles are walked together: their operands stay in L2
 

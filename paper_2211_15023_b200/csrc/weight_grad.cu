@@ -9,7 +9,7 @@
 // codes and 32 KB of dy; eight warps (two groups of them, in turn) turn the codes into 16 KB of operand (one block of 32 values a thread: a
 // byte permutation, a subtraction and a multiplication for every two); one thread issues the four instructions of the
 // stage; four warps write the previous tile out meanwhile (two accumulators of 256 columns fill tensor memory).
-// (8192 x 4096 x 4096 into fp32 388 us this way, 2047 x 2592 x 256 16 us.)
+// (2047 x 2592 x 256 14.4 us; 8192 x 4096 x 4096 into fp32 388 us this way, by the pairs below 256 to 273.)
 //
 // Where the tiles do not cover the chip the tokens are split over a cluster, whose CTAs add their parts through
 // distributed shared memory in a fixed order.  db is a tile of its own whose decoded operand is all ones.
@@ -947,6 +947,10 @@ extern "C" accerl_status accerl_ckpt_weight_grad(const accerl_weight_grad_args *
     p.out_dtype = a->out_dtype;
     p.accumulate = a->accumulate != 0;
     p.n_tile = pair ? kPairTile : std::min(256, (a->n + 63) / 64 * 64);
+    // Tiles of 128 channels where four times those of 256 fit the chip: smaller parts to exchange, and clusters of fewer CTAs, which
+    // find room more easily.  128 / 256 wide, tokens x channels x k, bf16 in a captured graph: 2047 x 256 x 2592 13.1 / 14.9 us,
+    // 512 x 256 x 2592 9.8 / 11.9, 2048 x 1024 x 512 13.1 / 26.4, 300 x 300 x 900 11.9 / 15.0; but 2048 x 768 x 384 16.6 / 14.1 and, where
+    // clusters have eight CTAs either way and twice as many do not run at once, 8192 x 256 x 1024 28.9 / 19.2.
     if (!pair && p.n_tile == 256 && ((long long)a->n + 255) / 256 * ((a->k + kTileK - 1) / kTileK) * 4 <= sm_count) p.n_tile = 128;
     p.n_tiles = (a->n + p.n_tile - 1) / p.n_tile;
     const int k_tile = pair ? kPairTile : kTileK;
