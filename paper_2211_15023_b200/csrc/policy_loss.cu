@@ -380,11 +380,22 @@ __device__ __forceinline__ bool meets(uint32_t z, uint32_t r, uint32_t low)
     }
 }
 // What -inf, and anything below, is taken for (finite, so that its probability of 0 times its logarithm is 0), as a word of
-// one or two elements; a row or part of a row with nothing above it is looked at again, see `low_part`.  Where the reference
-// lies below it and the policy above, its logarithm counts: such rows (parts) are `odd`, summed up and differentiated element by
-// element in double.
+// one or two elements.  Where the reference lies below it and the policy above, its logarithm counts: such rows (parts) are
+// `odd`, summed up and differentiated element by element in double.
 template <typename T>
-__device__ __forceinline__ constexpr float low_value() { return std::is_same<T, __half>::value ? -65504.f : -1e30f; }
+__device__ __forceinline__ constexpr float low_value() { return std::is_same<T, __half>::value ? -65504.f : -33554432.f; }
+// A row or part whose maximum is that far from 0 is `apart`: read again and kept relative to its maximum.  Below: so far down that
+// what is taken for the low value might have a probability.  Above, and below: the shift -c log2(e), rounded, is off by up to 2
+// at 2^25 (which cancels), and by more than an exponential bears further out.  (fp16 values are off by 2^-8 at most.)
+template <typename T>
+__device__ __forceinline__ bool is_below(float c) { return c <= 0.5f * low_value<T>(); }
+template <typename T>
+__device__ __forceinline__ bool is_above(float c) { return !std::is_same<T, __half>::value && c >= -0.5f * low_value<T>() && c != INFINITY; }
+template <typename T>
+__device__ __forceinline__ bool apart(float c) { return is_below<T>(c) || is_above<T>(c); }
+// A reference with this maximum makes a row odd: ordinary values may lie far below it, or it is infinite or a NaN.
+template <typename T>
+__device__ __forceinline__ bool too_high(float cr) { return std::is_same<T, __half>::value ? !(cr < INFINITY) : !(cr < -0.5f * low_value<T>()); }
 template <typename T>
 __device__ __forceinline__ uint32_t low_word()
 {
@@ -412,8 +423,6 @@ __device__ __forceinline__ const uint32_t *words(const uint4 &v) { return reinte
 // = e_v (k0 + kt t_v - kr t'_v), logarithms in base 2; and what the action's logit gets on top.
 struct RowCoef {
     float c, cr, k0, kt, kr, at_a;
-    // b of k0 + kt t - kr t' as a function of the pieces' values: one multiply-add a value
-    __device__ __forceinline__ float constant(float sh, float shr) const { return fmaf(kt, sh, fmaf(-kr, shr, k0)); }
 };
 // log2 of a positive sum: the exponent and the mantissa's logarithm apart, off by 1e-7 whatever its size
 __device__ __forceinline__ double log2_of(double x)
@@ -424,10 +433,14 @@ __device__ __forceinline__ double log2_of(double x)
     return (double)((hi >> 20) - 1023) + (double)log2f((float)m);
 }
 
+// -c log2(e) rounded, and not as part of a multiply-add: the same everywhere
+__device__ __forceinline__ float minus_log2(float c) { return -__fmul_rn(c, kLog2e); }
+
 // What every t of a row with maximum c is too large by, since its shift is rounded (half a step of c log2(e): at logits around
 // 1000 some 1e-4).  Sums, KL, entropy and the gradient hold differences of t and lose it, a log-probability does not.
 // (The rounding error of a product is a float, so this is exact.)
-__device__ __forceinline__ float excess_of(float base, float c, float sh) { return base == 0.f && c != -INFINITY ? fmaf(c, kLog2e, sh) : 0.f; }
+template <typename T>
+__device__ __forceinline__ float excess_of(float c) { return apart<T>(c) ? 0.f : fmaf(c, kLog2e, minus_log2(c)); }
 
 // `excess`: of the policy's t, of which the sums are made
 template <bool REF>
@@ -441,7 +454,10 @@ __device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, fl
     const float d = (float)(so - ss) / fs, ratio = REF ? (fabsf(d) < 0.5f ? log1pf(d) * kLog2e : (float)(lso - log2_of(ss))) : 0.f;
     const float H = (float)kLn2 * (float)(lso - (double)((float)st * inv));
     float kl = REF ? (float)kLn2 * ((float)sd * inv - ratio) : 0.f;
-    if (REF && __builtin_expect(fabsf(kl) > 1e37f, 0)) kl = (float)(kLn2 * (double)inv * sd - kLn2 * (double)ratio);  // (its parts may lie beyond fp32)
+    if (REF && __builtin_expect(fabsf(kl) > 1e37f, 0)) {  // (its parts may lie beyond fp32, it does only where it is infinite)
+        const double x = kLn2 * (double)inv * sd - kLn2 * (double)ratio;
+        kl = x < (double)INFINITY ? (float)fmin(x, 3.4028234663852886e38) : (float)x;
+    }
     const double at_c = (double)za - (double)C + kLn2 * (double)excess;  // (apart from the sums, which take longer)
     const double logp = empty ? (double)-INFINITY : known ? at_c - kLn2 * lso : (double)NAN;
     const RowResult<float> f = finish_row<float>(p, row, logp, kl, H, empty, writer);
@@ -456,14 +472,12 @@ __device__ __forceinline__ RowCoef row_coef(const LossArgs &p, long long row, fl
     return r;
 }
 
-// -c log2(e) rounded, and not as part of a multiply-add: the same everywhere
-__device__ __forceinline__ float minus_log2(float c) { return -__fmul_rn(c, kLog2e); }
-
-// t of a piece's logits kept relative to `base`, when the row's maximum is c (a part far below the rest: its probabilities
-// are 0, their logarithms kept finite)
+// t of a piece's logits kept relative to `base` (0, or the maximum of a part that is apart), when the row's maximum is c; far
+// below it probabilities are 0, and logarithms kept finite
+template <typename T>
 __device__ __forceinline__ float shift_of(float base, float c)
 {
-    return c == -INFINITY ? 0.f : base == 0.f ? minus_log2(c) : max_nan((base - c) * kLog2e, -1e30f);
+    return c == -INFINITY ? 0.f : base == 0.f ? minus_log2(c) : max_nan(fmaf(base - c, kLog2e, excess_of<T>(c)), -1e30f);
 }
 
 template <typename T, bool REF>
@@ -494,13 +508,12 @@ __device__ __forceinline__ void put_gradient(const LossArgs &p, T *g_row, int at
     float z[V], zr[V], g[V];
     unpack<T>(raw, z);
     if constexpr (REF) unpack<T>(raw_r, zr);
-    const float b0 = f.constant(sh, REF ? shr : 0.f), bz = f.kt * kLog2e, br = -f.kr * kLog2e;
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-        const float e = exp2_fast(fmaf(z[k], kLog2e, sh));
-        float b = fmaf(bz, z[k], b0);
-        if constexpr (REF) b = fmaf(br, zr[k], b);
-        g[k] = e * b;
+    for (int k = 0; k < V; ++k) {  // (t and t' once more: what is left of the coefficients' terms without their shifts would be off by the offset)
+        const float t = fmaf(z[k], kLog2e, sh);
+        float b = fmaf(f.kt, t, f.k0);
+        if constexpr (REF) b = fmaf(-f.kr, fmaf(zr[k], kLog2e, shr), b);
+        g[k] = exp2_fast(t) * b;
     }
     if ((unsigned)(a - at) < (unsigned)V) {
 #pragma unroll
@@ -511,9 +524,10 @@ __device__ __forceinline__ void put_gradient(const LossArgs &p, T *g_row, int at
 }
 
 // t of one logit in double, relative to what the sums of a row or part with maximum c are relative to
-__device__ __forceinline__ double t_of(float x, float c, float low)
+template <typename T>
+__device__ __forceinline__ double t_of(float x, float c)
 {
-    return x == -INFINITY ? (double)-INFINITY : c > low ? fma((double)x, (double)kLog2e, (double)shift_of(0.f, c)) : ((double)x - (double)c) * (double)kLog2e;
+    return x == -INFINITY ? (double)-INFINITY : apart<T>(c) ? ((double)x - (double)c) * (double)kLog2e : fma((double)x, (double)kLog2e, (double)minus_log2(c));
 }
 
 // the sums of elements begin, begin + step ... of an odd row or part: e, e t, e', e (t - t')
@@ -522,13 +536,13 @@ __device__ __forceinline__ void odd_sums(const T *z_row, const T *r_row, int beg
 {
     sum[0] = sum[1] = sum[2] = sum[3] = 0.0;
     for (int v = begin; v < end; v += step) {
-        const double t = t_of(to_float(z_row[v]), c, low_value<T>()), tr = t_of(to_float(r_row[v]), cr, low_value<T>());
-        const float e = exp2_fast((float)t);
+        const double t = t_of<T>(to_float(z_row[v]), c), tr = t_of<T>(to_float(r_row[v]), cr);
+        const double e = exp2(t);  // (what fp32 has no number for counts beside a logarithm of 1e38)
         sum[0] += e;
         sum[2] += exp2_fast((float)tr);
-        if (e != 0.f) {
-            sum[1] += (double)e * t;
-            sum[3] += (double)e * (t - tr);
+        if (e != 0.0) {
+            sum[1] += e * t;
+            sum[3] += e * (t - tr);
         }
     }
 }
@@ -557,27 +571,16 @@ __device__ __noinline__ bool odd_meets(const uint4 *z_s, const uint4 *r_s, const
     return false;
 }
 
-// the last of them, of a CTA's part: a warp's share
-template <typename T>
-__device__ __noinline__ double odd_part(const T *z_row, const T *r_row, int begin, int end, float c, float cr)
-{
-    double sum[4];
-    odd_sums(z_row, r_row, begin, end, (int)blockDim.x, c, cr, sum);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum[3] += __shfl_xor_sync(0xffffffffu, sum[3], o);
-    return sum[3];
-}
-
 // and their gradients (f: of the row)
 template <typename T>
 __device__ __noinline__ void odd_gradient(const T *z_row, const T *r_row, T *g_row, int begin, int end, int step, int a, const RowCoef &f)
 {
     for (int v = begin; v < end; v += step) {
-        const double t = t_of(to_float(z_row[v]), f.c, low_value<T>());
-        const float e = exp2_fast((float)t);
+        const double t = t_of<T>(to_float(z_row[v]), f.c);
+        const double e = exp2(t);
         double b = (double)f.k0 + (double)f.kt * t;
-        if (f.kr != 0.f) b -= (double)f.kr * t_of(to_float(r_row[v]), f.cr, low_value<T>());
-        g_row[v] = from_float<T>((e != 0.f ? (float)((double)e * b) : 0.f) + (v == a ? f.at_a : 0.f));
+        if (f.kr != 0.f) b -= (double)f.kr * t_of<T>(to_float(r_row[v]), f.cr);
+        g_row[v] = from_float<T>((e != 0.0 ? (float)(e * b) : 0.f) + (v == a ? f.at_a : 0.f));
     }
 }
 
@@ -604,8 +607,7 @@ __device__ __noinline__ void odd_row(const LossArgs &p, long long row, float w, 
     for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
-    const RowCoef f = row_coef<true>(p, row, w, a >= 0, za, C, CR, sum[0], sum[1], sum[2], sum[3],
-                                     excess_of(C <= low_value<T>() ? C : 0.f, C, shift_of(0.f, C)), lane == 0);
+    const RowCoef f = row_coef<true>(p, row, w, a >= 0, za, C, CR, sum[0], sum[1], sum[2], sum[3], excess_of<T>(C), lane == 0);
     if (p.grad) odd_gradient<T>(z_row, r_row, static_cast<T *>(p.grad) + row * p.ld_grad, lane, p.A, 32, a, f);
 }
 
@@ -645,7 +647,7 @@ __global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ?
     const uint32_t low_w = low_word<T>();
     float low[2];
     unpack_word(low_w, low, (const T *)nullptr);
-    // the maximum; -inf raised to the low value; pieces are relative to `base` (0 but where all lies at that value or below)
+    // the maximum; -inf raised to the low value; pieces are relative to `base` (0, or the maximum of a row that is apart)
     auto prepare = [&](auto &x, const T *x_row, float &base) {
         uint32_t m = low_w;
 #pragma unroll
@@ -659,7 +661,7 @@ __global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ?
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) c = max_nan(c, __shfl_xor_sync(0xffffffffu, c, o));
         base = 0.f;
-        if (c <= low[0]) {
+        if (apart<T>(c)) {
             c = -INFINITY;
             for (int v = lane; v < p.A; v += 32) c = fmaxf(c, to_float(x_row[v]));
 #pragma unroll
@@ -690,17 +692,18 @@ __global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ?
             for (int j = 0; j < 4; ++j) least = min_words<T>(least, words(raw_r[i])[j]);
         bool odd = false;
         if (word_min<T>(least) < low[0]) {
-            odd = C <= low[0];  // (what the policy's words stand for is not in them)
+            odd = apart<T>(C);  // (what the policy's words stand for is not in them)
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) odd |= meets<T>(words(raw[i])[j], words(raw_r[i])[j], low_w);
         }
-        if (__any_sync(0xffffffffu, odd)) return odd_row<T>(p, row, w, a, za);
+        odd = __any_sync(0xffffffffu, odd);
         CR = prepare(raw_r, r_row, base_r);
+        if (odd || too_high<T>(CR)) return odd_row<T>(p, row, w, a, za);
     }
     float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f;
-    float sh = shift_of(base, C), shr = shift_of(base_r, CR);
+    float sh = shift_of<T>(base, C), shr = shift_of<T>(base_r, CR);
 #pragma unroll
     for (int i = 0; i < NV; ++i) add_sums<T, REF>(raw[i], raw_r[REF ? i : 0], sh, shr, so, st, ss, sd);
 #pragma unroll
@@ -712,8 +715,9 @@ __global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ?
             sd += __shfl_xor_sync(0xffffffffu, sd, o);
         }
     }
-    const RowCoef f = row_coef<REF>(p, row, w, a >= 0, za, C, CR, so, st, CR == -INFINITY ? 0.0 : (double)ss, sd, excess_of(base, C, sh), lane == 0);
+    const RowCoef f = row_coef<REF>(p, row, w, a >= 0, za, C, CR, so, st, CR == -INFINITY ? 0.0 : (double)ss, sd, excess_of<T>(C), lane == 0);
     if (!g_row) return;
+    asm volatile("" : "+f"(sh), "+f"(shr));  // (t anew: kept from the sums it would take the registers that hold the row)
 #pragma unroll
     for (int i = 0; i < NV; ++i) put_gradient<T, REF>(p, g_row, first + i * step, a, raw[i], raw_r[REF ? i : 0], f, sh, shr);
 }
@@ -721,15 +725,53 @@ __global__ void __launch_bounds__(128, NV * (REF ? 2 : 1) <= 4 ? 6 : NV * (REF ?
 struct Partial {  // of one CTA: maxima, and sums relative to their shifts
     double so, st, ss, sd;
     float c, cr;
+    int rare;  // 1: odd; 2: odd if the whole row is masked
 };
 
-// what t of a part with maximum c lacks to t of the row, whose maximum is C (parts of the low value and below, and so rows,
-// are relative to their maxima themselves)
-__device__ __forceinline__ float rebase(float c, float C, float low) { return c > low ? shift_of(0.f, C) - shift_of(0.f, c) : (c - C) * kLog2e; }
-// what t - t' lacks (in double where the reference's part lies so low that its distance may be beyond fp32)
-__device__ __forceinline__ double rebase_difference(float d, float dr, const Partial &b, float CR, float low)
+// what t of a part with maximum c lacks to t of the row, whose maximum is C
+template <typename T>
+__device__ __forceinline__ float rebase(float c, float C) { return fmaf(c - C, kLog2e, excess_of<T>(C) - excess_of<T>(c)); }
+// A whole odd row by a cluster, elements begin .. end by this CTA.  `parts`: the CTAs' maxima, which all have read; `scratch`: of
+// the CTA, [kRowThreads / 32][4]; `coef`: of the CTA.
+constexpr int kMaxCluster = 16, kRowThreads = 256;
+template <typename T>
+__device__ __noinline__ void odd_cluster_row(const LossArgs &p, long long row, float w, int a, float za, int begin, int end, Partial *parts,
+                                             double *scratch, RowCoef *coef)
 {
-    return b.ss != 0.0 && b.cr <= low ? (double)d - ((double)b.cr - (double)CR) * (double)kLog2e : (double)(d - dr);
+    namespace cg = cooperative_groups;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
+    const int share = (int)cg::this_cluster().num_blocks(), rank = (int)cg::this_cluster().block_rank();
+    const T *z_row = static_cast<const T *>(p.logits) + row * p.ld, *r_row = static_cast<const T *>(p.ref) + row * p.ld_ref;
+    float C = -INFINITY, CR = -INFINITY;
+    for (int i = 0; i < share; ++i) {
+        C = max_nan(C, parts[i].c);
+        CR = max_nan(CR, parts[i].cr);
+    }
+    cg::this_cluster().sync();  // (the parts are written again)
+    double sum[4];
+    odd_sums(z_row, r_row, begin + (int)threadIdx.x, end, (int)blockDim.x, C, CR, sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+    if (lane < 4) scratch[4 * warp + lane] = lane == 0 ? sum[0] : lane == 1 ? sum[1] : lane == 2 ? sum[2] : sum[3];
+    __syncthreads();
+    if ((int)threadIdx.x < share) {
+        double v[4] = {};
+        for (int i = 0; i < warps; ++i)
+            for (int k = 0; k < 4; ++k) v[k] += scratch[4 * i + k];
+        Partial *to = cg::this_cluster().map_shared_rank(&parts[rank], threadIdx.x);
+        to->so = v[0], to->st = v[1], to->ss = v[2], to->sd = v[3];
+    }
+    cg::this_cluster().sync();
+    if (threadIdx.x == 0) {
+        double v[4] = {};
+        for (int i = 0; i < share; ++i) v[0] += parts[i].so, v[1] += parts[i].st, v[2] += parts[i].ss, v[3] += parts[i].sd;
+        *coef = row_coef<true>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], excess_of<T>(C), rank == 0);
+    }
+    __syncthreads();
+    if (p.grad)
+        odd_gradient<T>(z_row, r_row, static_cast<T *>(p.grad) + row * p.ld_grad, begin + (int)threadIdx.x, end, (int)blockDim.x, a, *coef);
 }
 
 // Longer rows: the CTAs of a cluster share a row (one CTA up to 72 KB of it, the reference's included), each keeps its part in
@@ -740,7 +782,6 @@ __device__ __forceinline__ double rebase_difference(float d, float dr, const Par
 // finite and the maximum found two 16-bit logits at a time, t is one multiply-add of the logit, and what depends on the row
 // only is worked out by one warp.  Sums of a warp are float, from there on double.  4096 rows of 49999 bf16: 171 to 177 us,
 // 4.7 TB/s; 2048 of 128001 with a reference: 497 us.
-constexpr int kMaxCluster = 16, kRowThreads = 256;
 template <typename T, bool REF>
 __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_constant__ LossArgs p)
 {
@@ -749,10 +790,9 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
     __shared__ Partial parts[kMaxCluster];
     __shared__ float4 s_sum[kRowThreads / 32];
     __shared__ float s_max[2][kRowThreads / 32];
-    __shared__ double s_odd[kRowThreads / 32];
     __shared__ RowCoef s_row;
     __shared__ uint64_t s_bar;
-    __shared__ int s_abort;
+    __shared__ int s_abort, s_odd;
     namespace cg = cooperative_groups;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
     const int share = (int)cg::this_cluster().num_blocks(), rank = (int)cg::this_cluster().block_rank();
@@ -838,7 +878,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
         for (int o = kRowThreads / 64; o > 0; o >>= 1) c = max_nan(c, __shfl_xor_sync(0xffffffffu, c, o));
         return c;
     };
-    // a part with nothing above the low value: read again, relative to its own maximum (returned; -inf: no logit)
+    // a part that is apart: read again, relative to its own maximum (returned; -inf: no logit)
     auto low_part = [&](uint4 *x_s, const T *x_row, int which) {
         float c = -INFINITY;
         for (int v = max(first, 0) + (int)threadIdx.x; v < min(first + n * V, p.A); v += blockDim.x) c = fmaxf(c, to_float(x_row[v]));
@@ -862,25 +902,24 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
     if (REF) prepare(r_s, 1);
     odd = __syncthreads_or(odd);
     float c = block_max(0), cr = REF ? block_max(1) : -INFINITY, base = 0.f, base_r = 0.f;
-    if (c <= low[0]) {
+    // (entries masked in both arrays: what the policy's words stood for was not in them, but it counts only if the whole row is
+    // like that, which the CTAs learn from one another)
+    int rare = 0;
+    if (apart<T>(c)) {
+        if (REF && __syncthreads_or(lower && is_below<T>(c))) rare = 2;
         c = low_part(z_s, z_row, 0);
         base = c == -INFINITY ? 0.f : c;
-        if (REF) odd = __syncthreads_or(lower);  // (what the policy's words stood for was not in them)
     }
-    if (REF && cr <= low[0]) {
+    if (REF && (odd || too_high<T>(cr))) rare = 1;
+    if (REF && apart<T>(cr)) {
         cr = low_part(r_s, r_row, 1);
         base_r = cr == -INFINITY ? 0.f : cr;
     }
     float so = 0.f, st = 0.f, ss = 0.f, sd = 0.f;
     {
-        const float sh = shift_of(base, c), shr = shift_of(base_r, cr);
+        const float sh = shift_of<T>(base, c), shr = shift_of<T>(base_r, cr);
 #pragma unroll 2
         for (int j = threadIdx.x; j < n; j += blockDim.x) add_sums<T, REF>(z_s[j], r_s[j], sh, shr, so, st, ss, sd);
-    }
-    const int from = max(first, 0) + (int)threadIdx.x, end = min(first + n * V, p.A);
-    if (REF && odd) {
-        const double sum = odd_part(z_row, r_row, from, end, c, cr);
-        if (lane == 0) s_odd[warp] = sum;
     }
     float sums[4] = {so, st, ss, sd};
 #pragma unroll
@@ -894,7 +933,6 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
         Partial mine;
         const float4 part = lane < warps ? s_sum[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
         double v[4] = {part.x, part.y, part.z, part.w};
-        if (REF && odd) v[3] = lane < warps ? s_odd[lane] : 0.0;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -905,6 +943,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
         mine.sd = c == -INFINITY ? 0.0 : v[3];
         mine.c = c;
         mine.cr = cr;
+        mine.rare = rare;
         if (lane < share) *cg::this_cluster().map_shared_rank(&parts[rank], lane) = mine;
     }
     cg::this_cluster().sync();
@@ -921,26 +960,38 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
             CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
         }
         // a part's sums, relative to the row's shifts (as the gradient takes them) instead of its own
-        const float d = b.so != 0.0 ? rebase(b.c, C, low[0]) : 0.f, dr = b.ss != 0.0 ? rebase(b.cr, CR, low[0]) : 0.f;
-        const double f = (double)exp2f(d), df = (double)d, dd = rebase_difference(d, dr, b, CR, low[0]);
+        const float d = b.so != 0.0 ? rebase<T>(b.c, C) : 0.f, dr = b.ss != 0.0 ? rebase<T>(b.cr, CR) : 0.f;
+        const double f = (double)exp2f(d), df = (double)d, dd = (double)(d - dr);
         double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, (double)exp2f(dr) * b.ss, f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int o = kMaxCluster / 2; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        const RowCoef r = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], excess_of(C <= low[0] ? C : 0.f, C, shift_of(0.f, C)),
-                                          rank == 0 && lane == 0);
-        if (lane == 0) s_row = r;
+        // (the vote is of all lanes; those from 16 on have no part, and another C)
+        const int any = REF ? __reduce_or_sync(0xffffffffu, b.rare) : 0;
+        if (REF && lane == 0) s_odd = (any & 1) || (any && is_below<T>(C));
+        if (!any || !((any & 1) || is_below<T>(C))) {
+            const RowCoef r = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], excess_of<T>(C), rank == 0 && lane == 0);
+            if (lane == 0) s_row = r;
+        }
     }
     __syncthreads();
+    if (REF && s_odd)  // (the same in every CTA of the cluster)
+        return odd_cluster_row<T>(p, row, w, a, za, max(first, 0), min(first + n * V, p.A), parts, reinterpret_cast<double *>(s_piece), &s_row);
     if (g_row) {
-        const RowCoef f = s_row;
-        if (REF && odd) {
-            odd_gradient(z_row, r_row, g_row, from, end, (int)blockDim.x, a, s_row);
+        RowCoef f = s_row;
+        float sh = shift_of<T>(base, f.c), shr = shift_of<T>(base_r, f.cr);
+        if (base == 0.f && apart<T>(f.c)) {  // a part that is not in a row that is
+            if (c == -INFINITY) {
+                sh = -1e30f;  // (no logit here)
+            } else {  // (far up: what the shift is off by where the part's logits are near enough to matter)
+                const float scale = exp2f(-fminf(fmaxf(fmaf(f.c, kLog2e, sh), -4.f), 4.f));
+                f.k0 *= scale, f.kt *= scale, f.kr *= scale;
+            }
         }
-        const float sh = shift_of(base, f.c), shr = shift_of(base_r, f.cr);
+        if (REF && (f.kr == 0.f || (base_r == 0.f && is_below<T>(f.cr)))) shr = 0.f;  // (it does not count; no logit here, and the policy's are masked)
 #pragma unroll 2
-        for (int j = REF && odd ? n : (int)threadIdx.x; j < n; j += blockDim.x) put_gradient<T, REF>(p, g_row, first + j * V, a, z_s[j], r_s[j], f, sh, shr);
+        for (int j = threadIdx.x; j < n; j += blockDim.x) put_gradient<T, REF>(p, g_row, first + j * V, a, z_s[j], r_s[j], f, sh, shr);
     }
     if (s_abort)
         for (int i = 0; i < 200; ++i) __nanosleep(1000);  // copies still in flight land first
@@ -1062,12 +1113,12 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                     }
                 }
                 const float top = word_max<T>(m);
-                if (top > c) {
-                    const float to = minus_log2(top), d = so != 0.f ? to - nc : 0.f, f = exp2_fast(d);
+                if (!(top <= c)) {  // (a NaN too)
+                    c = max_nan(c, top);
+                    const float to = minus_log2(c), d = so != 0.f ? to - nc : 0.f, f = exp2_fast(d);
                     st = f * (st + d * so);
                     sd = f * (sd + d * so);
                     so *= f;
-                    c = top;
                     nc = to;
                 }
                 if constexpr (REF) {
@@ -1076,11 +1127,11 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                         for (int i = 0; i < 4; ++i) meet |= meets<T>(words(raw)[i], words(was)[i], low_w);
                     }
                     const float top_r = word_max<T>(mr);
-                    if (top_r > cr) {
-                        const float to = minus_log2(top_r);
+                    if (!(top_r <= cr)) {
+                        cr = max_nan(cr, top_r);
+                        const float to = minus_log2(cr);
                         sd -= (to - ncr) * so;
                         ss *= exp2_fast(ss != 0.f ? to - ncr : 0.f);
-                        cr = top_r;
                         ncr = to;
                     }
                 }
@@ -1096,7 +1147,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 for (int h = 0; h < kStreamPer; ++h)
                     if (j + h * kStreamThreads < w1) take(at[h * kStreamThreads], at[kStreamPieces + h * kStreamThreads]);
                 // (always so; it waits for the values to be in every lane's registers, not merely asked for)
-                if (__all_sync(0xffffffffu, c >= low[0] && cr >= low[0]) && lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
+                if (__all_sync(0xffffffffu, !(c < low[0]) && !(cr < low[0])) && lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
                 next();
             }
             // a warp's sums, relative to its maxima
@@ -1133,9 +1184,9 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 C = max_nan(C, __shfl_xor_sync(0xffffffffu, C, o));
                 CR = max_nan(CR, __shfl_xor_sync(0xffffffffu, CR, o));
             }
-            // Nothing above the low value in one of the rows (masks of the type's lowest value only, or none left at all), or
-            // the reference below it where the policy is not: the row is done from memory, value by value.
-            const bool odd = C <= low[0] || (REF && (CR <= low[0] || s_odd));
+            // One of the rows far from 0 (masks of the type's lowest value only, or none left at all), a broken reference, or the
+            // reference below the low value where the policy is not: the row is done from memory, value by value.
+            const bool odd = apart<T>(C) || is_below<T>(CR) || too_high<T>(CR) || s_odd;
             if (odd) {
                 C = CR = -INFINITY;
                 for (int v = threadIdx.x; v < p.A; v += kStreamThreads) {
@@ -1168,16 +1219,15 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             }
             if (warp == 0) {
                 const Partial b = s_part[lane % kStreamWarps];
-                const float d = b.so != 0.0 ? rebase(b.c, C, low[0]) : 0.f, dr = b.ss != 0.0 ? rebase(b.cr, CR, low[0]) : 0.f;
-                const double f = lane < kStreamWarps ? (double)exp2f(d) : 0.0, df = (double)d, dd = rebase_difference(d, dr, b, CR, low[0]);
+                const float d = b.so != 0.0 ? rebase<T>(b.c, C) : 0.f, dr = b.ss != 0.0 ? rebase<T>(b.cr, CR) : 0.f;
+                const double f = lane < kStreamWarps ? (double)exp2f(d) : 0.0, df = (double)d, dd = (double)(d - dr);
                 double v[4] = {f * b.so, f != 0.0 ? f * (b.st + df * b.so) : 0.0, lane < kStreamWarps ? (double)exp2f(dr) * b.ss : 0.0,
                                f != 0.0 ? f * (b.sd + dd * b.so) : 0.0};
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-                const RowCoef f0 = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], excess_of(C <= low[0] ? C : 0.f, C, shift_of(0.f, C)),
-                                                   lane == 0);
+                const RowCoef f0 = row_coef<REF>(p, row, w, a >= 0, za, C, CR, v[0], v[1], v[2], v[3], excess_of<T>(C), lane == 0);
                 if (lane == 0) {
                     s_row = f0;
                     if (s_odd) s_odd = 0;  // (then every warp has come past two barriers since it looked)
@@ -1186,7 +1236,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             all();
             if (!g_row) continue;
             const RowCoef f = s_row;
-            const float sh = shift_of(0.f, f.c), shr = shift_of(0.f, f.cr);
+            const float sh = shift_of<T>(0.f, f.c), shr = shift_of<T>(0.f, f.cr);
             if (!odd && ragged != INT_MIN) {
                 uint4 raw = load_piece<T>(z_row, ragged, p.A, low[0]), raw_r = load_piece<T>(r_row, ragged, p.A, low[0]);
                 raise(raw);

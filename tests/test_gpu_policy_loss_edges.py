@@ -254,3 +254,70 @@ def test_streamed_rows_of_which_l2_does_not_hold_all(dtype, t, v):
         torch.testing.assert_close(out[k][-40:], other[k], rtol=8e-6, atol=2e-5)
     assert torch.equal(loss(s, grad=s["z"], kl_coef=0.05, entropy_coef=0.02)["grad"], out["grad"])
     P.device_check()
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("mask", [-1e4, -1e9, -1e10, -1e20])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_masks_that_are_added(t, v, mask, dtype):
+    """A third of every row lies around `mask` in both arrays (parts of a row hold nothing else), some rows lie there whole, or
+    as far up; rounded shifts of such parts are off by up to 2^39."""
+    dt = TYPES[dtype]
+    s = inputs(t, v, dt, v + 8)
+    s["w"][:] = 0.5
+    s["a"][:] = 0
+    third = max(1, v // 3)
+    for x in ("z", "zr"):
+        s[x][:, -third:] = (s[x][:, -third:].float() + mask).to(dt)
+        s[x][1] = (s[x][1].float() + mask).to(dt)
+        s[x][2] = (s[x][2].float().clamp(min=-8) - 2 * mask).to(dt)
+        s[x][3, 1:] = (s[x][3, 1:].float() + mask).to(dt)
+    lp = torch.log_softmax(s["z"].double(), 1)[:, 0]
+    s["logp_old"] = (lp.clamp(min=-30) + 0.1).float()
+    s["logp_ref"] = (lp.clamp(min=-30) - 0.1).float()
+    rows = [i for i in range(8) if float(lp[i]) > -1e5]  # (an action that a row's mask takes away has a log-prob near `mask`)
+    for ref in ("none", "logits"):
+        out = loss(s, ref=ref, kl_coef=0.05, entropy_coef=0.02)
+        assert torch.isfinite(out["grad"]).all() and torch.isfinite(out["stats"]).all()
+        part = {k: x[rows] for k, x in s.items()}
+        sub = {k: (x[rows] if x is not None and x.shape[0] == t else x) for k, x in out.items()}
+        sub["stats"] = None
+        want = definition(part["z"], part["a"], part["logp_old"], part["adv"], part["w"], part["zr"] if ref == "logits" else None,
+                          kl_coef=0.05, entropy_coef=0.02)
+        want["z"] = part["z"].double().cpu()
+        want["onehot"] = torch.nn.functional.one_hot(part["a"].long().cpu(), v).double()
+        sub["stats"], want["stats"] = torch.zeros(8), torch.zeros(8, dtype=torch.float64)
+        check(sub, want, dt, scale_of(part))
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("offset", [1e4, -1e5, 1e6, -2e7, 4e7, -1e9])
+def test_gradients_do_not_depend_on_the_logits_offset(t, v, offset):
+    """fp32 rows far from 0, on both sides of where they are kept relative to their maximum (a step of fp32 there is up to 64)."""
+    s = inputs(t, v, torch.float32, v + 9)
+    for x in ("z", "zr"):
+        s[x].copy_(s[x] + offset)
+    lp = torch.log_softmax(s["z"][:16].double(), 1).gather(1, s["a"][:16, None])[:, 0]
+    s["logp_old"][:16] = (lp.clamp(min=-30) + 0.1).float()
+    s["w"][1] = 1.0
+    rows = [i for i in range(min(t, 16)) if float(lp[i]) > -40]
+    s = {k: torch.cat([x[rows], x[len(rows):]]) for k, x in s.items()}
+    for ref in ("none", "logits"):
+        out = loss(s, ref=ref, kl_coef=0.5, entropy_coef=0.5)
+        against_definition(s, out, torch.float32, ref=ref, rows=len(rows), kl_coef=0.5, entropy_coef=0.5)
+
+
+@pytest.mark.parametrize("t,v", WIDTHS)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_broken_reference_that_is_only_watched(t, v, dtype):
+    """NaN and infinities in the reference, kl_coef 0: its KL is not finite, the gradient is the loss's without it."""
+    s = inputs(t, v, TYPES[dtype], v + 10)
+    s["w"][:] = 0.5
+    s["zr"][1, 2], s["zr"][2, v - 1], s["zr"][3, :], s["zr"][4, v // 2] = math.nan, math.nan, math.nan, math.inf
+    out = loss(s, kl_coef=0.0, entropy_coef=0.02)
+    assert torch.isnan(out["kl"][1:4]).all() and not torch.isfinite(out["kl"][4]) and torch.isfinite(out["kl"][5:]).all()
+    alone = loss(s, ref="none", kl_coef=0.0, entropy_coef=0.02)
+    half = torch.finfo(TYPES[dtype]).eps
+    torch.testing.assert_close(out["grad"].float(), alone["grad"].float(), rtol=2 * half, atol=1e-6)
+    broken = loss(s, kl_coef=0.05, entropy_coef=0.02)
+    assert torch.isnan(broken["grad"][1]).any() and torch.isnan(broken["grad"][3]).any() and torch.isfinite(broken["grad"][5:]).all()
