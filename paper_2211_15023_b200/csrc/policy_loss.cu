@@ -937,6 +937,10 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int o = kRowThreads / 64; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        if (share > kRowThreads / 32) {  // (the sums are in the lanes that have a warp each; a lane sends to each CTA)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], lane % (kRowThreads / 32));
+        }
         mine.so = c == -INFINITY ? 0.0 : v[0];
         mine.st = c == -INFINITY ? 0.0 : v[1];
         mine.ss = cr == -INFINITY ? 0.0 : v[2];

@@ -38,6 +38,7 @@ def against_definition(s, out, dtype, ref="logits", rows=16, **kw):
     if s["z"].shape[0] > rows:
         got["stats"], want["stats"] = torch.zeros(8), torch.zeros(8, dtype=torch.float64)
     check(got, want, dtype, scale_of(part))
+    assert not torch.isnan(got["grad"].cpu()[~torch.isnan(want["grad"])]).any()
     return want
 
 
@@ -288,6 +289,7 @@ def test_masks_that_are_added(t, v, mask, dtype):
         want["onehot"] = torch.nn.functional.one_hot(part["a"].long().cpu(), v).double()
         sub["stats"], want["stats"] = torch.zeros(8), torch.zeros(8, dtype=torch.float64)
         check(sub, want, dt, scale_of(part))
+        assert not torch.isnan(sub["grad"]).any()
 
 
 @pytest.mark.parametrize("t,v", WIDTHS)
@@ -321,3 +323,17 @@ def test_a_broken_reference_that_is_only_watched(t, v, dtype):
     torch.testing.assert_close(out["grad"].float(), alone["grad"].float(), rtol=2 * half, atol=1e-6)
     broken = loss(s, kl_coef=0.05, entropy_coef=0.02)
     assert torch.isnan(broken["grad"][1]).any() and torch.isnan(broken["grad"][3]).any() and torch.isfinite(broken["grad"][5:]).all()
+
+
+@pytest.mark.parametrize("dtype,t,v", [("fp32", 4, 80001), ("fp32", 40, 129830), ("fp32", 147, 77465), ("fp32", 2, 262128), ("bf16", 3, 150001),
+                                       ("fp16", 2, 262128)])
+@pytest.mark.parametrize("ref", ["none", "logp", "logits"])
+def test_every_part_of_a_row_has_a_gradient(dtype, t, v, ref):
+    """Rows that are split over up to sixteen CTAs, by the definition; no part without one."""
+    s = inputs(t, v, TYPES[dtype], v)
+    s["w"][:] = 0.5
+    out = loss(s, ref=ref, kl_coef=0.05, entropy_coef=0.02)
+    assert torch.isfinite(out["grad"]).all()
+    against_definition(s, out, TYPES[dtype], ref=ref, rows=4, kl_coef=0.05, entropy_coef=0.02)
+    sixteenths = out["grad"][0].float().abs().tensor_split(16)
+    assert all(float(x.max()) > 0 for x in sixteenths)
