@@ -20,6 +20,7 @@ def test_dw_is_the_same_whether_db_is_wanted(t, n, k, out):
     alone, none = P.ckpt_weight_grad(dy, ckpt, k, out_dtype=TYPES[out], bias=False)
     P.device_check()
     assert none is None and torch.equal(dw, alone)
+    assert torch.isfinite(dw).all() and torch.isfinite(db).all()
     want, mag = sums(dy, ckpt, k)
     check((dw, db), want, mag, TYPES[out])
 
