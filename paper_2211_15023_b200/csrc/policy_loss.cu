@@ -1006,7 +1006,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) loss_rows_kernel(const __grid_
 // gradient.  The second time it comes from L2, as far as that holds the rows of all CTAs.  Against
 // the kernel above a row's end (barriers, one warp's arithmetic: some 2 us in which an SM does little else) comes once for
 // a whole row instead of once for an eighth of one, and the loads of what follows go on meanwhile: 497 -> 414 us for
-// 2048 rows of 128001.  It is bound by the instructions a pair of logits (some 33; 16 warps instead of 24: 492 us), so every
+// 2048 rows of 128001.  It is bound by the instructions a pair of logits (some 34; 16 warps instead of 24: 492 us), so every
 // thread keeps a maximum of its own and rebases its sums when it rises.  Without a reference, which halves them, the
 // kernel above is no slower.
 constexpr int kStreamWarps = 24, kStreamThreads = 32 * kStreamWarps, kStreamPer = 2, kStreamStages = 4;
@@ -1117,8 +1117,8 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                     }
                 }
                 const float top = word_max<T>(m);
-                if (!(top <= c)) {  // (a NaN too)
-                    c = max_nan(c, top);
+                if (top > c) {
+                    c = top;
                     const float to = minus_log2(c), d = so != 0.f ? to - nc : 0.f, f = exp2_fast(d);
                     st = f * (st + d * so);
                     sd = f * (sd + d * so);
@@ -1131,8 +1131,8 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                         for (int i = 0; i < 4; ++i) meet |= meets<T>(words(raw)[i], words(was)[i], low_w);
                     }
                     const float top_r = word_max<T>(mr);
-                    if (!(top_r <= cr)) {
-                        cr = max_nan(cr, top_r);
+                    if (top_r > cr) {
+                        cr = top_r;
                         const float to = minus_log2(cr);
                         sd -= (to - ncr) * so;
                         ss *= exp2_fast(ss != 0.f ? to - ncr : 0.f);
@@ -1151,7 +1151,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
                 for (int h = 0; h < kStreamPer; ++h)
                     if (j + h * kStreamThreads < w1) take(at[h * kStreamThreads], at[kStreamPieces + h * kStreamThreads]);
                 // (always so; it waits for the values to be in every lane's registers, not merely asked for)
-                if (__all_sync(0xffffffffu, !(c < low[0]) && !(cr < low[0])) && lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
+                if (__all_sync(0xffffffffu, c >= low[0] && cr >= low[0]) && lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
                 next();
             }
             // a warp's sums, relative to its maxima
@@ -1180,7 +1180,7 @@ __global__ void __launch_bounds__(kStreamThreads + 32, 1) loss_stream_kernel(con
             }
             s.so = so, s.st = st, s.ss = ss, s.sd = sd;
             if (lane == 0) s_part[warp] = s;
-            if (meet) s_odd = 1;
+            if (meet || ss != ss) s_odd = 1;  // (a NaN passes by the maximum, not by the sum)
             all();
             float C = s_part[lane % kStreamWarps].c, CR = s_part[lane % kStreamWarps].cr;
 #pragma unroll
