@@ -464,7 +464,9 @@ typedef enum { ACCERL_F32 = 0, ACCERL_BF16 = 1, ACCERL_F16 = 2 } accerl_dtype;
  * A row of weight 0 is not read: its grad, logp, kl and entropy are 0, whatever its arrays hold.  A logit of
  * -inf has probability 0, takes no part in the sums and gets gradient 0; a row that has no other logits counts
  * as loss 0 and gets gradient 0 and logp -inf.  Where p_v > 0 = q_v the KL is infinite and the gradient is not
- * finite.  An action outside 0..n_actions-1 makes its row NaN.
+ * finite, unless kl_coef is 0 (a KL, or an estimate of it, that is only watched does not reach the loss or the gradient).  Logits of
+ * any finite size count as they are, masks of the type's lowest value among them; where w kl_coef kl goes beyond fp32 the
+ * gradient is not finite.  An action outside 0..n_actions-1 makes its row NaN.
  */
 typedef struct {
     const void *logits;      /* [rows][n_actions] of `dtype` */
@@ -501,7 +503,7 @@ accerl_status accerl_policy_loss(const accerl_policy_loss_args *args, void *cuda
  * with products of the exact 16-bit values and sums in fp32, in an order that depends on the sizes alone (the same
  * call gives the same bits, and dw's are the same whether db is wanted), rounded once to out_dtype.  `accumulate`: added to what dw and db hold (out_dtype
  * ACCERL_F32 only), as a sum over micro-batches needs it.  With ACCERL_F16 gradients x^ is taken as fp16: beyond its
- * range it is infinite.  Needs bf16 or fp16 dy.
+ * range it is infinite (and 2^128, what bf16's largest is kept as, in bf16).  Needs bf16 or fp16 dy.
  */
 typedef struct {
     const void *dy;   /* [tokens][n] of dy_dtype (ACCERL_BF16 or ACCERL_F16) */
